@@ -32,6 +32,8 @@ constexpr int kLightBin = kNumBins;      // how the row count marks them
 // tile list that the dense symbolic kernel plans exists for every row the dense numeric kernel sees.
 static_assert(kSymHashLarge <= kNumHashLarge, "dense numeric rows need a dense symbolic pass");
 
+constexpr int kDirectMinDefault = 6144;  // a block with at least this many entries becomes a direct tile
+
 // Control block shared by host and device (one small device allocation per plan).
 struct Control {
   unsigned hist[2][kNumBins];     // [0] symbolic, [1] numeric: rows per bin

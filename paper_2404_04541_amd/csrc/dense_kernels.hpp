@@ -44,7 +44,6 @@ constexpr int kTileBudget = 66 * 1024; // LDS bytes of one numeric tile (flags +
 constexpr int kWideTileBudget = 135 * 1024;   // ... of a wide one: one workgroup (wide_tiles_from says which products)
 constexpr int kRankBlkBytes = kBlkCols / 32 * 8;   // flag word + rank per 32 columns of a ranked tile
 constexpr int kRankEntryBytes = 8;                // sum per entry of a ranked tile (its column goes straight to C)
-constexpr int kDirectMinDefault = 6144; // a block with at least this many entries becomes a direct tile
 constexpr int kRunTiles = 16;           // tiles handed to a workgroup at a time
 constexpr int kListSlab = 1 << 20;      // list entries and tile records that a symbolic workgroup draws at a time
 constexpr int kTileSlab = 512;

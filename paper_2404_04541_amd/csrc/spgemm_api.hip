@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "common.hpp"
+#include "context.hpp"
 #include "entry_order.hpp"
 #include "plan_room.hpp"
 #include "setup_kernels.hpp"
@@ -37,88 +38,6 @@ static_assert(num_wide_lds<double>() <= 160 * 1024, "numeric dense kernel exceed
 static_assert(sym_dense_lds<16, 1024>(kSymFlagWords) <= 160 * 1024, "symbolic dense kernel exceeds LDS");
 static_assert(sym_dense_lds<16, 512>(kSymNarrowCols / 32) <= 80 * 1024 && sym_dense_lds<16, 1024>(kSymShortCols / 32) <= 80 * 1024 && num_tiles_lds<double>() <= 80 * 1024, "two workgroups on a compute unit");
 static_assert(staged_lds<double>() <= 160 * 1024 && staged_lds<float>() <= 160 * 1024, "staged kernel exceeds LDS");
-
-// Pinned host memory where kernels leave numbers for the host (the symbolic ones the control block).  Allocating and releasing it costs 50 to
-// 300 us, so a few blocks wait for the next calls; a call holds its own from before its first kernel until its stream has been
-// waited for, whatever handle, stream or thread it comes from: the lease itself waits where the call returns before it has (an
-// allocation that is refused while kernels are on their way).
-namespace {
-
-class PinnedBlocks {
- public:
-  Control* take() {
-    {
-      std::lock_guard<std::mutex> lock(mutex_);
-      if (n_ > 0) return free_[--n_];
-    }
-    void* p = nullptr;
-    if (hipHostMalloc(&p, sizeof(Control), hipHostMallocPortable) == hipSuccess) return static_cast<Control*>(p);
-    (void)hipGetLastError();
-    return nullptr;
-  }
-  void give(Control* p) {
-    {
-      std::lock_guard<std::mutex> lock(mutex_);
-      if (n_ < kKeep) { free_[n_++] = p; return; }
-    }
-    (void)hipHostFree(p);
-  }
-
- private:
-  static constexpr int kKeep = 16;
-  std::mutex mutex_;
-  Control* free_[kKeep] = {};
-  int n_ = 0;
-};
-PinnedBlocks g_pinned;
-
-struct PinnedLease {
-  Control* p;
-  explicit PinnedLease(hipStream_t stream) : p(g_pinned.take()), stream_(stream) {}
-  ~PinnedLease() {
-    if (!p) return;
-    if (written_) (void)hipStreamSynchronize(stream_);
-    g_pinned.give(p);
-  }
-  void written() { written_ = true; }   // kernels that write to the block are about to be launched
-  void waited() { written_ = false; }   // and all of them are done
-  PinnedLease(const PinnedLease&) = delete;
-  PinnedLease& operator=(const PinnedLease&) = delete;
-
- private:
-  hipStream_t stream_;
-  bool written_ = false;
-};
-
-}  // namespace
-
-struct TimedLaunch {
-  int cls;
-  hipEvent_t start, stop;
-};
-
-struct spgemm_context {
-  hipStream_t stream = nullptr;
-  spgemm_allocator alloc{};
-  bool has_alloc = false;
-  int timing = 0;
-  int force = 0;
-  int direct_min = kDirectMinDefault;
-  int64_t col_list = 1;   // 0 off, 1 automatic size, larger: byte limit
-  int block_table = 1;    // 0: never build the block-offset table of B (pieces are bisected)
-  int64_t merge_limit = 0xffffffffLL;   // components of the outer product's all array and a batch together: fewer
-  int search_ratio = 4;   // searched tiles for rows with at most this many products per entry (0: never)
-  int row_block = 0;      // 1: A is a block of rows of a larger matrix (row pointer values are that matrix's positions)
-  double whole_ip = 0;    // ... and the products of all its rows
-  std::string err = "";
-  bool device_ready = false;
-  bool big_lds_ready = false;
-  int num_cus = 0;
-  std::vector<TimedLaunch> timed;        // launches of the phase in flight
-  std::vector<hipEvent_t> event_pool;
-  hipStream_t second = nullptr;   // of spgemm_pipelined, and the device it is on: made when first wanted, released with the handle
-  int second_device = -1;
-};
 
 struct spgemm_plan_s {
   spgemm_context* h = nullptr;
@@ -166,18 +85,6 @@ struct spgemm_plan_s {
 
 namespace {
 
-int fail(spgemm_context* h, int code, const std::string& msg) {
-  if (h) h->err = msg;
-  return code;
-}
-
-#define HIP_TRY(h, expr)                                                                 \
-  do {                                                                                   \
-    hipError_t e_ = (expr);                                                              \
-    if (e_ != hipSuccess)                                                                \
-      return fail((h), SPGEMM_HIP_ERROR, std::string(#expr) + ": " + hipGetErrorString(e_)); \
-  } while (0)
-
 int check_csr(spgemm_context* h, const spgemm_csr* M, const char* name) {
   if (!M) return fail(h, SPGEMM_INVALID_ARG, std::string(name) + " is null");
   if (M->rows < 0 || M->cols < 0 || M->nnz < 0) return fail(h, SPGEMM_INVALID_ARG, std::string(name) + ": negative size");
@@ -196,39 +103,6 @@ int check_pair(spgemm_context* h, const spgemm_csr* A, const spgemm_csr* B) {
   if (rc) return rc;
   if (A->cols != B->rows) return fail(h, SPGEMM_DIM_MISMATCH, "A.cols != B.rows");
   if (A->dtype != B->dtype) return fail(h, SPGEMM_DTYPE_MISMATCH, "A and B value types differ");
-  return SPGEMM_OK;
-}
-
-void* dev_alloc(spgemm_context* h, size_t bytes) {
-  if (bytes == 0) bytes = 256;
-  if (h->has_alloc) return h->alloc.alloc(h->alloc.ctx, bytes);
-  void* p = nullptr;
-  if (hipMalloc(&p, bytes) == hipSuccess) return p;
-  (void)hipGetLastError();   // (the thread's last error stays until it is asked for: a call that goes on without would find it behind its kernels)
-  return nullptr;
-}
-
-void dev_free(spgemm_context* h, void* p) {
-  if (!p) return;
-  if (h->has_alloc) h->alloc.free(h->alloc.ctx, p);
-  else (void)hipFree(p);
-}
-
-template <typename K>
-int allow_lds(spgemm_context* h, K kernel, size_t bytes) {
-  HIP_TRY(h, hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-  return SPGEMM_OK;
-}
-
-int ensure_device(spgemm_context* h) {
-  if (h->device_ready) return SPGEMM_OK;
-  int dev = 0;
-  HIP_TRY(h, hipGetDevice(&dev));
-  hipDeviceProp_t prop;
-  HIP_TRY(h, hipGetDeviceProperties(&prop, dev));
-  if (prop.warpSize != kWave) return fail(h, SPGEMM_UNSUPPORTED, "device is not wave64");
-  h->num_cus = prop.multiProcessorCount > 0 ? prop.multiProcessorCount : 256;
-  h->device_ready = true;
   return SPGEMM_OK;
 }
 
@@ -315,8 +189,6 @@ void drop_timed(spgemm_context* h) {
   h->timed.clear();
 }
 
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 inline unsigned grid_for(int64_t items, int64_t per_block, int64_t cap) {
   int64_t g = ceil_div(items > 0 ? items : 1, per_block);
   if (g > cap) g = cap;
@@ -337,8 +209,6 @@ constexpr int64_t kFlagMaxNnz = int64_t(1) << 20;
 // products, both phases, us sorted list | flags: 500 rows 10.8 | 12.4, 2000 11.0 | 12.2, 4000 13.2 | 13.1, 8000 17.9 | 14.8, 32 000 44.8 | 26.6.
 constexpr int64_t kFlagMinRows = 4096;
 constexpr size_t kAskFreeAbove = (size_t)64 << 20;   // optional memory below this is taken without asking the device what it has free
-
-size_t align_up(size_t v) { return (v + 255) & ~(size_t)255; }
 
 // Whether the rows of classes 0 and 1 take the flag-list workspace (flag_kernels.hpp) instead of the sorted list, where there are
 // kFlagMinRows of them.
@@ -1052,6 +922,10 @@ int spgemm_destroy(spgemm_handle h) {
   for (auto e : h->event_pool) (void)hipEventDestroy(e);
   for (auto& t : h->timed) { (void)hipEventDestroy(t.start); (void)hipEventDestroy(t.stop); }
   if (h->second) (void)hipStreamDestroy(h->second);
+  if (h->work) {
+    (void)hipStreamSynchronize(h->stream);   // (kernels that use it may be on their way)
+    dev_free(h, h->work);
+  }
   delete h;
   return SPGEMM_OK;
 }
