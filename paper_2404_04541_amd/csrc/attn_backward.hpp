@@ -1,0 +1,287 @@
+// Attention over a planned mask, gradients.
+//
+// With P = 2^(x - lse2) (x: the shaped scores in units of log 2, lse2 the row's logarithm from the forward pass), dP = dO V^T and
+// delta_i = sum_d dO_id O_id:  dV = P^T dO,  dS = P (dP - delta) (1 - tanh^2),  dQ = scale dS K,  dK = scale dS^T Q.
+// Two kernels, each with a fixed order of its sums (no atomics: the same inputs give the same bits): k_attn_dq goes over the keys of 128
+// queries as the forward kernel does and leaves delta and lse2 for k_attn_dkv, which goes over the queries, of all heads that share
+// them, of 128 keys.  That computes S and dP twice, seven products where five would do with atomics on dQ in 32 bits.
+// P, dS are rounded to 16 bits once, as operands; all sums are held in 32 bits.
+#pragma once
+#include "attn_forward.hpp"
+
+namespace spg {
+
+template <typename T, int D, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
+  using S = TileShape<D>;
+  __shared__ __align__(16) unsigned char k_even[kKeyTile * D * 2], v_even[kKeyTile * D * 2], k_odd[kKeyTile * D * 2], v_odd[kKeyTile * D * 2];
+  int head, qt;
+  head_and_tile(blockIdx.x, a.heads, a.q_tiles, &head, &qt);
+  const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
+  const int row_base = S::row_base(lane), across_base = S::across_base(lane);
+  const int row = qt * kPatTile + wave * kRowGroup + (lane & 31);
+  const int groups = ceil_div_d(a.q_len, kRowGroup);
+  int lo = 0x7fffffff, hi = 0;
+  GroupBound mine{0, 0, 0, 0};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int n = qt * 4 + w;
+    if (n >= groups) break;
+    const GroupBound b = load_uniform(a.plan.groups + n);
+    if (b.hi > b.lo) { lo = min(lo, b.lo); hi = max(hi, b.hi); }
+    if (w == wave) mine = b;
+  }
+  lo = uniform(lo);
+  hi = uniform(hi);
+  mine = {uniform(mine.lo), uniform(mine.hi), uniform(mine.all_lo), uniform(mine.all_hi)};
+  float scale2, cap2, slope2;
+  score_factors<CAP, BIAS>(a.score, head, &scale2, &cap2, &slope2);
+  const bool real = row < a.q_len;
+  const RowBound rb = real ? a.plan.rows[row] : RowBound{0, 0, 0, 0};
+  vec8<T> q[D / 16], d_o[D / 16];
+  load_row<T, D>(g.d_o.of(head), row, real, a.bytes, half, d_o);
+  float delta = 0.0f, lse2 = INFINITY;
+  {
+    load_row<T, D>(a.o.of(head), row, real, a.bytes, half, q);   // (O for the moment)
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)d_o[i][j], (float)q[i][j], delta);
+    delta = add_halves(delta);
+  }
+  if (real) {
+    const int64_t at = (int64_t)head * a.q_len + row;
+    const float v = a.lse[at];
+    lse2 = v == -INFINITY ? INFINITY : v * kLog2e;
+    if (half == 0) { g.lse2[at] = lse2; g.delta[at] = delta; }
+  }
+  load_row<T, D>(a.q.of(head), row, real, a.bytes, half, q);
+  const int kv = uniform(head / a.group);
+  const RowSource ks = a.k.of(kv), vs = a.v.of(kv);
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
+
+  const unsigned* flags = a.plan.seen_words ? a.plan.seen + (int64_t)qt * a.plan.seen_words : nullptr;
+  const int end = hi > lo ? ceil_div_d(hi, kKeyTile) : 0;
+
+  auto compute = [&](const unsigned char* kt, const unsigned char* vt, int k0) {
+    if (mine.lo >= k0 + kKeyTile || mine.hi <= k0) return;
+    const bool whole = mine.all_lo <= k0 && mine.all_hi >= k0 + kKeyTile;
+    const int at_row = in_loop(row_base), at_across = in_loop(across_base);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      f32x16 s = {}, dp = {}, th;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) s = mma(S::template row<T>(kt, at_row, 32 * t, i), q[i], s);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) dp = mma(S::template row<T>(vt, at_row, 32 * t, i), d_o[i], dp);
+      shape_scores<CAP, BIAS, true>(s, scale2, cap2, slope2, (float)(rb.diag - k0 - 4 * half - 32 * t), &th);
+      const unsigned span = rb.hi > rb.lo ? rb.hi - rb.lo : 0;
+      const int off = k0 + 4 * half + 32 * t - rb.lo;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float ds = fast_exp2(s[i] - lse2) * (dp[i] - delta);
+        if constexpr (CAP) ds *= __builtin_fmaf(-th[i], th[i], 1.0f);
+        s[i] = ds;
+      }
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = (unsigned)(off + 8 * (i / 4) + i % 4) < span ? s[i] : 0.0f;
+      }
+      vec8<T> p[2];
+      to_operand<T>(s, p);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) acc[i] = mma(S::template across<T>(kt, at_across, 32 * t + 16 * u, i), p[u], acc[i]);
+    }
+  };
+  auto load = [&](unsigned char* kt, unsigned char* vt, int k0) {
+    load_tile<D, kKeyTile, 256>(ks, kt, k0, lo, hi, a.bytes);
+    load_tile<D, kKeyTile, 256>(vs, vt, k0, lo, hi, a.bytes);
+  };
+
+  int c = next_tile(flags, hi > lo ? lo / kKeyTile : 0, end, 1);
+  if (c < end) load(k_even, v_even, c * kKeyTile);
+  while (c < end) {
+    int next = next_tile(flags, c + 1, end, 1);
+    tiles_ready();
+    if (next < end) load(k_odd, v_odd, next * kKeyTile);
+    compute(k_even, v_even, c * kKeyTile);
+    c = next;
+    if (c >= end) break;
+    next = next_tile(flags, c + 1, end, 1);
+    tiles_ready();
+    if (next < end) load(k_even, v_even, next * kKeyTile);
+    compute(k_odd, v_odd, c * kKeyTile);
+    c = next;
+  }
+
+  if (!real) return;
+  const RowSource os = g.dq.of(head);
+  unsigned char* out = const_cast<unsigned char*>(os.base) + (int64_t)row * os.stride;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int byte = (32 * i + 8 * r + 4 * half) * 2;
+      T v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = (T)(acc[i][4 * r + j] * a.score.scale);
+      if (byte < a.bytes) *reinterpret_cast<u32x2*>(out + byte) = __builtin_bit_cast(u32x2, v);
+    }
+}
+
+// A workgroup has 128 keys of a key head, a wave 32 of them: keys and values stay in registers as right operands, queries and dO come through LDS
+// in tiles of 32 rows, with their lse2, delta and bounds, one tile ahead, head by head.
+constexpr int kQueryTile = 32;
+
+template <int D>
+struct QueryTile {
+  unsigned char q[kQueryTile * D * 2], d_o[kQueryTile * D * 2];
+  float lse2[64], delta[64];          // (the load fills 64 places; those behind the tile are not read)
+  RowBound rows[64];
+};
+
+template <typename T, int D, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
+  using S = TileShape<D>;
+  __shared__ __align__(16) QueryTile<D> even, odd;
+  const int kv_heads = a.heads / a.group, k_tiles = ceil_div_d(a.k_len, kPatTile);
+  int kv, kt;
+  head_and_tile(blockIdx.x, kv_heads, k_tiles, &kv, &kt);
+  kt = k_tiles - 1 - kt;              // first keys first: under a causal mask the most queries see them
+  const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
+  const int row_base = S::row_base(lane), across_base = S::across_base(lane);
+  const int k0 = kt * kPatTile + wave * 32, key = k0 + (lane & 31);
+  const bool real = key < a.k_len;
+  vec8<T> k[D / 16], v[D / 16];
+  load_row<T, D>(a.k.of(kv), key, real, a.bytes, half, k);
+  load_row<T, D>(a.v.of(kv), key, real, a.bytes, half, v);
+  f32x16 dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) { dk[i] = f32x16{}; dv[i] = f32x16{}; }
+
+  const int2 span = load_uniform(a.plan.cols + kt);
+  const int lo = uniform(span.x), hi = uniform(span.y);
+  const unsigned* flags = a.plan.seen_by_words ? a.plan.seen_by + (int64_t)kt * a.plan.seen_by_words : nullptr;
+  const int end = hi > lo ? ceil_div_d(hi, kQueryTile) : 0;
+  const int begin = next_tile(flags, hi > lo ? lo / kQueryTile : 0, end, 2);
+
+  auto load = [&](QueryTile<D>& t, int head, int tile) {
+    const int first = tile * kQueryTile;
+    load_tile<D, kQueryTile, 256>(a.q.of(head), t.q, first, lo, hi, a.bytes);
+    load_tile<D, kQueryTile, 256>(g.d_o.of(head), t.d_o, first, lo, hi, a.bytes);
+    const int64_t at = (int64_t)head * a.q_len + first;
+    const unsigned rows = a.q_len - first < kQueryTile ? a.q_len - first : kQueryTile;
+    if (wave == 0) {
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(g.lse2 + at), 0, rows * 4, 0x00027000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)t.lse2, 4, in_loop(lane) * 4, 0, 0, 0);
+    } else if (wave == 1) {
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(g.delta + at), 0, rows * 4, 0x00027000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)t.delta, 4, in_loop(lane) * 4, 0, 0, 0);
+    } else if (wave == 2) {
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(a.plan.rows + first), 0, rows * 16, 0x00027000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)t.rows, 16, in_loop(lane) * 16, 0, 0, 0);
+    }
+  };
+  float scale2, cap2, slope2;
+  auto compute = [&](const QueryTile<D>& t, int tile) {
+    const GroupBound b = load_uniform(a.plan.groups + tile);
+    if (b.lo >= k0 + 32 || b.hi <= k0) return;
+    const bool whole = b.all_lo <= k0 && b.all_hi >= k0 + 32 && (tile + 1) * kQueryTile <= a.q_len;
+    const int at_row = in_loop(row_base), at_across = in_loop(across_base);
+    f32x16 s = {}, dp = {};
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) s = mma(S::template row<T>(t.q, at_row, 0, i), k[i], s);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) dp = mma(S::template row<T>(t.d_o, at_row, 0, i), v[i], dp);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const f32x4 l2 = *reinterpret_cast<const f32x4*>(&t.lse2[8 * r + 4 * half]), de = *reinterpret_cast<const f32x4*>(&t.delta[8 * r + 4 * half]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 4 * r + j;
+        float x, back = 1.0f;
+        if constexpr (CAP) {
+          const float th = tanh_of(s[i] * scale2);
+          back = __builtin_fmaf(-th, th, 1.0f);
+          x = th * cap2;
+        } else {
+          x = s[i] * scale2;
+        }
+        if constexpr (BIAS) x -= slope2 * fabsf((float)(t.rows[8 * r + 4 * half + j].diag - key));
+        s[i] = fast_exp2(x - l2[j]);
+        dp[i] = s[i] * (dp[i] - de[j]) * back;
+      }
+    }
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int2 rb = *reinterpret_cast<const int2*>(&t.rows[8 * (i / 4) + 4 * half + i % 4]);   // lo, hi
+        const bool sees = key >= rb.x && key < rb.y;
+        s[i] = sees ? s[i] : 0.0f;
+        dp[i] = sees ? dp[i] : 0.0f;
+      }
+    }
+    vec8<T> p[2];
+    to_operand<T>(s, p);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) dv[i] = mma(S::template across<T>(t.d_o, at_across, 16 * u, i), p[u], dv[i]);
+    to_operand<T>(dp, p);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) dk[i] = mma(S::template across<T>(t.q, at_across, 16 * u, i), p[u], dk[i]);
+  };
+
+  // head by head, tile by tile, in pairs of buffers
+  int head = kv * a.group, c = begin;
+  const int last = head + a.group;
+  auto step = [&](int* h, int* tile) {
+    *tile = next_tile(flags, *tile + 1, end, 2);
+    if (*tile >= end) { *tile = begin; ++*h; }
+  };
+  if (begin < end) {
+    load(even, head, c);
+    while (head < last) {
+      int h2 = head, c2 = c;
+      step(&h2, &c2);
+      tiles_ready();
+      if (h2 < last) load(odd, h2, c2);
+      score_factors<CAP, BIAS>(a.score, head, &scale2, &cap2, &slope2);
+      compute(even, c);
+      head = h2; c = c2;
+      if (head >= last) break;
+      step(&h2, &c2);
+      tiles_ready();
+      if (h2 < last) load(even, h2, c2);
+      score_factors<CAP, BIAS>(a.score, head, &scale2, &cap2, &slope2);
+      compute(odd, c);
+      head = h2; c = c2;
+    }
+  }
+
+  if (!real) return;
+  const RowSource ks = g.dk.of(kv), vs = g.dv.of(kv);
+  unsigned char* out_k = const_cast<unsigned char*>(ks.base) + (int64_t)key * ks.stride;
+  unsigned char* out_v = const_cast<unsigned char*>(vs.base) + (int64_t)key * vs.stride;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int byte = (32 * i + 8 * r + 4 * half) * 2;
+      T x[4], y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { x[j] = (T)(dk[i][4 * r + j] * a.score.scale); y[j] = (T)dv[i][4 * r + j]; }
+      if (byte < a.bytes) {
+        *reinterpret_cast<u32x2*>(out_k + byte) = __builtin_bit_cast(u32x2, x);
+        *reinterpret_cast<u32x2*>(out_v + byte) = __builtin_bit_cast(u32x2, y);
+      }
+    }
+}
+
+}  // namespace spg

@@ -1,0 +1,130 @@
+// The structure of a mask: bounds of its rows, of groups of rows and of columns, and a pattern's flags.  Bandwidth does not matter here (28 bytes a row);
+// what a plan costs is its launches: two without a pattern, three with one.
+#pragma once
+#include "attn_common.hpp"
+
+namespace spg {
+
+struct MaskView {
+  int q_len, k_len, docs, causal, window;
+  const int64_t* q_ptr;     // docs + 1, or null: one document of everything
+  const int64_t* k_ptr;
+  const int64_t* prefix;    // docs, or null
+  const int64_t* pat_ptr;   // of the pattern's rows of tiles, or null
+  const int32_t* pat_col;
+  int64_t pat_nnz;
+};
+
+__device__ __forceinline__ int clamp_to(int64_t v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : (int)v; }
+
+// Row i of the mask.  Bounds come out in ascending order over the rows (also of rows that see nothing: lo >= hi there), which k_plan_cols bisects.
+__device__ inline RowBound row_bound(const MaskView& m, int i) {
+  int qe = m.q_len, kb = 0, ke = m.k_len;
+  int64_t prompt = 0;
+  if (m.q_ptr) {
+    if (i < m.q_ptr[0]) return {0, 0, 0, 0};
+    int a = 0, b = m.docs;               // the last document that begins at or before i
+    while (b - a > 1) {
+      const int c = a + (b - a) / 2;
+      if (m.q_ptr[c] <= i) a = c; else b = c;
+    }
+    qe = clamp_to(m.q_ptr[a + 1], 0, m.q_len);
+    kb = clamp_to(m.k_ptr[a], 0, m.k_len);
+    ke = clamp_to(m.k_ptr[a + 1], kb, m.k_len);
+    if (i >= qe) return {m.k_len, m.k_len, 0, 0};   // behind the last document: behind every tile of keys too
+    if (m.prefix) prompt = clamp_to(m.prefix[a], 0, m.k_len);
+  } else if (m.prefix) {
+    prompt = clamp_to(m.prefix[0], 0, m.k_len);
+  }
+  const int diag = i + ke - qe;
+  int lo = kb, hi = ke;
+  if (m.causal) {
+    const int64_t p = kb + prompt;
+    hi = clamp_to(p > diag + 1 ? p : diag + 1, kb, ke);
+  }
+  if (m.window) lo = clamp_to((int64_t)diag - m.window + 1, kb, ke);
+  return {lo, hi, diag, 0};
+}
+
+// One thread a row, groups from their lanes; the first workgroup checks the documents too.  The flags of a pattern are cleared here.
+__global__ void __launch_bounds__(256) k_plan_rows(MaskView m, PlanView p) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  const int64_t words = (int64_t)ceil_div_d(m.q_len, kPatTile) * p.seen_words, by_words = (int64_t)ceil_div_d(m.k_len, kPatTile) * p.seen_by_words;
+  for (int64_t w = i; w < words; w += (int64_t)gridDim.x * 256) p.seen[w] = 0;
+  for (int64_t w = i; w < by_words; w += (int64_t)gridDim.x * 256) p.seen_by[w] = 0;
+  RowBound r{0, 0, 0, 0};
+  if (i < m.q_len) {
+    r = row_bound(m, i);
+    p.rows[i] = r;
+  }
+  GroupBound g{r.lo < r.hi ? r.lo : 0x7fffffff, r.lo < r.hi ? r.hi : 0, i < m.q_len ? r.lo : 0, i < m.q_len ? r.hi : 0x7fffffff};
+#pragma unroll
+  for (int d = kRowGroup / 2; d; d >>= 1) {
+    g.lo = min(g.lo, __shfl_xor(g.lo, d)); g.hi = max(g.hi, __shfl_xor(g.hi, d));
+    g.all_lo = max(g.all_lo, __shfl_xor(g.all_lo, d)); g.all_hi = min(g.all_hi, __shfl_xor(g.all_hi, d));
+  }
+  if (i % kRowGroup == 0 && i < m.q_len) p.groups[i / kRowGroup] = {g.hi ? g.lo : 0, g.hi, g.all_lo, g.all_hi};
+  if (blockIdx.x == 0) {
+    __shared__ int bad;
+    if (threadIdx.x == 0) bad = 0;
+    __syncthreads();
+    if (m.q_ptr) {
+      for (int d = threadIdx.x; d < m.docs; d += 256) {
+        const int64_t a = m.q_ptr[d], b = m.q_ptr[d + 1], c = m.k_ptr[d], e = m.k_ptr[d + 1];
+        if (a < 0 || b < a || b > m.q_len || c < 0 || e < c || e > m.k_len) bad = 1;
+        if (m.prefix && m.prefix[d] < 0) bad = 1;
+      }
+    } else if (m.prefix && threadIdx.x == 0 && m.prefix[0] < 0) {
+      bad = 1;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) *p.error = bad;
+  }
+}
+
+// How many of n ascending numbers at(0) .. at(n - 1) lie below `limit`, by the whole wave: 64 of them are looked at together.
+template <typename F>
+__device__ __forceinline__ int wave_count_below(int n, int64_t limit, F at) {
+  int a = 0;                                     // at(i) < limit for i < a
+  while (n - a > 0) {
+    const int step = ceil_div_d(n - a, kWave);   // lane l looks at the last of its share
+    const int i = a + (lane_id() + 1) * step - 1;
+    const bool below = (int64_t)a + (int64_t)(lane_id() + 1) * step - 1 < n && at(i) < limit;
+    const int shares = __popcll(__ballot(below));
+    a += shares * step;
+    if (step == 1) return a;
+    n = (int64_t)a + step < n ? a + step : n;    // the next share's last number is not below
+  }
+  return a;
+}
+
+// The queries that can see any key of a tile, a wave a tile: from the first row that ends behind its first key to before the first that begins
+// behind its last.
+__global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanView p) {
+  const int c = blockIdx.x * 4 + threadIdx.x / kWave;
+  if (c >= ceil_div_d(k_len, kPatTile)) return;
+  const int first = c * kPatTile, last = k_len - first > kPatTile ? first + kPatTile : k_len;
+  const int from = wave_count_below(q_len, (int64_t)first + 1, [&](int i) { return p.rows[i].hi; });
+  const int to = wave_count_below(q_len, last, [&](int i) { return p.rows[i].lo; });
+  if (lane_id() == 0) p.cols[c] = make_int2(from, to);
+}
+
+// The pattern's flags, a wave a row of tiles.  Bits are only set, so neither the order of a row's columns nor repeated ones matter.
+__global__ void __launch_bounds__(256) k_plan_pattern(MaskView m, PlanView p) {
+  const int rows = ceil_div_d(m.q_len, kPatTile), cols = ceil_div_d(m.k_len, kPatTile);
+  const int r = blockIdx.x * 4 + threadIdx.x / kWave;
+  if (r >= rows) return;
+  const int64_t a = m.pat_ptr[r], b = m.pat_ptr[r + 1];
+  if (a < 0 || b < a || b > m.pat_nnz) {
+    if (lane_id() == 0) *p.error = 1;
+    return;
+  }
+  for (int64_t e = a + lane_id(); e < b; e += kWave) {
+    const int c = m.pat_col[e];
+    if (c < 0 || c >= cols) { *p.error = 1; continue; }
+    atomicOr(&p.seen[(int64_t)r * p.seen_words + c / 32], 1u << (c % 32));
+    atomicOr(&p.seen_by[(int64_t)c * p.seen_by_words + r / 32], 1u << (r % 32));
+  }
+}
+
+}  // namespace spg
