@@ -102,7 +102,7 @@ PlanView carve_plan(const spattn_mask* m, void* mem, size_t* bytes) {
   p.error = c.take<int>(1);
   p.rows = c.take<RowBound>(m->q_len);
   p.groups = c.take<GroupBound>(ceil_div(m->q_len, kRowGroup));
-  p.cols = c.take<int2>(k_tiles);
+  p.cols = c.take<int2>(ceil_div(m->k_len, kKeyTile));
   if (m->tiles) {
     p.seen_words = (int)ceil_div(k_tiles > 0 ? k_tiles : 1, 32);
     p.seen_by_words = (int)ceil_div(q_tiles > 0 ? q_tiles : 1, 32);
@@ -145,7 +145,7 @@ int check_args(spgemm_context* h, const spattn_args* a) {
   if ((rc = check_tensor(h, a->q, a->mask->q_len, "q"))) return rc;
   if ((rc = check_tensor(h, a->k, a->mask->k_len, "k"))) return rc;
   if ((rc = check_tensor(h, a->v, a->mask->k_len, "v"))) return rc;
-  if (ceil_div(a->mask->q_len, kPatTile) * a->heads > 0x7fffffffLL || ceil_div(a->mask->k_len, kPatTile) * a->kv_heads > 0x7fffffffLL)
+  if (ceil_div(a->mask->q_len, kPatTile) * a->heads > 0x7fffffffLL || ceil_div(a->mask->k_len, kKeyTile) * a->kv_heads > 0x7fffffffLL)
     return fail(h, SPGEMM_UNSUPPORTED, "too many tiles");
   return SPGEMM_OK;
 }
@@ -261,7 +261,7 @@ int spattn_symbolic(spgemm_handle h, const spattn_mask* mask, void* plan_mem, si
     if (mask->tiles) { m.pat_ptr = mask->tiles->rowptr; m.pat_col = mask->tiles->colidx; m.pat_nnz = mask->tiles->nnz; }
     k_plan_rows<<<dim3((unsigned)ceil_div(mask->q_len > 0 ? mask->q_len : 1, 256)), dim3(256), 0, h->stream>>>(m, p);
     if (mask->k_len > 0)
-      k_plan_cols<<<dim3((unsigned)ceil_div(ceil_div(mask->k_len, kPatTile), 4)), dim3(256), 0, h->stream>>>(m.q_len, m.k_len, p);
+      k_plan_cols<<<dim3((unsigned)ceil_div(ceil_div(mask->k_len, kKeyTile), 4)), dim3(256), 0, h->stream>>>(m.q_len, m.k_len, p);
     if (mask->tiles && mask->q_len > 0)
       k_plan_pattern<<<dim3((unsigned)ceil_div(ceil_div(mask->q_len, kPatTile), 4)), dim3(256), 0, h->stream>>>(m, p);
     if ((rc = launched(h))) return rc;
@@ -306,7 +306,7 @@ int spattn_backward(spgemm_handle h, const spattn_args* a, spattn_tensor o, cons
     if ((rc = scratch(h, 2 * stats, &mem))) return rc;
     AttnArgs g = attn_args(a, o, lse);
     AttnGrads r{view(d_o), view(dq), view(dk), view(dv), static_cast<float*>(mem), reinterpret_cast<float*>(static_cast<unsigned char*>(mem) + stats)};
-    const unsigned q_grid = (unsigned)(g.q_tiles * g.heads), k_grid = (unsigned)(ceil_div(k_len, kPatTile) * a->kv_heads);
+    const unsigned q_grid = (unsigned)(g.q_tiles * g.heads), k_grid = (unsigned)(ceil_div(k_len, kKeyTile) * a->kv_heads);
     dispatch(a->dtype, a->head_dim, a->cap > 0, a->slopes != nullptr, [&](auto type, auto dim, auto cap, auto bias) {
       if (q_grid) k_attn_dq<decltype(type), dim(), cap(), bias()><<<dim3(q_grid), dim3(256), 0, h->stream>>>(g, r);
       if (k_grid) k_attn_dkv<decltype(type), dim(), cap(), bias()><<<dim3(k_grid), dim3(256), 0, h->stream>>>(g, r);

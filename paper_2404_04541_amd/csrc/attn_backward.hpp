@@ -133,28 +133,29 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
     }
 }
 
-// A workgroup has 128 keys of a key head, a wave 32 of them: keys and values stay in registers as right operands, queries and dO come through LDS
-// in tiles of 32 rows, with their lse2, delta and bounds, one tile ahead, head by head.
-constexpr int kQueryTile = 32;
+// A workgroup has 64 keys of a key head and goes over their queries in tiles of 64 rows, head by head.  Wave w has keys 32 (w % 2) .. and of every
+// tile the rows 32 (w / 2) ..; keys and values stay in registers as right operands, queries and dO come through LDS with their lse2, delta
+// and bounds, one tile ahead.  At the end the two waves of the same keys exchange sums: one adds up dK, the other dV.
+constexpr int kQueryTile = 64;
 
 template <int D>
 struct QueryTile {
   unsigned char q[kQueryTile * D * 2], d_o[kQueryTile * D * 2];
-  float lse2[64], delta[64];          // (the load fills 64 places; those behind the tile are not read)
-  RowBound rows[64];
+  float lse2[kQueryTile], delta[kQueryTile];
+  RowBound rows[kQueryTile];
 };
 
 template <typename T, int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
   using S = TileShape<D>;
   __shared__ __align__(16) QueryTile<D> even, odd;
-  const int kv_heads = a.heads / a.group, k_tiles = ceil_div_d(a.k_len, kPatTile);
+  const int kv_heads = a.heads / a.group, k_tiles = ceil_div_d(a.k_len, kKeyTile);
   int kv, kt;
   head_and_tile(blockIdx.x, kv_heads, k_tiles, &kv, &kt);
   kt = k_tiles - 1 - kt;              // first keys first: under a causal mask the most queries see them
-  const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
+  const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave), part = wave >> 1;
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
-  const int k0 = kt * kPatTile + wave * 32, key = k0 + (lane & 31);
+  const int k0 = kt * kKeyTile + (wave & 1) * 32, key = k0 + (lane & 31);
   const bool real = key < a.k_len;
   vec8<T> k[D / 16], v[D / 16];
   load_row<T, D>(a.k.of(kv), key, real, a.bytes, half, k);
@@ -165,9 +166,9 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
 
   const int2 span = load_uniform(a.plan.cols + kt);
   const int lo = uniform(span.x), hi = uniform(span.y);
-  const unsigned* flags = a.plan.seen_by_words ? a.plan.seen_by + (int64_t)kt * a.plan.seen_by_words : nullptr;
+  const unsigned* flags = a.plan.seen_by_words ? a.plan.seen_by + (int64_t)(kt * kKeyTile / kPatTile) * a.plan.seen_by_words : nullptr;
   const int end = hi > lo ? ceil_div_d(hi, kQueryTile) : 0;
-  const int begin = next_tile(flags, hi > lo ? lo / kQueryTile : 0, end, 2);
+  const int begin = next_tile(flags, hi > lo ? lo / kQueryTile : 0, end, 1);
 
   auto load = [&](QueryTile<D>& t, int head, int tile) {
     const int first = tile * kQueryTile;
@@ -188,18 +189,22 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
   };
   float scale2, cap2, slope2;
   auto compute = [&](const QueryTile<D>& t, int tile) {
-    const GroupBound b = load_uniform(a.plan.groups + tile);
+    const int group = tile * (kQueryTile / kRowGroup) + part;
+    if (group * kRowGroup >= a.q_len) return;
+    const GroupBound b = load_uniform(a.plan.groups + group);
     if (b.lo >= k0 + 32 || b.hi <= k0) return;
-    const bool whole = b.all_lo <= k0 && b.all_hi >= k0 + 32 && (tile + 1) * kQueryTile <= a.q_len;
-    const int at_row = in_loop(row_base), at_across = in_loop(across_base);
+    const bool whole = b.all_lo <= k0 && b.all_hi >= k0 + 32 && (group + 1) * kRowGroup <= a.q_len;
+    const unsigned char *tq = t.q + part * (kRowGroup * D * 2), *to = t.d_o + part * (kRowGroup * D * 2);
+    const int at_row = in_loop(row_base), at_across = in_loop(across_base), r0 = part * kRowGroup + 4 * half;
     f32x16 s = {}, dp = {};
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) s = mma(S::template row<T>(t.q, at_row, 0, i), k[i], s);
+    for (int i = 0; i < D / 16; ++i) s = mma(S::template row<T>(tq, at_row, 0, i), k[i], s);
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) dp = mma(S::template row<T>(t.d_o, at_row, 0, i), v[i], dp);
+    for (int i = 0; i < D / 16; ++i) dp = mma(S::template row<T>(to, at_row, 0, i), v[i], dp);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const f32x4 l2 = *reinterpret_cast<const f32x4*>(&t.lse2[8 * r + 4 * half]), de = *reinterpret_cast<const f32x4*>(&t.delta[8 * r + 4 * half]);
+      __builtin_amdgcn_sched_barrier(0);      // (all of them at once would cost 32 registers)
+      const f32x4 l2 = *reinterpret_cast<const f32x4*>(&t.lse2[r0 + 8 * r]), de = *reinterpret_cast<const f32x4*>(&t.delta[r0 + 8 * r]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int i = 4 * r + j;
@@ -211,7 +216,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
         } else {
           x = s[i] * scale2;
         }
-        if constexpr (BIAS) x -= slope2 * fabsf((float)(t.rows[8 * r + 4 * half + j].diag - key));
+        if constexpr (BIAS) x -= slope2 * fabsf((float)(t.rows[r0 + 8 * r + j].diag - key));
         s[i] = fast_exp2(x - l2[j]);
         dp[i] = s[i] * (dp[i] - de[j]) * back;
       }
@@ -219,7 +224,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
     if (!whole) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int2 rb = *reinterpret_cast<const int2*>(&t.rows[8 * (i / 4) + 4 * half + i % 4]);   // lo, hi
+        const int2 rb = *reinterpret_cast<const int2*>(&t.rows[r0 + 8 * (i / 4) + i % 4]);   // lo, hi
         const bool sees = key >= rb.x && key < rb.y;
         s[i] = sees ? s[i] : 0.0f;
         dp[i] = sees ? dp[i] : 0.0f;
@@ -230,19 +235,19 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) dv[i] = mma(S::template across<T>(t.d_o, at_across, 16 * u, i), p[u], dv[i]);
+      for (int i = 0; i < D / 32; ++i) dv[i] = mma(S::template across<T>(to, at_across, 16 * u, i), p[u], dv[i]);
     to_operand<T>(dp, p);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) dk[i] = mma(S::template across<T>(t.q, at_across, 16 * u, i), p[u], dk[i]);
+      for (int i = 0; i < D / 32; ++i) dk[i] = mma(S::template across<T>(tq, at_across, 16 * u, i), p[u], dk[i]);
   };
 
   // head by head, tile by tile, in pairs of buffers
   int head = kv * a.group, c = begin;
   const int last = head + a.group;
   auto step = [&](int* h, int* tile) {
-    *tile = next_tile(flags, *tile + 1, end, 2);
+    *tile = next_tile(flags, *tile + 1, end, 1);
     if (*tile >= end) { *tile = begin; ++*h; }
   };
   if (begin < end) {
@@ -265,22 +270,35 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
     }
   }
 
+  // wave (keys, part 0) takes over the other's dK, wave (keys, part 1) its dV
+  __syncthreads();
+  f32x4* room = reinterpret_cast<f32x4*>((wave & 1) ? odd.q : even.q) + part * (D / 8 * kWave) + lane;
+  static_assert(2 * (D / 8) * kWave * 16 <= 2 * kQueryTile * D * 2, "both waves' sums fit a buffer's queries and dO");
+  const f32x4* other = reinterpret_cast<const f32x4*>((wave & 1) ? odd.q : even.q) + (1 - part) * (D / 8 * kWave) + lane;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      f32x4 x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = part ? dk[i][4 * r + j] : dv[i][4 * r + j];
+      room[(4 * i + r) * kWave] = x;
+    }
+  __syncthreads();
   if (!real) return;
-  const RowSource ks = g.dk.of(kv), vs = g.dv.of(kv);
-  unsigned char* out_k = const_cast<unsigned char*>(ks.base) + (int64_t)key * ks.stride;
-  unsigned char* out_v = const_cast<unsigned char*>(vs.base) + (int64_t)key * vs.stride;
+  const RowSource to = (part ? g.dv : g.dk).of(kv);
+  const float by = part ? 1.0f : a.score.scale;
+  unsigned char* out = const_cast<unsigned char*>(to.base) + (int64_t)key * to.stride;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int byte = (32 * i + 8 * r + 4 * half) * 2;
-      T x[4], y[4];
+      const f32x4 x = other[(4 * i + r) * kWave];
+      T y[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { x[j] = (T)(dk[i][4 * r + j] * a.score.scale); y[j] = (T)dv[i][4 * r + j]; }
-      if (byte < a.bytes) {
-        *reinterpret_cast<u32x2*>(out_k + byte) = __builtin_bit_cast(u32x2, x);
-        *reinterpret_cast<u32x2*>(out_v + byte) = __builtin_bit_cast(u32x2, y);
-      }
+      for (int j = 0; j < 4; ++j) y[j] = (T)(((part ? dv[i][4 * r + j] : dk[i][4 * r + j]) + x[j]) * by);
+      if (byte < a.bytes) *reinterpret_cast<u32x2*>(out + byte) = __builtin_bit_cast(u32x2, y);
     }
 }
 

@@ -31,7 +31,8 @@ __device__ __forceinline__ f32x4 mma(vec8<f16_t> a, vec8<f16_t> b, f32x4 c) { re
 
 __host__ __device__ constexpr int ceil_div_d(int a, int b) { return a / b + (a % b != 0); }
 
-constexpr int kPatTile = 128;    // rows and columns of a pattern's tiles; queries (forward, dQ) or keys (dK, dV) of a workgroup
+constexpr int kPatTile = 128;    // rows and columns of a pattern's tiles; queries of a workgroup (forward, dQ)
+constexpr int kKeyTile = 64;     // keys that come through LDS together (forward, dQ), or that a workgroup has (dK, dV)
 constexpr int kRowGroup = 32;    // rows whose bounds the plan sums up: a wave's queries
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -45,7 +46,7 @@ struct GroupBound { int lo, hi, all_lo, all_hi; };
 struct PlanView {
   RowBound* rows;          // q_len
   GroupBound* groups;      // ceil(q_len / kRowGroup)
-  int2* cols;              // per kPatTile keys: the queries that can see any of them
+  int2* cols;              // per kKeyTile keys: the queries that can see any of them
   unsigned* seen;          // ceil(q_len / kPatTile) rows of seen_words
   unsigned* seen_by;       // ceil(k_len / kPatTile) rows of seen_by_words
   int* error;
@@ -151,22 +152,26 @@ struct RowSource {
 // rows before lo.
 template <int D, int ROWS, int THREADS>
 __device__ __forceinline__ void load_tile(const RowSource& src, unsigned char* tile, int first, int lo, int hi, int bytes) {
-  constexpr int kChunks = TileShape<D>::kChunks;
-  constexpr int kPerWave = ROWS * kChunks / (THREADS / kWave);
-  static_assert(kPerWave % kWave == 0, "whole instructions");
+  using S = TileShape<D>;
+  constexpr int kLoads = ROWS * S::kChunks / THREADS, kStep = kWave / S::kChunks;   // instructions a wave; rows of one
+  static_assert(kLoads * THREADS == ROWS * S::kChunks && 16 % kStep == 0 && (kLoads * kStep) % 16 == 0, "a wave's rows begin at a multiple of 16");
   const int wave = uniform(threadIdx.x / kWave), lane = in_loop(lane_id());
   const int from = first < lo ? lo : first;                      // the buffer begins at the first row that is read
   const int rows = hi - from < ROWS ? hi - from : ROWS;
   const unsigned char* base = src.base + (int64_t)from * src.stride;
-  const unsigned limit = rows > 0 ? (unsigned)((rows - 1) * src.stride) + (unsigned)bytes : 0u;
+  const unsigned stride = (unsigned)src.stride;
+  const unsigned limit = rows > 0 ? (unsigned)(rows - 1) * stride + (unsigned)bytes : 0u;
   const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, limit, 0x00027000);
+  const int r = wave * (kLoads * kStep) + lane / S::kChunks;     // the first instruction's row
+  const int chunk = (lane % S::kChunks) ^ S::swizzle(lane / S::kChunks);
+  const int row0 = r + first - from;
+  const unsigned at0 = (unsigned)row0 * stride;
 #pragma unroll
-  for (int i = 0; i < kPerWave / kWave; ++i) {
-    const int slot = wave * kPerWave + i * kWave + lane;
-    const int r = slot / kChunks, chunk = (slot % kChunks) ^ TileShape<D>::swizzle(r);
-    const int row = first + r - from;
-    const unsigned at = row >= 0 && row < rows && chunk * 16 < bytes ? (unsigned)row * (unsigned)src.stride + (unsigned)chunk * 16u : 0x80000000u;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(tile + (wave * kPerWave + i * kWave) * 16), 16, (int)at, 0, 0, 0);
+  for (int i = 0; i < kLoads; ++i) {
+    const int c = (chunk ^ S::swizzle(i * kStep)) * 16;          // (the swizzle is linear: rows add up without carries)
+    const unsigned row = (unsigned)(row0 + i * kStep);           // (before lo: very large)
+    const unsigned at = row < (unsigned)rows && c < bytes ? at0 + (unsigned)(i * kStep) * stride + (unsigned)c : 0x80000000u;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(tile + (wave * kLoads + i) * (kWave * 16)), 16, (int)at, 0, 0, 0);
   }
 }
 

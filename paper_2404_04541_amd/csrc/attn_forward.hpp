@@ -11,7 +11,6 @@
 
 namespace spg {
 
-constexpr int kKeyTile = 64;
 constexpr float kLazyMax = 8.0f;   // probabilities stay below 2^8 times the running maximum's
 
 struct HeadTensor {       // rows of a packed tensor with heads: token t of head h begins at base + t * stride + h * head (bytes)

@@ -102,8 +102,8 @@ __device__ __forceinline__ int wave_count_below(int n, int64_t limit, F at) {
 // behind its last.
 __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanView p) {
   const int c = blockIdx.x * 4 + threadIdx.x / kWave;
-  if (c >= ceil_div_d(k_len, kPatTile)) return;
-  const int first = c * kPatTile, last = k_len - first > kPatTile ? first + kPatTile : k_len;
+  if (c >= ceil_div_d(k_len, kKeyTile)) return;
+  const int first = c * kKeyTile, last = k_len - first > kKeyTile ? first + kKeyTile : k_len;
   const int from = wave_count_below(q_len, (int64_t)first + 1, [&](int i) { return p.rows[i].hi; });
   const int to = wave_count_below(q_len, last, [&](int i) { return p.rows[i].lo; });
   if (lane_id() == 0) p.cols[c] = make_int2(from, to);
