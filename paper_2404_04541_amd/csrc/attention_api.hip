@@ -100,9 +100,12 @@ PlanView carve_plan(const spattn_mask* m, void* mem, size_t* bytes) {
   Carve c{static_cast<unsigned char*>(mem)};
   PlanView p{};
   p.error = c.take<int>(1);
+  p.done = c.take<unsigned>(1);
   p.rows = c.take<RowBound>(m->q_len);
   p.groups = c.take<GroupBound>(ceil_div(m->q_len, kRowGroup));
   p.cols = c.take<int2>(ceil_div(m->k_len, kKeyTile));
+  p.q_order = c.take<int>(q_tiles);
+  p.k_order = c.take<int>(ceil_div(m->k_len, kKeyTile));
   if (m->tiles) {
     p.seen_words = (int)ceil_div(k_tiles > 0 ? k_tiles : 1, 32);
     p.seen_by_words = (int)ceil_div(q_tiles > 0 ? q_tiles : 1, 32);
@@ -260,8 +263,7 @@ int spattn_symbolic(spgemm_handle h, const spattn_mask* mask, void* plan_mem, si
     m.q_ptr = mask->q_ptr; m.k_ptr = mask->k_ptr; m.prefix = mask->prefix;
     if (mask->tiles) { m.pat_ptr = mask->tiles->rowptr; m.pat_col = mask->tiles->colidx; m.pat_nnz = mask->tiles->nnz; }
     k_plan_rows<<<dim3((unsigned)ceil_div(mask->q_len > 0 ? mask->q_len : 1, 256)), dim3(256), 0, h->stream>>>(m, p);
-    if (mask->k_len > 0)
-      k_plan_cols<<<dim3((unsigned)ceil_div(ceil_div(mask->k_len, kKeyTile), 4)), dim3(256), 0, h->stream>>>(m.q_len, m.k_len, p);
+    k_plan_cols<<<dim3((unsigned)(ceil_div(ceil_div(mask->k_len, kKeyTile), 4) + 1)), dim3(256), 0, h->stream>>>(m.q_len, m.k_len, p);
     if (mask->tiles && mask->q_len > 0)
       k_plan_pattern<<<dim3((unsigned)ceil_div(ceil_div(mask->q_len, kPatTile), 4)), dim3(256), 0, h->stream>>>(m, p);
     if ((rc = launched(h))) return rc;

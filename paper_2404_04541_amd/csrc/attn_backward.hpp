@@ -3,7 +3,7 @@
 // With P = 2^(x - lse2) (x: the shaped scores in units of log 2, lse2 the row's logarithm from the forward pass), dP = dO V^T and
 // delta_i = sum_d dO_id O_id:  dV = P^T dO,  dS = P (dP - delta) (1 - tanh^2),  dQ = scale dS K,  dK = scale dS^T Q.
 // Two kernels, each with a fixed order of its sums (no atomics: the same inputs give the same bits): k_attn_dq goes over the keys of 128
-// queries as the forward kernel does and leaves delta and lse2 for k_attn_dkv, which goes over the queries, of all heads that share
+// queries as the forward kernel does and leaves -delta and what exponents begin with for k_attn_dkv, which goes over the queries, of all heads that share
 // them, of 128 keys.  That computes S and dP twice, seven products where five would do with atomics on dQ in 32 bits.
 // P, dS are rounded to 16 bits once, as operands; all sums are held in 32 bits.
 #pragma once
@@ -16,7 +16,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
   using S = TileShape<D>;
   __shared__ __align__(16) unsigned char k_even[kKeyTile * D * 2], v_even[kKeyTile * D * 2], k_odd[kKeyTile * D * 2], v_odd[kKeyTile * D * 2];
   int head, qt;
-  head_and_tile(blockIdx.x, a.heads, a.q_tiles, &head, &qt);
+  head_and_tile(blockIdx.x, a.heads, a.plan.q_order, &head, &qt);
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
   const int row = qt * kPatTile + wave * kRowGroup + (lane & 31);
@@ -34,13 +34,12 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
   lo = uniform(lo);
   hi = uniform(hi);
   mine = {uniform(mine.lo), uniform(mine.hi), uniform(mine.all_lo), uniform(mine.all_hi)};
-  float scale2, cap2, slope2;
-  score_factors<CAP, BIAS>(a.score, head, &scale2, &cap2, &slope2);
+  const ScoreFactors f = score_factors<CAP, BIAS>(a.score, head);
   const bool real = row < a.q_len;
   const RowBound rb = real ? a.plan.rows[row] : RowBound{0, 0, 0, 0};
   vec8<T> q[D / 16], d_o[D / 16];
   load_row<T, D>(g.d_o.of(head), row, real, a.bytes, half, d_o);
-  float delta = 0.0f, lse2 = INFINITY;
+  float delta = 0.0f, lse2 = INFINITY;   // (a row that sees nothing: every power is 0)
   {
     load_row<T, D>(a.o.of(head), row, real, a.bytes, half, q);   // (O for the moment)
 #pragma unroll
@@ -53,11 +52,13 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
     const int64_t at = (int64_t)head * a.q_len + row;
     const float v = a.lse[at];
     lse2 = v == -INFINITY ? INFINITY : v * kLog2e;
-    if (half == 0) { g.lse2[at] = lse2; g.delta[at] = delta; }
+    if (half == 0) { g.base[at] = f.add - lse2; g.less[at] = -delta; }
   }
+  const float base = f.add - lse2;
   load_row<T, D>(a.q.of(head), row, real, a.bytes, half, q);
   const int kv = uniform(head / a.group);
   const RowSource ks = a.k.of(kv), vs = a.v.of(kv);
+  const TileLoader<D, kKeyTile, 256> load_k(ks.stride, lane), load_v(vs.stride, lane);
   f32x16 acc[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
@@ -71,19 +72,20 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
     const int at_row = in_loop(row_base), at_across = in_loop(across_base);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      f32x16 s = {}, dp = {}, th;
+      f32x16 s = {}, dp = {};
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) s = mma(S::template row<T>(kt, at_row, 32 * t, i), q[i], s);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) dp = mma(S::template row<T>(vt, at_row, 32 * t, i), d_o[i], dp);
-      shape_scores<CAP, BIAS, true>(s, scale2, cap2, slope2, (float)(rb.diag - k0 - 4 * half - 32 * t), &th);
+      const float away = (float)(rb.diag - k0 - 4 * half - 32 * t);
       const unsigned span = rb.hi > rb.lo ? rb.hi - rb.lo : 0;
       const int off = k0 + 4 * half + 32 * t - rb.lo;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float ds = fast_exp2(s[i] - lse2) * (dp[i] - delta);
-        if constexpr (CAP) ds *= __builtin_fmaf(-th[i], th[i], 1.0f);
-        s[i] = ds;
+        float back;
+        const float x = shaped<CAP, BIAS>(s[i], f, f.slope2 * fabsf(away - (float)(8 * (i / 4) + i % 4)), &back);
+        s[i] = fast_exp2(__builtin_fmaf(x, f.mul, base)) * (dp[i] - delta);
+        if constexpr (CAP) s[i] *= back;
       }
       if (!whole) {
 #pragma unroll
@@ -98,8 +100,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
     }
   };
   auto load = [&](unsigned char* kt, unsigned char* vt, int k0) {
-    load_tile<D, kKeyTile, 256>(ks, kt, k0, lo, hi, a.bytes);
-    load_tile<D, kKeyTile, 256>(vs, vt, k0, lo, hi, a.bytes);
+    load_tile(load_k, ks.base, kt, k0, lo, hi, a.bytes);
+    load_tile(load_v, vs.base, vt, k0, lo, hi, a.bytes);
   };
 
   int c = next_tile(flags, hi > lo ? lo / kKeyTile : 0, end, 1);
@@ -119,6 +121,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
   }
 
   if (!real) return;
+  const float by = CAP ? 4.0f * a.score.scale : a.score.scale;
   const RowSource os = g.dq.of(head);
   unsigned char* out = const_cast<unsigned char*>(os.base) + (int64_t)row * os.stride;
 #pragma unroll
@@ -128,20 +131,20 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
       const int byte = (32 * i + 8 * r + 4 * half) * 2;
       T v[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = (T)(acc[i][4 * r + j] * a.score.scale);
+      for (int j = 0; j < 4; ++j) v[j] = (T)(acc[i][4 * r + j] * by);
       if (byte < a.bytes) *reinterpret_cast<u32x2*>(out + byte) = __builtin_bit_cast(u32x2, v);
     }
 }
 
 // A workgroup has 64 keys of a key head and goes over their queries in tiles of 64 rows, head by head.  Wave w has keys 32 (w % 2) .. and of every
-// tile the rows 32 (w / 2) ..; keys and values stay in registers as right operands, queries and dO come through LDS with their lse2, delta
-// and bounds, one tile ahead.  At the end the two waves of the same keys exchange sums: one adds up dK, the other dV.
+// tile the rows 32 (w / 2) ..; keys and values stay in registers as right operands, queries and dO come through LDS with what their exponents and dP
+// begin with and their bounds, one tile ahead.  At the end the two waves of the same keys exchange sums: one adds up dK, the other dV.
 constexpr int kQueryTile = 64;
 
 template <int D>
 struct QueryTile {
   unsigned char q[kQueryTile * D * 2], d_o[kQueryTile * D * 2];
-  float lse2[kQueryTile], delta[kQueryTile];
+  float base[kQueryTile], less[kQueryTile];
   RowBound rows[kQueryTile];
 };
 
@@ -149,10 +152,8 @@ template <typename T, int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
   using S = TileShape<D>;
   __shared__ __align__(16) QueryTile<D> even, odd;
-  const int kv_heads = a.heads / a.group, k_tiles = ceil_div_d(a.k_len, kKeyTile);
   int kv, kt;
-  head_and_tile(blockIdx.x, kv_heads, k_tiles, &kv, &kt);
-  kt = k_tiles - 1 - kt;              // first keys first: under a causal mask the most queries see them
+  head_and_tile(blockIdx.x, a.heads / a.group, a.plan.k_order, &kv, &kt);
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave), part = wave >> 1;
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
   const int k0 = kt * kKeyTile + (wave & 1) * 32, key = k0 + (lane & 31);
@@ -172,22 +173,23 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
 
   auto load = [&](QueryTile<D>& t, int head, int tile) {
     const int first = tile * kQueryTile;
-    load_tile<D, kQueryTile, 256>(a.q.of(head), t.q, first, lo, hi, a.bytes);
-    load_tile<D, kQueryTile, 256>(g.d_o.of(head), t.d_o, first, lo, hi, a.bytes);
+    const TileLoader<D, kQueryTile, 256> load_q(a.q.stride, in_loop(lane)), load_do(g.d_o.stride, in_loop(lane));   // (made anew: registers are short)
+    load_tile(load_q, a.q.of(head).base, t.q, first, lo, hi, a.bytes);
+    load_tile(load_do, g.d_o.of(head).base, t.d_o, first, lo, hi, a.bytes);
     const int64_t at = (int64_t)head * a.q_len + first;
     const unsigned rows = a.q_len - first < kQueryTile ? a.q_len - first : kQueryTile;
     if (wave == 0) {
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(g.lse2 + at), 0, rows * 4, 0x00027000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)t.lse2, 4, in_loop(lane) * 4, 0, 0, 0);
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(g.base + at), 0, rows * 4, 0x00027000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)t.base, 4, in_loop(lane) * 4, 0, 0, 0);
     } else if (wave == 1) {
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(g.delta + at), 0, rows * 4, 0x00027000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)t.delta, 4, in_loop(lane) * 4, 0, 0, 0);
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(g.less + at), 0, rows * 4, 0x00027000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)t.less, 4, in_loop(lane) * 4, 0, 0, 0);
     } else if (wave == 2) {
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(a.plan.rows + first), 0, rows * 16, 0x00027000);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)t.rows, 16, in_loop(lane) * 16, 0, 0, 0);
     }
   };
-  float scale2, cap2, slope2;
+  ScoreFactors f;
   auto compute = [&](const QueryTile<D>& t, int tile) {
     const int group = tile * (kQueryTile / kRowGroup) + part;
     if (group * kRowGroup >= a.q_len) return;
@@ -196,36 +198,37 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
     const bool whole = b.all_lo <= k0 && b.all_hi >= k0 + 32 && (group + 1) * kRowGroup <= a.q_len;
     const unsigned char *tq = t.q + part * (kRowGroup * D * 2), *to = t.d_o + part * (kRowGroup * D * 2);
     const int at_row = in_loop(row_base), at_across = in_loop(across_base), r0 = part * kRowGroup + 4 * half;
-    f32x16 s = {}, dp = {};
+    f32x16 s = {}, dp;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) s = mma(S::template row<T>(tq, at_row, 0, i), k[i], s);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {                // dP - delta
+      const f32x4 x = *reinterpret_cast<const f32x4*>(&t.less[r0 + 8 * r]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) dp[4 * r + j] = x[j];
+    }
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) dp = mma(S::template row<T>(to, at_row, 0, i), v[i], dp);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      __builtin_amdgcn_sched_barrier(0);      // (all of them at once would cost 32 registers)
-      const f32x4 l2 = *reinterpret_cast<const f32x4*>(&t.lse2[r0 + 8 * r]), de = *reinterpret_cast<const f32x4*>(&t.delta[r0 + 8 * r]);
+      __builtin_amdgcn_sched_barrier(0);      // (all of them at once would cost 16 registers)
+      const f32x4 base = *reinterpret_cast<const f32x4*>(&t.base[r0 + 8 * r]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int i = 4 * r + j;
-        float x, back = 1.0f;
-        if constexpr (CAP) {
-          const float th = tanh_of(s[i] * scale2);
-          back = __builtin_fmaf(-th, th, 1.0f);
-          x = th * cap2;
-        } else {
-          x = s[i] * scale2;
-        }
-        if constexpr (BIAS) x -= slope2 * fabsf((float)(t.rows[r0 + 8 * r + j].diag - key));
-        s[i] = fast_exp2(x - l2[j]);
-        dp[i] = s[i] * (dp[i] - de[j]) * back;
+        float back, d = 0.0f;
+        if constexpr (BIAS) d = f.slope2 * fabsf((float)(t.rows[r0 + 8 * r + j].diag - key));
+        const float x = shaped<CAP, BIAS>(s[i], f, d, &back);
+        s[i] = fast_exp2(__builtin_fmaf(x, f.mul, base[j]));
+        dp[i] *= s[i];
+        if constexpr (CAP) dp[i] *= back;
       }
     }
     if (!whole) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int2 rb = *reinterpret_cast<const int2*>(&t.rows[r0 + 8 * (i / 4) + i % 4]);   // lo, hi
-        const bool sees = key >= rb.x && key < rb.y;
+        const bool sees = (key >= rb.x) & (key < rb.y);
         s[i] = sees ? s[i] : 0.0f;
         dp[i] = sees ? dp[i] : 0.0f;
       }
@@ -257,14 +260,14 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
       step(&h2, &c2);
       tiles_ready();
       if (h2 < last) load(odd, h2, c2);
-      score_factors<CAP, BIAS>(a.score, head, &scale2, &cap2, &slope2);
+      f = score_factors<CAP, BIAS>(a.score, head);
       compute(even, c);
       head = h2; c = c2;
       if (head >= last) break;
       step(&h2, &c2);
       tiles_ready();
       if (h2 < last) load(even, h2, c2);
-      score_factors<CAP, BIAS>(a.score, head, &scale2, &cap2, &slope2);
+      f = score_factors<CAP, BIAS>(a.score, head);
       compute(odd, c);
       head = h2; c = c2;
     }
@@ -287,7 +290,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
   __syncthreads();
   if (!real) return;
   const RowSource to = (part ? g.dv : g.dk).of(kv);
-  const float by = part ? 1.0f : a.score.scale;
+  const float by = part ? 1.0f : CAP ? 4.0f * a.score.scale : a.score.scale;
   unsigned char* out = const_cast<unsigned char*>(to.base) + (int64_t)key * to.stride;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)

@@ -47,6 +47,8 @@ struct PlanView {
   RowBound* rows;          // q_len
   GroupBound* groups;      // ceil(q_len / kRowGroup)
   int2* cols;              // per kKeyTile keys: the queries that can see any of them
+  int *q_order, *k_order;  // tiles of kPatTile queries and of kKeyTile keys, the ones with the most to do first
+  unsigned* done;          // workgroups of k_plan_cols that are through
   unsigned* seen;          // ceil(q_len / kPatTile) rows of seen_words
   unsigned* seen_by;       // ceil(k_len / kPatTile) rows of seen_by_words
   int* error;
@@ -65,6 +67,19 @@ __device__ __forceinline__ float fast_rcp(float x) { return __builtin_amdgcn_rcp
 
 // tanh(x), given x * 2 log2(e): 1 - 2 / (exp(2x) + 1).  Off by at most about 2e-7 in absolute terms, which is what a capped score needs.
 __device__ __forceinline__ float tanh_of(float x2) { return 1.0f - 2.0f * fast_rcp(fast_exp2(x2) + 1.0f); }
+
+// The largest and the smallest of three, as one instruction each (fmaxf and fminf first bring what might be a signalling NaN into order); NaN is
+// passed over.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float r;
+  asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 // A value that all lanes have, in a scalar register: descriptors and addresses that depend on it then need no loop over the lanes.
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -147,31 +162,40 @@ struct RowSource {
 };
 
 // Brings rows first .. first + ROWS - 1 into a tile, from global memory straight to LDS: each lane asks for the chunk that belongs where its 16
-// bytes land (lane l of an instruction writes 16 l bytes behind a common address).  Rows outside [lo, hi) and chunks behind the head's
-// `bytes` become zero: their lanes' offsets lie outside the buffer that the resource describes.  lo <= hi; a tile begins at most ROWS - 1
-// rows before lo.
+// bytes land (lane l of an instruction writes 16 l bytes behind a common address).  Rows outside [lo, hi) and chunks behind the head's `bytes` become
+// zero: their lanes' offsets lie outside the buffer that the resource describes.  Most tiles have neither: two operations a load.
 template <int D, int ROWS, int THREADS>
-__device__ __forceinline__ void load_tile(const RowSource& src, unsigned char* tile, int first, int lo, int hi, int bytes) {
+struct TileLoader {
   using S = TileShape<D>;
-  constexpr int kLoads = ROWS * S::kChunks / THREADS, kStep = kWave / S::kChunks;   // instructions a wave; rows of one
-  static_assert(kLoads * THREADS == ROWS * S::kChunks && 16 % kStep == 0 && (kLoads * kStep) % 16 == 0, "a wave's rows begin at a multiple of 16");
-  const int wave = uniform(threadIdx.x / kWave), lane = in_loop(lane_id());
-  const int from = first < lo ? lo : first;                      // the buffer begins at the first row that is read
-  const int rows = hi - from < ROWS ? hi - from : ROWS;
-  const unsigned char* base = src.base + (int64_t)from * src.stride;
-  const unsigned stride = (unsigned)src.stride;
-  const unsigned limit = rows > 0 ? (unsigned)(rows - 1) * stride + (unsigned)bytes : 0u;
-  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, limit, 0x00027000);
-  const int r = wave * (kLoads * kStep) + lane / S::kChunks;     // the first instruction's row
-  const int chunk = (lane % S::kChunks) ^ S::swizzle(lane / S::kChunks);
-  const int row0 = r + first - from;
-  const unsigned at0 = (unsigned)row0 * stride;
+  static constexpr int kLoads = ROWS * S::kChunks / THREADS, kStep = kWave / S::kChunks;   // instructions a wave; rows of one
+  static_assert(kLoads * THREADS == ROWS * S::kChunks && 16 % kStep == 0, "whole instructions");
+  int wave, row0, chunk;      // of the first instruction; the swizzle is linear, so those of the others follow without carries
+  unsigned stride, at0;
+  __device__ __forceinline__ TileLoader(int64_t stride_, int lane) : wave(uniform(threadIdx.x / kWave)), stride((unsigned)stride_) {
+    row0 = wave * (kLoads * kStep) + lane / S::kChunks;
+    chunk = ((lane % S::kChunks) ^ S::swizzle(row0)) * 16;
+    at0 = (unsigned)row0 * stride;
+  }
+};
+
+template <int D, int ROWS, int THREADS>
+__device__ __forceinline__ void load_tile(const TileLoader<D, ROWS, THREADS>& l, const unsigned char* base, unsigned char* tile, int first, int lo, int hi, int bytes) {
+  using L = TileLoader<D, ROWS, THREADS>;
+  const unsigned limit = (ROWS - 1) * l.stride + (unsigned)bytes;
+  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)first * l.stride), 0, limit, 0x00027000);
+  if (first >= lo && first + ROWS <= hi && bytes == 2 * D) {
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int c = (chunk ^ S::swizzle(i * kStep)) * 16;          // (the swizzle is linear: rows add up without carries)
-    const unsigned row = (unsigned)(row0 + i * kStep);           // (before lo: very large)
-    const unsigned at = row < (unsigned)rows && c < bytes ? at0 + (unsigned)(i * kStep) * stride + (unsigned)c : 0x80000000u;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(tile + (wave * kLoads + i) * (kWave * 16)), 16, (int)at, 0, 0, 0);
+    for (int i = 0; i < L::kLoads; ++i) {
+      const unsigned at = l.at0 + (unsigned)(i * L::kStep) * l.stride + (unsigned)(l.chunk ^ (L::S::swizzle(i * L::kStep) * 16));
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(tile + (l.wave * L::kLoads + i) * (kWave * 16)), 16, (int)at, 0, 0, 0);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < L::kLoads; ++i) {
+      const int row = first + l.row0 + i * L::kStep, c = l.chunk ^ (L::S::swizzle(i * L::kStep) * 16);
+      const unsigned at = row >= lo && row < hi && c < bytes ? l.at0 + (unsigned)(i * L::kStep) * l.stride + (unsigned)c : 0x80000000u;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(tile + (l.wave * L::kLoads + i) * (kWave * 16)), 16, (int)at, 0, 0, 0);
+    }
   }
 }
 

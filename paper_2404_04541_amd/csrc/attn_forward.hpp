@@ -29,21 +29,24 @@ struct AttnArgs {
 
 struct AttnGrads {
   HeadTensor d_o, dq, dk, dv;
-  float* lse2;            // workspace [heads][q_len]: the rows' logarithms in units of log 2, +inf for a row that sees nothing
-  float* delta;           // workspace [heads][q_len]: the sum of dO * O
+  float* base;            // workspace [heads][q_len]: what a row's exponents add to s * mul (ScoreFactors): add - its logarithm in units of log 2; -inf
+                          // for a row that sees nothing
+  float* less;            // workspace [heads][q_len]: minus the sum of dO * O
 };
 
-// Which head and tile of rows a workgroup has.  Workgroups go to the eight dies in turn: heads that share keys stay on one, whose L2 cache then
-// holds them once.  Last rows first: under a causal mask they are the longest.
-__device__ __forceinline__ void head_and_tile(int n, int heads, int tiles, int* head, int* tile) {
+// Which head and tile a workgroup has.  Workgroups go to the eight dies in turn: heads that share keys stay on one, whose L2 cache then
+// holds them once.  The tiles with the most to do come first.
+__device__ __forceinline__ void head_and_tile(int n, int heads, const int* order, int* head, int* tile) {
+  int rank;
   if (heads % 8 == 0) {
     const int per = heads / 8, j = n / 8;
     *head = uniform(n % 8 * per + j % per);
-    *tile = uniform(tiles - 1 - j / per);
+    rank = uniform(j / per);
   } else {
     *head = uniform(n % heads);
-    *tile = uniform(tiles - 1 - n / heads);
+    rank = uniform(n / heads);
   }
+  *tile = load_uniform(order + rank);
 }
 
 // The first tile at or behind c, before end, whose flag is set; 1 << shift tiles share a flag.
@@ -58,39 +61,41 @@ __device__ __forceinline__ int next_tile(const unsigned* flags, int c, int end, 
   return end;
 }
 
-// Scores of 32 keys by the lane's query in units of log 2.  `away`: diag - (the lane's first key); for a masked pair -inf.
-// keep: tanh of the capped score, for the gradient.
-template <bool CAP, bool BIAS, bool KEEP>
-__device__ __forceinline__ void shape_scores(f32x16& s, float scale2, float cap2, float slope2, float away, f32x16* keep) {
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    float x;
-    if constexpr (CAP) {
-      const float t = tanh_of(s[i] * scale2);
-      if constexpr (KEEP) (*keep)[i] = t;
-      x = t * cap2;
-    } else {
-      x = s[i] * scale2;
-    }
-    if constexpr (BIAS) x -= slope2 * fabsf(away - (float)(8 * (i / 4) + i % 4));
-    s[i] = x;
-  }
+// Factors of a head's scores, and how what shape_scores leaves becomes an exponent: x = s * mul + add.
+struct ScoreFactors { float scale2, cap2, slope2, mul, add; };
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ ScoreFactors score_factors(const ScoreShape& sh, int head) {
+  ScoreFactors f;
+  f.scale2 = CAP ? sh.scale / sh.cap * (2.0f * kLog2e) : sh.scale * kLog2e;
+  f.cap2 = sh.cap * kLog2e;
+  f.slope2 = BIAS ? load_uniform(sh.slopes + head) * kLog2e : 0.0f;
+  f.mul = BIAS ? 1.0f : CAP ? -2.0f * f.cap2 : f.scale2;
+  f.add = CAP && !BIAS ? f.cap2 : 0.0f;
+  return f;
 }
 
-// scale2, cap2, slope2 of shape_scores.
+// A score from a product s, `d` = slope2 |diag - j|.  Without a cap: x = scale2 s - d, in units of log 2 (s itself where there is no distance
+// either).  With one: r = 1 / (1 + e^2y), where y is the score by the cap, so that tanh y = 1 - 2r and 1 - tanh^2 y = 4 (r - r^2) (`back` is a
+// quarter of that); without distances r itself is left, which spares two operations an entry: x = cap2 - 2 cap2 r falls with r.
 template <bool CAP, bool BIAS>
-__device__ __forceinline__ void score_factors(const ScoreShape& sh, int head, float* scale2, float* cap2, float* slope2) {
-  *scale2 = CAP ? sh.scale / sh.cap * (2.0f * kLog2e) : sh.scale * kLog2e;
-  *cap2 = sh.cap * kLog2e;
-  *slope2 = BIAS ? load_uniform(sh.slopes + head) * kLog2e : 0.0f;
+__device__ __forceinline__ float shaped(float s, const ScoreFactors& f, float d, float* back) {
+  if constexpr (CAP) {
+    s = fast_rcp(fast_exp2(s * f.scale2) + 1.0f);
+    if (back) *back = __builtin_fmaf(-s, s, s);
+    if constexpr (BIAS) s = __builtin_fmaf(s, -2.0f * f.cap2, f.cap2 - d);
+  } else if constexpr (BIAS) {
+    s = __builtin_fmaf(s, f.scale2, -d);
+  }
+  return s;
 }
 
 template <typename T, int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
   using S = TileShape<D>;
-  __shared__ __align__(16) unsigned char k_even[kKeyTile * D * 2], v_even[kKeyTile * D * 2], k_odd[kKeyTile * D * 2], v_odd[kKeyTile * D * 2];
+  constexpr int KT = 64, kFlagShift = KT == 32 ? 2 : 1;
+  __shared__ __align__(16) unsigned char k_even[KT * D * 2], v_even[KT * D * 2], k_odd[KT * D * 2], v_odd[KT * D * 2];
   int head, qt;
-  head_and_tile(blockIdx.x, a.heads, a.q_tiles, &head, &qt);
+  head_and_tile(blockIdx.x, a.heads, a.plan.q_order, &head, &qt);
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
   const int row = qt * kPatTile + wave * kRowGroup + (lane & 31);
@@ -108,49 +113,54 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
   lo = uniform(lo);
   hi = uniform(hi);
   mine = {uniform(mine.lo), uniform(mine.hi), uniform(mine.all_lo), uniform(mine.all_hi)};
-  float scale2, cap2, slope2;
-  score_factors<CAP, BIAS>(a.score, head, &scale2, &cap2, &slope2);
+  const ScoreFactors f = score_factors<CAP, BIAS>(a.score, head);
   const RowBound rb = row < a.q_len ? a.plan.rows[row] : RowBound{0, 0, 0, 0};
   vec8<T> q[D / 16];
   load_row<T, D>(a.q.of(head), row, row < a.q_len, a.bytes, half, q);
   const int kv = uniform(head / a.group);
   const RowSource ks = a.k.of(kv), vs = a.v.of(kv);
+  const TileLoader<D, KT, 256> load_k(ks.stride, lane), load_v(vs.stride, lane);
   f32x16 acc[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
   float m = -INFINITY, l = 0.0f;
 
   const unsigned* flags = a.plan.seen_words ? a.plan.seen + (int64_t)qt * a.plan.seen_words : nullptr;
-  const int end = hi > lo ? ceil_div_d(hi, kKeyTile) : 0;
+  const int end = hi > lo ? ceil_div_d(hi, KT) : 0;
 
+  constexpr bool kFalls = CAP && !BIAS;              // the smallest s is the largest score
+  const float hidden = kFalls ? INFINITY : -INFINITY;
   auto compute = [&](const unsigned char* kt, const unsigned char* vt, int k0) {
-    if (mine.lo >= k0 + kKeyTile || mine.hi <= k0) return;
-    const bool whole = mine.all_lo <= k0 && mine.all_hi >= k0 + kKeyTile;
-    const int at_row = in_loop(row_base), at_across = in_loop(across_base);
-    f32x16 s[2];
+    if (mine.lo >= k0 + KT || mine.hi <= k0) return;
+    const bool whole = mine.all_lo <= k0 && mine.all_hi >= k0 + KT;
+    f32x16 s[KT / 32];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < KT / 32; ++t) {
       s[t] = f32x16{};
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) s[t] = mma(S::template row<T>(kt, at_row, 32 * t, i), q[i], s[t]);
+      for (int i = 0; i < D / 16; ++i) s[t] = mma(S::template row<T>(kt, row_base, 32 * t, i), q[i], s[t]);
     }
     if constexpr (CAP || BIAS) {
-      shape_scores<CAP, BIAS, false>(s[0], scale2, cap2, slope2, (float)(rb.diag - k0 - 4 * half), nullptr);
-      shape_scores<CAP, BIAS, false>(s[1], scale2, cap2, slope2, (float)(rb.diag - k0 - 4 * half - 32), nullptr);
+      const float away = (float)(rb.diag - k0 - 4 * half);
+#pragma unroll
+      for (int t = 0; t < KT / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[t][i] = shaped<CAP, BIAS>(s[t][i], f, f.slope2 * fabsf(away - (float)(32 * t + 8 * (i / 4) + i % 4)), nullptr);
     }
-    const float c = CAP || BIAS ? 1.0f : scale2;
     if (!whole) {
       const unsigned span = rb.hi > rb.lo ? rb.hi - rb.lo : 0;
       const int off = k0 + 4 * half - rb.lo;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < KT / 32; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[t][i] = (unsigned)(off + 32 * t + 8 * (i / 4) + i % 4) < span ? s[t][i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) s[t][i] = (unsigned)(off + 32 * t + 8 * (i / 4) + i % 4) < span ? s[t][i] : hidden;
     }
-    float top = fmaxf(s[0][0], s[1][0]);
+    float top = hidden;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(s[0][i], s[1][i]));
-    top = max_halves(top) * c;
+    for (int t = 0; t < KT / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) top = kFalls ? min3(top, s[t][i], s[t][i + 1]) : max3(top, s[t][i], s[t][i + 1]);
+    top = max_halves(__builtin_fmaf(top, f.mul, f.add));
     if (__any(top > m + kLazyMax)) {
       const float now = fmaxf(m, top);
       const float by = m == now ? 1.0f : fast_exp2(m - now);
@@ -159,13 +169,13 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) acc[i] *= by;
     }
-    const float base = m == -INFINITY ? 0.0f : m;
+    const float base = f.add - (m == -INFINITY ? 0.0f : m);
     float sum = 0.0f;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < KT / 32; ++t) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[t][i] = fast_exp2(__builtin_fmaf(s[t][i], c, -base));
+        s[t][i] = fast_exp2(__builtin_fmaf(s[t][i], f.mul, base));
         sum += s[t][i];
       }
       vec8<T> p[2];
@@ -173,28 +183,28 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) acc[i] = mma(S::template across<T>(vt, at_across, 32 * t + 16 * u, i), p[u], acc[i]);
+        for (int i = 0; i < D / 32; ++i) acc[i] = mma(S::template across<T>(vt, across_base, 32 * t + 16 * u, i), p[u], acc[i]);
     }
     l += sum;
   };
   auto load = [&](unsigned char* kt, unsigned char* vt, int k0) {
-    load_tile<D, kKeyTile, 256>(ks, kt, k0, lo, hi, a.bytes);
-    load_tile<D, kKeyTile, 256>(vs, vt, k0, lo, hi, a.bytes);
+    load_tile(load_k, ks.base, kt, k0, lo, hi, a.bytes);
+    load_tile(load_v, vs.base, vt, k0, lo, hi, a.bytes);
   };
 
-  int c = next_tile(flags, hi > lo ? lo / kKeyTile : 0, end, 1);
-  if (c < end) load(k_even, v_even, c * kKeyTile);
+  int c = next_tile(flags, hi > lo ? lo / KT : 0, end, kFlagShift);
+  if (c < end) load(k_even, v_even, c * KT);
   while (c < end) {
-    int next = next_tile(flags, c + 1, end, 1);
+    int next = next_tile(flags, c + 1, end, kFlagShift);
     tiles_ready();                                  // the tile is there, and nobody reads the other one any more
-    if (next < end) load(k_odd, v_odd, next * kKeyTile);
-    compute(k_even, v_even, c * kKeyTile);
+    if (next < end) load(k_odd, v_odd, next * KT);
+    compute(k_even, v_even, c * KT);
     c = next;
     if (c >= end) break;
-    next = next_tile(flags, c + 1, end, 1);
+    next = next_tile(flags, c + 1, end, kFlagShift);
     tiles_ready();
-    if (next < end) load(k_even, v_even, next * kKeyTile);
-    compute(k_odd, v_odd, c * kKeyTile);
+    if (next < end) load(k_even, v_even, next * KT);
+    compute(k_odd, v_odd, c * KT);
     c = next;
   }
 

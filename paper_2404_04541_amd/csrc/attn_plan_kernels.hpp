@@ -78,7 +78,10 @@ __global__ void __launch_bounds__(256) k_plan_rows(MaskView m, PlanView p) {
       bad = 1;
     }
     __syncthreads();
-    if (threadIdx.x == 0) *p.error = bad;
+    if (threadIdx.x == 0) {
+      *p.error = bad;
+      *p.done = 0;
+    }
   }
 }
 
@@ -98,15 +101,81 @@ __device__ __forceinline__ int wave_count_below(int n, int64_t limit, F at) {
   return a;
 }
 
+// Numbers 0 .. n - 1 by falling work(i), as far as 256 steps of the largest tell it, by one workgroup of 256 threads.  (Which of two alike comes first
+// may differ from call to call; it decides only when their workgroups run.)
+constexpr int kOrderKept = 2048;                 // works that LDS holds between the passes; with more tiles they are made again
+template <typename F>
+__device__ __forceinline__ void order_by_work(int n, int* order, F work) {
+  __shared__ unsigned most, count[256];
+  __shared__ int kept[kOrderKept];
+  if (threadIdx.x == 0) most = 1;
+  count[threadIdx.x] = 0;
+  __syncthreads();
+  int top = 0;
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int w = work(i);
+    if (n <= kOrderKept) kept[i] = w;
+    top = w > top ? w : top;
+  }
+  atomicMax(&most, (unsigned)top);
+  __syncthreads();
+  auto bucket = [&](int i) { return 255 - (int)((uint64_t)(n <= kOrderKept ? kept[i] : work(i)) * 255 / most); };
+  for (int i = threadIdx.x; i < n; i += 256) atomicAdd(&count[bucket(i)], 1u);
+  __syncthreads();
+  if (threadIdx.x < kWave) {                     // exclusive sums, four numbers a lane
+    int v[4], sum = 0;
+    for (int j = 0; j < 4; ++j) { v[j] = count[threadIdx.x * 4 + j]; sum += v[j]; }
+    int before = wave_incl_scan(sum) - sum;
+    for (int j = 0; j < 4; ++j) { count[threadIdx.x * 4 + j] = before; before += v[j]; }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += 256) order[atomicAdd(&count[bucket(i)], 1u)] = i;
+}
+
 // The queries that can see any key of a tile, a wave a tile: from the first row that ends behind its first key to before the first that begins
-// behind its last.
+// behind its last.  And both kinds of tiles in order, the tiles of queries by a workgroup of its own, those of keys by the last one to
+// finish: the card holds a few workgroups a compute unit, and long rows that begin late are waited for (two documents of 4000 tokens, tiles
+// from the last row backwards: 1.3 waves a SIMD on average where two fit).  Few tiles all run at once and need no order.
+constexpr int kOrderFrom = 17;
 __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanView p) {
+  const int q_tiles = ceil_div_d(q_len, kPatTile), k_tiles = ceil_div_d(k_len, kKeyTile);
+  if (blockIdx.x == gridDim.x - 1) {
+    if (q_tiles < kOrderFrom) {
+      if ((int)threadIdx.x < q_tiles) p.q_order[threadIdx.x] = q_tiles - 1 - threadIdx.x;
+      return;
+    }
+    order_by_work(q_tiles, p.q_order, [&](int i) {
+      int lo = 0x7fffffff, hi = 0;
+      for (int g = i * (kPatTile / kRowGroup); g < (i + 1) * (kPatTile / kRowGroup) && g < ceil_div_d(q_len, kRowGroup); ++g) {
+        const GroupBound b = p.groups[g];
+        if (b.hi > b.lo) { lo = min(lo, b.lo); hi = max(hi, b.hi); }
+      }
+      return hi > lo ? hi - lo : 0;
+    });
+    return;
+  }
   const int c = blockIdx.x * 4 + threadIdx.x / kWave;
-  if (c >= ceil_div_d(k_len, kKeyTile)) return;
-  const int first = c * kKeyTile, last = k_len - first > kKeyTile ? first + kKeyTile : k_len;
-  const int from = wave_count_below(q_len, (int64_t)first + 1, [&](int i) { return p.rows[i].hi; });
-  const int to = wave_count_below(q_len, last, [&](int i) { return p.rows[i].lo; });
-  if (lane_id() == 0) p.cols[c] = make_int2(from, to);
+  if (c < k_tiles) {
+    const int first = c * kKeyTile, last = k_len - first > kKeyTile ? first + kKeyTile : k_len;
+    const int from = wave_count_below(q_len, (int64_t)first + 1, [&](int i) { return p.rows[i].hi; });
+    const int to = wave_count_below(q_len, last, [&](int i) { return p.rows[i].lo; });
+    if (lane_id() == 0) {
+      p.cols[c] = make_int2(from, to);
+      if (k_tiles < kOrderFrom) p.k_order[c] = c;
+    }
+  }
+  if (k_tiles < kOrderFrom) return;
+  __shared__ bool final;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) final = atomicAdd(p.done, 1u) == gridDim.x - 2;
+  __syncthreads();
+  if (!final) return;
+  __threadfence();
+  order_by_work(k_tiles, p.k_order, [&](int i) {
+    const int2 c = p.cols[i];
+    return c.y > c.x ? c.y - c.x : 0;
+  });
 }
 
 // The pattern's flags, a wave a row of tiles.  Bits are only set, so neither the order of a row's columns nor repeated ones matter.
