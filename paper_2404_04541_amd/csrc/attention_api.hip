@@ -101,6 +101,7 @@ PlanView carve_plan(const spattn_mask* m, void* mem, size_t* bytes) {
   PlanView p{};
   p.error = c.take<int>(1);
   p.done = c.take<unsigned>(1);
+  p.totals = c.take<unsigned long long>(2);
   p.rows = c.take<RowBound>(m->q_len);
   p.groups = c.take<GroupBound>(ceil_div(m->q_len, kRowGroup));
   p.cols = c.take<int2>(ceil_div(m->k_len, kKeyTile));
@@ -164,6 +165,27 @@ AttnArgs attn_args(const spattn_args* a, const spattn_tensor& o, const float* ls
   g.plan = carve_plan(a->mask, const_cast<void*>(a->plan_mem), &bytes);
   g.score = {a->scale, a->cap, a->slopes};
   return g;
+}
+
+// How a pass over `blocks` workgroups, each with at most `tiles` tiles, may be shared: the card holds `resident` of them a compute unit; where the
+// workgroups fill it nothing is shared, nor where the longest is short, else there are places for pieces until it is filled twice.
+int split_pieces(spgemm_context* h, int64_t blocks, int64_t tiles, int resident) {
+  const int64_t slots = (int64_t)h->num_cus * resident;
+  if (blocks == 0 || blocks >= slots || tiles <= 2 * kLeastTiles) return 1;
+  const int64_t most = ceil_div(2 * slots, blocks) + 1;
+  return (int)(most < 64 ? most : 64);
+}
+size_t split_bytes(int64_t blocks, int most, int room) {
+  return most == 1 ? 0 : align_up((size_t)blocks * most * 128 * room * sizeof(float)) + align_up((size_t)blocks * most * kPatTile * sizeof(float2));
+}
+Split split_of(spgemm_context* h, int64_t blocks, int most, int resident, int room, void* mem) {
+  Carve c{static_cast<unsigned char*>(mem)};
+  Split s{most, h->num_cus * resident, nullptr, nullptr};
+  if (most > 1) {
+    s.sums = c.take<f32x4>(blocks * most * 32 * room);
+    s.tops = c.take<float2>(blocks * most * kPatTile);
+  }
+  return s;
 }
 
 // Calls f.template operator()<type, padded head, cap, bias>() for what the arguments say.
@@ -283,11 +305,21 @@ int spattn_forward(spgemm_handle h, const spattn_args* a, spattn_tensor o, float
     if (a->mask->q_len == 0) return SPGEMM_OK;
     if (!lse) return fail(h, SPGEMM_INVALID_ARG, "lse is null");
     if ((rc = ensure_device(h))) return rc;
-    const AttnArgs g = attn_args(a, o, lse);
-    const unsigned grid = (unsigned)(g.q_tiles * g.heads);
+    AttnArgs g = attn_args(a, o, lse);
+    const int64_t blocks = (int64_t)g.q_tiles * g.heads;
+    const int room = a->head_dim <= 64 ? 64 : 128, resident = room == 64 ? 4 : 2;
+    const int most = split_pieces(h, blocks, ceil_div(a->mask->k_len, kKeyTile), resident);
+    void* mem = nullptr;
+    if (most > 1 && (rc = scratch(h, split_bytes(blocks, most, room), &mem))) return rc;
+    g.split = split_of(h, blocks, most, resident, room, mem);
+    const dim3 grid((unsigned)blocks, (unsigned)most);
     dispatch(a->dtype, a->head_dim, a->cap > 0, a->slopes != nullptr, [&](auto type, auto dim, auto cap, auto bias) {
-      k_attn_fwd<decltype(type), dim(), cap(), bias()><<<dim3(grid), dim3(256), 0, h->stream>>>(g);
+      k_attn_fwd<decltype(type), dim(), cap(), bias()><<<grid, dim3(256), 0, h->stream>>>(g);
     });
+    if (most > 1)
+      dispatch(a->dtype, a->head_dim, false, false, [&](auto type, auto dim, auto, auto) {
+        k_attn_join<decltype(type), dim()><<<dim3((unsigned)blocks), dim3(256), 0, h->stream>>>(g);
+      });
     return launched(h);
   });
 }
@@ -303,16 +335,31 @@ int spattn_backward(spgemm_handle h, const spattn_args* a, spattn_tensor o, cons
       return rc;
     if (q_len > 0 && !lse) return fail(h, SPGEMM_INVALID_ARG, "lse is null");
     if ((rc = ensure_device(h))) return rc;
-    const size_t stats = align_up((size_t)a->heads * q_len * sizeof(float));
+    const size_t facts = align_up((size_t)a->heads * ceil_div(q_len, kPatTile) * (kPatTile / kQueryTile) * sizeof(RowFacts));
+    const int64_t q_blocks = ceil_div(q_len, kPatTile) * a->heads, k_blocks = ceil_div(k_len, kKeyTile) * a->kv_heads;
+    const int room = a->head_dim <= 64 ? 64 : 128, resident = room == 64 ? 3 : 2;
+    const int64_t g_heads = a->heads / a->kv_heads;
+    const int q_most = split_pieces(h, q_blocks, ceil_div(k_len, kKeyTile), resident), k_most = split_pieces(h, k_blocks, ceil_div(q_len, kQueryTile) * g_heads, resident);
+    const size_t q_part = split_bytes(q_blocks, q_most, room), k_part = split_bytes(k_blocks, k_most, room);
     void* mem = nullptr;
-    if ((rc = scratch(h, 2 * stats, &mem))) return rc;
+    if ((rc = scratch(h, facts + (q_part > k_part ? q_part : k_part), &mem))) return rc;
+    unsigned char* part = static_cast<unsigned char*>(mem) + facts;      // (one kernel's pieces are joined before the next one's come)
     AttnArgs g = attn_args(a, o, lse);
-    AttnGrads r{view(d_o), view(dq), view(dk), view(dv), static_cast<float*>(mem), reinterpret_cast<float*>(static_cast<unsigned char*>(mem) + stats)};
-    const unsigned q_grid = (unsigned)(g.q_tiles * g.heads), k_grid = (unsigned)(ceil_div(k_len, kKeyTile) * a->kv_heads);
-    dispatch(a->dtype, a->head_dim, a->cap > 0, a->slopes != nullptr, [&](auto type, auto dim, auto cap, auto bias) {
-      if (q_grid) k_attn_dq<decltype(type), dim(), cap(), bias()><<<dim3(q_grid), dim3(256), 0, h->stream>>>(g, r);
-      if (k_grid) k_attn_dkv<decltype(type), dim(), cap(), bias()><<<dim3(k_grid), dim3(256), 0, h->stream>>>(g, r);
-    });
+    AttnGrads r{view(d_o), view(dq), view(dk), view(dv), static_cast<RowFacts*>(mem)};
+    auto launch = [&](auto type, auto dim, auto cap, auto bias) {
+      using T = decltype(type);
+      if (q_blocks) {
+        g.split = split_of(h, q_blocks, q_most, resident, room, part);
+        k_attn_dq<T, dim(), cap(), bias()><<<dim3((unsigned)q_blocks, (unsigned)q_most), dim3(256), 0, h->stream>>>(g, r);
+        if (q_most > 1) k_attn_dq_join<T, dim(), cap()><<<dim3((unsigned)q_blocks), dim3(256), 0, h->stream>>>(g, r);
+      }
+      if (k_blocks) {
+        g.split = split_of(h, k_blocks, k_most, resident, room, part);
+        k_attn_dkv<T, dim(), cap(), bias()><<<dim3((unsigned)k_blocks, (unsigned)k_most), dim3(256), 0, h->stream>>>(g, r);
+        if (k_most > 1) k_attn_dkv_join<T, dim(), cap()><<<dim3((unsigned)k_blocks), dim3(256), 0, h->stream>>>(g, r);
+      }
+    };
+    dispatch(a->dtype, a->head_dim, a->cap > 0, a->slopes != nullptr, launch);
     return launched(h);
   });
 }

@@ -20,20 +20,12 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
   const int row = qt * kPatTile + wave * kRowGroup + (lane & 31);
-  const int groups = ceil_div_d(a.q_len, kRowGroup);
-  int lo = 0x7fffffff, hi = 0;
-  GroupBound mine{0, 0, 0, 0};
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const int n = qt * 4 + w;
-    if (n >= groups) break;
-    const GroupBound b = load_uniform(a.plan.groups + n);
-    if (b.hi > b.lo) { lo = min(lo, b.lo); hi = max(hi, b.hi); }
-    if (w == wave) mine = b;
-  }
-  lo = uniform(lo);
-  hi = uniform(hi);
-  mine = {uniform(mine.lo), uniform(mine.hi), uniform(mine.all_lo), uniform(mine.all_hi)};
+  GroupBound mine;
+  const int2 reach = tile_reach(a, qt, wave, &mine);
+  const int lo = reach.x, hi = reach.y;
+  const int begin = lo / kKeyTile;
+  const Share share = share_of(a.split, ceil_div_d(hi, kKeyTile) - begin, a.split.most > 1 ? load_uniform(a.plan.totals) : 0, a.heads, kLeastTiles, blockIdx.y);
+  if ((int)blockIdx.y >= share.pieces) return;
   const ScoreFactors f = score_factors<CAP, BIAS>(a.score, head);
   const bool real = row < a.q_len;
   const RowBound rb = real ? a.plan.rows[row] : RowBound{0, 0, 0, 0};
@@ -49,10 +41,17 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
     delta = add_halves(delta);
   }
   if (real) {
-    const int64_t at = (int64_t)head * a.q_len + row;
-    const float v = a.lse[at];
+    const float v = a.lse[(int64_t)head * a.q_len + row];
     lse2 = v == -INFINITY ? INFINITY : v * kLog2e;
-    if (half == 0) { g.base[at] = f.add - lse2; g.less[at] = -delta; }
+  }
+  if (half == 0 && blockIdx.y == 0) {
+    RowFacts& facts = g.facts[((int64_t)head * a.q_tiles + qt) * (kPatTile / kQueryTile) + wave / 2];
+    const int at = row % kQueryTile;
+    facts.base[at] = f.add - lse2;
+    facts.less[at] = -delta;
+    facts.lo[at] = rb.lo;
+    facts.hi[at] = rb.hi;
+    facts.diag[at] = rb.diag;
   }
   const float base = f.add - lse2;
   load_row<T, D>(a.q.of(head), row, real, a.bytes, half, q);
@@ -64,7 +63,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
   for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
 
   const unsigned* flags = a.plan.seen_words ? a.plan.seen + (int64_t)qt * a.plan.seen_words : nullptr;
-  const int end = hi > lo ? ceil_div_d(hi, kKeyTile) : 0;
+  const int end = begin + share.last;
 
   auto compute = [&](const unsigned char* kt, const unsigned char* vt, int k0) {
     if (mine.lo >= k0 + kKeyTile || mine.hi <= k0) return;
@@ -100,11 +99,10 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
     }
   };
   auto load = [&](unsigned char* kt, unsigned char* vt, int k0) {
-    load_tile(load_k, ks.base, kt, k0, lo, hi, a.bytes);
-    load_tile(load_v, vs.base, vt, k0, lo, hi, a.bytes);
+    load_tiles(load_k, ks.base, kt, load_v, vs.base, vt, k0, lo, hi, a.bytes);
   };
 
-  int c = next_tile(flags, hi > lo ? lo / kKeyTile : 0, end, 1);
+  int c = next_tile(flags, begin + share.first, end, 1);
   if (c < end) load(k_even, v_even, c * kKeyTile);
   while (c < end) {
     int next = next_tile(flags, c + 1, end, 1);
@@ -120,32 +118,36 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
     c = next;
   }
 
-  if (!real) return;
-  const float by = CAP ? 4.0f * a.score.scale : a.score.scale;
-  const RowSource os = g.dq.of(head);
-  unsigned char* out = const_cast<unsigned char*>(os.base) + (int64_t)row * os.stride;
+  if (share.pieces > 1) {
+    leave_sums<D>(a.split, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, acc);
+    return;
+  }
+  if (real) store_rows<T, D>(g.dq, head, row, half, a.bytes, acc, CAP ? 4.0f * a.score.scale : a.score.scale);
+}
+
+template <typename T, int D, bool CAP>
+__global__ void __launch_bounds__(256) k_attn_dq_join(AttnArgs a, AttnGrads g) {
+  int head, qt;
+  head_and_tile(blockIdx.x, a.heads, a.plan.q_order, &head, &qt);
+  const int lane = lane_id(), wave = uniform(threadIdx.x / kWave), row = qt * kPatTile + wave * kRowGroup + (lane & 31);
+  GroupBound mine;
+  const int2 reach = tile_reach(a, qt, wave, &mine);
+  const Share share = share_of(a.split, ceil_div_d(reach.y, kKeyTile) - reach.x / kKeyTile, load_uniform(a.plan.totals), a.heads, kLeastTiles, 0);
+  if (share.pieces == 1) return;
+  f32x16 acc[D / 32];
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int byte = (32 * i + 8 * r + 4 * half) * 2;
-      T v[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = (T)(acc[i][4 * r + j] * by);
-      if (byte < a.bytes) *reinterpret_cast<u32x2*>(out + byte) = __builtin_bit_cast(u32x2, v);
-    }
+  for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
+  for (int p = 0; p < share.pieces; ++p) add_sums<D>(a.split, (int64_t)p * gridDim.x + blockIdx.x, 1.0f, acc);
+  if (row < a.q_len) store_rows<T, D>(g.dq, head, row, lane >> 5, a.bytes, acc, CAP ? 4.0f * a.score.scale : a.score.scale);
 }
 
 // A workgroup has 64 keys of a key head and goes over their queries in tiles of 64 rows, head by head.  Wave w has keys 32 (w % 2) .. and of every
 // tile the rows 32 (w / 2) ..; keys and values stay in registers as right operands, queries and dO come through LDS with what their exponents and dP
 // begin with and their bounds, one tile ahead.  At the end the two waves of the same keys exchange sums: one adds up dK, the other dV.
-constexpr int kQueryTile = 64;
-
 template <int D>
 struct QueryTile {
   unsigned char q[kQueryTile * D * 2], d_o[kQueryTile * D * 2];
-  float base[kQueryTile], less[kQueryTile];
-  RowBound rows[kQueryTile];
+  RowFacts facts;
 };
 
 template <typename T, int D, bool CAP, bool BIAS>
@@ -168,34 +170,32 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
   const int2 span = load_uniform(a.plan.cols + kt);
   const int lo = uniform(span.x), hi = uniform(span.y);
   const unsigned* flags = a.plan.seen_by_words ? a.plan.seen_by + (int64_t)(kt * kKeyTile / kPatTile) * a.plan.seen_by_words : nullptr;
-  const int end = hi > lo ? ceil_div_d(hi, kQueryTile) : 0;
-  const int begin = next_tile(flags, hi > lo ? lo / kQueryTile : 0, end, 1);
+  const int low = hi > lo ? lo / kQueryTile : 0, end = hi > lo ? ceil_div_d(hi, kQueryTile) : 0, tiles = end - low;
+  const int begin = next_tile(flags, low, end, 1);
+  // the work is a list: all tiles of one head, then of the next
+  const Share share = share_of(a.split, tiles * a.group, a.split.most > 1 ? load_uniform(a.plan.totals + 1) : 0, a.heads, kLeastTiles, blockIdx.y);
+  if ((int)blockIdx.y >= share.pieces) return;
 
   auto load = [&](QueryTile<D>& t, int head, int tile) {
     const int first = tile * kQueryTile;
     const TileLoader<D, kQueryTile, 256> load_q(a.q.stride, in_loop(lane)), load_do(g.d_o.stride, in_loop(lane));   // (made anew: registers are short)
-    load_tile(load_q, a.q.of(head).base, t.q, first, lo, hi, a.bytes);
-    load_tile(load_do, g.d_o.of(head).base, t.d_o, first, lo, hi, a.bytes);
-    const int64_t at = (int64_t)head * a.q_len + first;
-    const unsigned rows = a.q_len - first < kQueryTile ? a.q_len - first : kQueryTile;
-    if (wave == 0) {
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(g.base + at), 0, rows * 4, 0x00027000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)t.base, 4, in_loop(lane) * 4, 0, 0, 0);
-    } else if (wave == 1) {
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(g.less + at), 0, rows * 4, 0x00027000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)t.less, 4, in_loop(lane) * 4, 0, 0, 0);
-    } else if (wave == 2) {
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(a.plan.rows + first), 0, rows * 16, 0x00027000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)t.rows, 16, in_loop(lane) * 16, 0, 0, 0);
-    }
+    load_tiles(load_q, a.q.of(head).base, t.q, load_do, g.d_o.of(head).base, t.d_o, first, lo, hi, a.bytes);
+    const RowFacts* from = g.facts + (int64_t)head * a.q_tiles * (kPatTile / kQueryTile) + tile;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, sizeof(RowFacts), 0x00027000);
+    if (wave == 0) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)&t.facts, 16, in_loop(lane) * 16, 0, 0, 0);
+    if (BIAS && wave == 1) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)t.facts.diag, 4, in_loop(lane) * 4 + 1024, 0, 0, 0);
   };
-  ScoreFactors f;
-  auto compute = [&](const QueryTile<D>& t, int tile) {
+  static_assert(sizeof(RowFacts) == 5 * 256 && offsetof(RowFacts, diag) == 1024, "one load of 16 bytes a lane for all but the diagonals");
+  const int groups = ceil_div_d(a.q_len, kRowGroup);
+  // bounds of the rows that this wave has of a tile
+  auto bounds = [&](int tile) {
     const int group = tile * (kQueryTile / kRowGroup) + part;
-    if (group * kRowGroup >= a.q_len) return;
-    const GroupBound b = load_uniform(a.plan.groups + group);
-    if (b.lo >= k0 + 32 || b.hi <= k0) return;
-    const bool whole = b.all_lo <= k0 && b.all_hi >= k0 + 32 && (group + 1) * kRowGroup <= a.q_len;
+    return group < groups ? load_uniform(a.plan.groups + group) : GroupBound{0, 0, 0, 0};
+  };
+  ScoreFactors f = score_factors<CAP, BIAS>(a.score, kv * a.group);
+  auto compute = [&](const QueryTile<D>& t, const GroupBound& b) {
+    if ((b.lo >= k0 + 32) | (b.hi <= k0)) return;
+    const bool whole = (b.all_lo <= k0) & (b.all_hi >= k0 + 32);
     const unsigned char *tq = t.q + part * (kRowGroup * D * 2), *to = t.d_o + part * (kRowGroup * D * 2);
     const int at_row = in_loop(row_base), at_across = in_loop(across_base), r0 = part * kRowGroup + 4 * half;
     f32x16 s = {}, dp;
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
     for (int i = 0; i < D / 16; ++i) s = mma(S::template row<T>(tq, at_row, 0, i), k[i], s);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {                // dP - delta
-      const f32x4 x = *reinterpret_cast<const f32x4*>(&t.less[r0 + 8 * r]);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(&t.facts.less[r0 + 8 * r]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) dp[4 * r + j] = x[j];
     }
@@ -212,12 +212,12 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       __builtin_amdgcn_sched_barrier(0);      // (all of them at once would cost 16 registers)
-      const f32x4 base = *reinterpret_cast<const f32x4*>(&t.base[r0 + 8 * r]);
+      const f32x4 base = *reinterpret_cast<const f32x4*>(&t.facts.base[r0 + 8 * r]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int i = 4 * r + j;
         float back, d = 0.0f;
-        if constexpr (BIAS) d = f.slope2 * fabsf((float)(t.rows[r0 + 8 * r + j].diag - key));
+        if constexpr (BIAS) d = f.slope2 * fabsf((float)(t.facts.diag[r0 + 8 * r + j] - key));
         const float x = shaped<CAP, BIAS>(s[i], f, d, &back);
         s[i] = fast_exp2(__builtin_fmaf(x, f.mul, base[j]));
         dp[i] *= s[i];
@@ -226,11 +226,15 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
     }
     if (!whole) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int2 rb = *reinterpret_cast<const int2*>(&t.rows[r0 + 8 * (i / 4) + i % 4]);   // lo, hi
-        const bool sees = (key >= rb.x) & (key < rb.y);
-        s[i] = sees ? s[i] : 0.0f;
-        dp[i] = sees ? dp[i] : 0.0f;
+      for (int r = 0; r < 4; ++r) {
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        const i32x4 from = *reinterpret_cast<const i32x4*>(&t.facts.lo[r0 + 8 * r]), until = *reinterpret_cast<const i32x4*>(&t.facts.hi[r0 + 8 * r]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool sees = (key >= from[j]) & (key < until[j]);
+          s[4 * r + j] = sees ? s[4 * r + j] : 0.0f;
+          dp[4 * r + j] = sees ? dp[4 * r + j] : 0.0f;
+        }
       }
     }
     vec8<T> p[2];
@@ -247,29 +251,39 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
   };
 
   // head by head, tile by tile, in pairs of buffers
-  int head = kv * a.group, c = begin;
-  const int last = head + a.group;
-  auto step = [&](int* h, int* tile) {
-    *tile = next_tile(flags, *tile + 1, end, 1);
+  const int head0 = kv * a.group;
+  auto place = [&](int h, int tile) { return (h - head0) * tiles + tile - low; };
+  auto settle = [&](int* h, int* tile) {              // the next tile that the pattern holds, of this head or the next one
+    *tile = next_tile(flags, *tile, end, 1);
     if (*tile >= end) { *tile = begin; ++*h; }
   };
-  if (begin < end) {
-    load(even, head, c);
-    while (head < last) {
-      int h2 = head, c2 = c;
-      step(&h2, &c2);
+  if (begin < end && share.first < share.last) {
+    int head = uniform(head0 + share.first / tiles), c = uniform(low + share.first % tiles);
+    settle(&head, &c);
+    bool more = place(head, c) < share.last;
+    if (more) load(even, head, c);
+    GroupBound here = bounds(c), there{0, 0, 0, 0};
+    auto next_one = [&](QueryTile<D>& t) {            // begins the next tile's loads; its bounds are there when its turn comes
+      int h2 = head, c2 = c + 1;
+      settle(&h2, &c2);
+      more = place(h2, c2) < share.last;
       tiles_ready();
-      if (h2 < last) load(odd, h2, c2);
-      f = score_factors<CAP, BIAS>(a.score, head);
-      compute(even, c);
-      head = h2; c = c2;
-      if (head >= last) break;
-      step(&h2, &c2);
-      tiles_ready();
-      if (h2 < last) load(even, h2, c2);
-      f = score_factors<CAP, BIAS>(a.score, head);
-      compute(odd, c);
-      head = h2; c = c2;
+      if (more) {
+        load(t, h2, c2);
+        there = bounds(c2);
+      }
+      if constexpr (BIAS) f.slope2 = load_uniform(a.score.slopes + head) * kLog2e;
+      head = h2;
+      c = c2;
+    };
+    while (more) {
+      next_one(odd);
+      compute(even, here);
+      here = there;
+      if (!more) break;
+      next_one(even);
+      compute(odd, here);
+      here = there;
     }
   }
 
@@ -288,21 +302,36 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
       room[(4 * i + r) * kWave] = x;
     }
   __syncthreads();
-  if (!real) return;
-  const RowSource to = (part ? g.dv : g.dk).of(kv);
-  const float by = part ? 1.0f : CAP ? 4.0f * a.score.scale : a.score.scale;
-  unsigned char* out = const_cast<unsigned char*>(to.base) + (int64_t)key * to.stride;
+  f32x16 sum[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int byte = (32 * i + 8 * r + 4 * half) * 2;
       const f32x4 x = other[(4 * i + r) * kWave];
-      T y[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = (T)(((part ? dv[i][4 * r + j] : dk[i][4 * r + j]) + x[j]) * by);
-      if (byte < a.bytes) *reinterpret_cast<u32x2*>(out + byte) = __builtin_bit_cast(u32x2, y);
+      for (int j = 0; j < 4; ++j) sum[i][4 * r + j] = (part ? dv[i][4 * r + j] : dk[i][4 * r + j]) + x[j];
     }
+  if (share.pieces > 1) {
+    leave_sums<D>(a.split, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, sum);
+    return;
+  }
+  if (real) store_rows<T, D>(part ? g.dv : g.dk, kv, key, half, a.bytes, sum, part ? 1.0f : CAP ? 4.0f * a.score.scale : a.score.scale);
+}
+
+template <typename T, int D, bool CAP>
+__global__ void __launch_bounds__(256) k_attn_dkv_join(AttnArgs a, AttnGrads g) {
+  int kv, kt;
+  head_and_tile(blockIdx.x, a.heads / a.group, a.plan.k_order, &kv, &kt);
+  const int lane = lane_id(), wave = uniform(threadIdx.x / kWave), part = wave >> 1, key = kt * kKeyTile + (wave & 1) * 32 + (lane & 31);
+  const int2 span = load_uniform(a.plan.cols + kt);
+  const int tiles = span.y > span.x ? ceil_div_d(span.y, kQueryTile) - span.x / kQueryTile : 0;
+  const Share share = share_of(a.split, tiles * a.group, load_uniform(a.plan.totals + 1), a.heads, kLeastTiles, 0);
+  if (share.pieces == 1) return;
+  f32x16 sum[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) sum[i] = f32x16{};
+  for (int p = 0; p < share.pieces; ++p) add_sums<D>(a.split, (int64_t)p * gridDim.x + blockIdx.x, 1.0f, sum);
+  if (key < a.k_len) store_rows<T, D>(part ? g.dv : g.dk, kv, key, lane >> 5, a.bytes, sum, part ? 1.0f : CAP ? 4.0f * a.score.scale : a.score.scale);
 }
 
 }  // namespace spg

@@ -33,6 +33,7 @@ __host__ __device__ constexpr int ceil_div_d(int a, int b) { return a / b + (a %
 
 constexpr int kPatTile = 128;    // rows and columns of a pattern's tiles; queries of a workgroup (forward, dQ)
 constexpr int kKeyTile = 64;     // keys that come through LDS together (forward, dQ), or that a workgroup has (dK, dV)
+constexpr int kQueryTile = 64;   // queries that come through LDS together (dK, dV)
 constexpr int kRowGroup = 32;    // rows whose bounds the plan sums up: a wave's queries
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -49,6 +50,7 @@ struct PlanView {
   int2* cols;              // per kKeyTile keys: the queries that can see any of them
   int *q_order, *k_order;  // tiles of kPatTile queries and of kKeyTile keys, the ones with the most to do first
   unsigned* done;          // workgroups of k_plan_cols that are through
+  unsigned long long* totals;   // tiles of kKeyTile keys that the tiles of queries go over, tiles of kQueryTile queries that those of keys go over
   unsigned* seen;          // ceil(q_len / kPatTile) rows of seen_words
   unsigned* seen_by;       // ceil(k_len / kPatTile) rows of seen_by_words
   int* error;
@@ -179,23 +181,29 @@ struct TileLoader {
 };
 
 template <int D, int ROWS, int THREADS>
-__device__ __forceinline__ void load_tile(const TileLoader<D, ROWS, THREADS>& l, const unsigned char* base, unsigned char* tile, int first, int lo, int hi, int bytes) {
+__device__ __forceinline__ void load_tile(const TileLoader<D, ROWS, THREADS>& l, const unsigned char* base, unsigned char* tile, int first, int lo, int hi, int bytes, bool inside) {
   using L = TileLoader<D, ROWS, THREADS>;
   const unsigned limit = (ROWS - 1) * l.stride + (unsigned)bytes;
-  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)first * l.stride), 0, limit, 0x00027000);
-  if (first >= lo && first + ROWS <= hi && bytes == 2 * D) {
+  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (uint64_t)(unsigned)first * l.stride), 0, limit, 0x00027000);
 #pragma unroll
-    for (int i = 0; i < L::kLoads; ++i) {
-      const unsigned at = l.at0 + (unsigned)(i * L::kStep) * l.stride + (unsigned)(l.chunk ^ (L::S::swizzle(i * L::kStep) * 16));
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(tile + (l.wave * L::kLoads + i) * (kWave * 16)), 16, (int)at, 0, 0, 0);
-    }
+  for (int i = 0; i < L::kLoads; ++i) {
+    const int row = first + l.row0 + i * L::kStep, c = l.chunk ^ (L::S::swizzle(i * L::kStep) * 16);
+    unsigned at = l.at0 + (unsigned)(i * L::kStep) * l.stride + (unsigned)c;
+    if (!inside) at = (row >= lo) & (row < hi) & (c < bytes) ? at : 0x80000000u;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(tile + (l.wave * L::kLoads + i) * (kWave * 16)), 16, (int)at, 0, 0, 0);
+  }
+}
+
+// Two tensors' tiles of the same rows: most are whole, and their loads cost two operations each.
+template <int D, int ROWS, int THREADS>
+__device__ __forceinline__ void load_tiles(const TileLoader<D, ROWS, THREADS>& la, const unsigned char* a, unsigned char* tile_a, const TileLoader<D, ROWS, THREADS>& lb,
+                                           const unsigned char* b, unsigned char* tile_b, int first, int lo, int hi, int bytes) {
+  if ((first >= lo) & (first + ROWS <= hi) & (bytes == 2 * D)) {
+    load_tile(la, a, tile_a, first, lo, hi, bytes, true);
+    load_tile(lb, b, tile_b, first, lo, hi, bytes, true);
   } else {
-#pragma unroll
-    for (int i = 0; i < L::kLoads; ++i) {
-      const int row = first + l.row0 + i * L::kStep, c = l.chunk ^ (L::S::swizzle(i * L::kStep) * 16);
-      const unsigned at = row >= lo && row < hi && c < bytes ? l.at0 + (unsigned)(i * L::kStep) * l.stride + (unsigned)c : 0x80000000u;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(tile + (l.wave * L::kLoads + i) * (kWave * 16)), 16, (int)at, 0, 0, 0);
-    }
+    load_tile(la, a, tile_a, first, lo, hi, bytes, false);
+    load_tile(lb, b, tile_b, first, lo, hi, bytes, false);
   }
 }
 

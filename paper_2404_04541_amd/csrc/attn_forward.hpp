@@ -19,19 +19,48 @@ struct HeadTensor {       // rows of a packed tensor with heads: token t of head
   __device__ __forceinline__ RowSource of(int h) const { return {base + (int64_t)h * head, stride}; }
 };
 
+// Long rows may be shared by several workgroups, each with a stretch of the tiles; their sums are joined by a kernel of their own.  A workgroup
+// leaves the registers of its accumulators as they are: float4 [piece][workgroup][4 D / 32][256], and for rows maximum and sum.
+struct Split {
+  int most;               // pieces that the grid has places for (1: nothing is shared)
+  int slots;              // workgroups that the card holds at once
+  f32x4* sums;
+  float2* tops;           // [piece][workgroup][128]: maximum in units of log 2, sum
+};
+
+// The stretch of n tiles that a piece has.  A piece is as long as the average of what the card's places have to do, and at least `least`: shorter
+// ones cost more in joining than they save.
+struct Share { int first, last, pieces; };
+__device__ __forceinline__ Share share_of(const Split& sp, int n, unsigned long long total, int heads, int least, int piece) {
+  if (sp.most == 1) return {0, n, 1};
+  const long long even = (long long)((total * heads + sp.slots - 1) / sp.slots);
+  int per = even > least ? (int)(even < n ? even : n) : least;
+  per = max(per, ceil_div_d(n, sp.most));
+  const int pieces = n > 2 * least ? ceil_div_d(n, per) : 1;
+  per = ceil_div_d(n, pieces);
+  return {uniform(min(piece * per, n)), uniform(min((piece + 1) * per, n)), uniform(pieces)};
+}
+constexpr int kLeastTiles = 4;
+
 struct AttnArgs {
   HeadTensor q, k, v, o;
   float* lse;             // [heads][q_len], natural logarithm
   int q_len, k_len, heads, group, bytes, q_tiles;
   PlanView plan;
   ScoreShape score;
+  Split split;
+};
+
+// What the kernel of dK and dV needs to know of 64 rows of a head: what their exponents add to s * mul (ScoreFactors; -inf for a row that sees nothing or
+// does not exist), minus the sums of dO * O, and their bounds.
+struct RowFacts {
+  float base[kQueryTile], less[kQueryTile];
+  int lo[kQueryTile], hi[kQueryTile], diag[kQueryTile];
 };
 
 struct AttnGrads {
   HeadTensor d_o, dq, dk, dv;
-  float* base;            // workspace [heads][q_len]: what a row's exponents add to s * mul (ScoreFactors): add - its logarithm in units of log 2; -inf
-                          // for a row that sees nothing
-  float* less;            // workspace [heads][q_len]: minus the sum of dO * O
+  RowFacts* facts;        // workspace [heads][ceil(q_len / 128) * 2]
 };
 
 // Which head and tile a workgroup has.  Workgroups go to the eight dies in turn: heads that share keys stay on one, whose L2 cache then
@@ -89,6 +118,66 @@ __device__ __forceinline__ float shaped(float s, const ScoreFactors& f, float d,
   return s;
 }
 
+// The keys that any query of a tile sees, and the bounds of a wave's rows.
+__device__ __forceinline__ int2 tile_reach(const AttnArgs& a, int tile, int wave, GroupBound* mine) {
+  const int groups = ceil_div_d(a.q_len, kRowGroup);
+  int lo = 0x7fffffff, hi = 0;
+  *mine = GroupBound{0, 0, 0, 0};
+#pragma unroll
+  for (int w = 0; w < kPatTile / kRowGroup; ++w) {
+    const int g = tile * (kPatTile / kRowGroup) + w;
+    if (g >= groups) break;
+    const GroupBound b = load_uniform(a.plan.groups + g);
+    if (b.hi > b.lo) { lo = min(lo, b.lo); hi = max(hi, b.hi); }
+    if (w == wave) *mine = b;
+  }
+  *mine = {uniform(mine->lo), uniform(mine->hi), uniform(mine->all_lo), uniform(mine->all_hi)};
+  return hi > lo ? make_int2(uniform(lo), uniform(hi)) : make_int2(0, 0);
+}
+
+// What both the kernel and the joining one end with: a row's output and logarithm, from its lanes' accumulators.
+template <typename T, int D>
+__device__ __forceinline__ void store_rows(const HeadTensor& to, int head, int row, int half, int bytes, const f32x16* acc, float by) {
+  unsigned char* out = to.base + (int64_t)head * to.head + (int64_t)row * to.stride;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int byte = (32 * i + 8 * r + 4 * half) * 2;
+      T v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = (T)(acc[i][4 * r + j] * by);
+      if (byte < bytes) *reinterpret_cast<u32x2*>(out + byte) = __builtin_bit_cast(u32x2, v);
+    }
+}
+template <typename T, int D>
+__device__ __forceinline__ void finish_rows(const AttnArgs& a, int head, int row, int half, const f32x16* acc, float m, float l) {
+  if (row >= a.q_len) return;
+  if (half == 0) a.lse[(int64_t)head * a.q_len + row] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  store_rows<T, D>(a.o, head, row, half, a.bytes, acc, l == 0.0f ? 0.0f : 1.0f / l);
+}
+
+template <int D>
+__device__ __forceinline__ void leave_sums(const Split& sp, int64_t cell, const f32x16* acc) {
+  f32x4* to = sp.sums + cell * (D / 8 * 256) + threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) to[(4 * i + r) * 256] = f32x4{acc[i][4 * r], acc[i][4 * r + 1], acc[i][4 * r + 2], acc[i][4 * r + 3]};
+}
+template <int D>
+__device__ __forceinline__ void add_sums(const Split& sp, int64_t cell, float by, f32x16* acc) {
+  const f32x4* from = sp.sums + cell * (D / 8 * 256) + threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const f32x4 x = from[(4 * i + r) * 256];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][4 * r + j] = __builtin_fmaf(x[j], by, acc[i][4 * r + j]);
+    }
+}
+
 template <typename T, int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
   using S = TileShape<D>;
@@ -99,20 +188,9 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
   const int row = qt * kPatTile + wave * kRowGroup + (lane & 31);
-  const int groups = ceil_div_d(a.q_len, kRowGroup);
-  int lo = 0x7fffffff, hi = 0;                       // keys that any query of the workgroup sees
-  GroupBound mine{0, 0, 0, 0};
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const int g = qt * 4 + w;
-    if (g >= groups) break;
-    const GroupBound b = load_uniform(a.plan.groups + g);
-    if (b.hi > b.lo) { lo = min(lo, b.lo); hi = max(hi, b.hi); }
-    if (w == wave) mine = b;
-  }
-  lo = uniform(lo);
-  hi = uniform(hi);
-  mine = {uniform(mine.lo), uniform(mine.hi), uniform(mine.all_lo), uniform(mine.all_hi)};
+  GroupBound mine;
+  const int2 reach = tile_reach(a, qt, wave, &mine);
+  const int lo = reach.x, hi = reach.y;
   const ScoreFactors f = score_factors<CAP, BIAS>(a.score, head);
   const RowBound rb = row < a.q_len ? a.plan.rows[row] : RowBound{0, 0, 0, 0};
   vec8<T> q[D / 16];
@@ -126,7 +204,10 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
   float m = -INFINITY, l = 0.0f;
 
   const unsigned* flags = a.plan.seen_words ? a.plan.seen + (int64_t)qt * a.plan.seen_words : nullptr;
-  const int end = hi > lo ? ceil_div_d(hi, KT) : 0;
+  const int begin = lo / KT;
+  const Share share = share_of(a.split, ceil_div_d(hi, KT) - begin, a.split.most > 1 ? load_uniform(a.plan.totals) : 0, a.heads, kLeastTiles, blockIdx.y);
+  if ((int)blockIdx.y >= share.pieces) return;
+  const int end = begin + share.last;
 
   constexpr bool kFalls = CAP && !BIAS;              // the smallest s is the largest score
   const float hidden = kFalls ? INFINITY : -INFINITY;
@@ -188,11 +269,10 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
     l += sum;
   };
   auto load = [&](unsigned char* kt, unsigned char* vt, int k0) {
-    load_tile(load_k, ks.base, kt, k0, lo, hi, a.bytes);
-    load_tile(load_v, vs.base, vt, k0, lo, hi, a.bytes);
+    load_tiles(load_k, ks.base, kt, load_v, vs.base, vt, k0, lo, hi, a.bytes);
   };
 
-  int c = next_tile(flags, hi > lo ? lo / KT : 0, end, kFlagShift);
+  int c = next_tile(flags, begin + share.first, end, kFlagShift);
   if (c < end) load(k_even, v_even, c * KT);
   while (c < end) {
     int next = next_tile(flags, c + 1, end, kFlagShift);
@@ -208,22 +288,41 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
     c = next;
   }
 
-  if (row >= a.q_len) return;
   l = add_halves(l);
-  const float by = l == 0.0f ? 0.0f : 1.0f / l;
-  if (half == 0) a.lse[(int64_t)head * a.q_len + row] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-  const RowSource os = a.o.of(head);
-  unsigned char* out = const_cast<unsigned char*>(os.base) + (int64_t)row * os.stride;
+  if (share.pieces > 1) {
+    const int64_t cell = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    leave_sums<D>(a.split, cell, acc);
+    if (half == 0) a.split.tops[cell * kPatTile + wave * kRowGroup + lane] = make_float2(m, l);
+    return;
+  }
+  finish_rows<T, D>(a, head, row, half, acc, m, l);
+}
+
+// Joins the pieces of rows that were shared, in their order.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
+  int head, qt;
+  head_and_tile(blockIdx.x, a.heads, a.plan.q_order, &head, &qt);
+  const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
+  const int row = qt * kPatTile + wave * kRowGroup + (lane & 31);
+  GroupBound mine;
+  const int2 reach = tile_reach(a, qt, wave, &mine);
+  const Share share = share_of(a.split, ceil_div_d(reach.y, kKeyTile) - reach.x / kKeyTile, load_uniform(a.plan.totals), a.heads, kLeastTiles, 0);
+  if (share.pieces == 1) return;
+  f32x16 acc[D / 32];
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int byte = (32 * i + 8 * r + 4 * half) * 2;
-      T v[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = (T)(acc[i][4 * r + j] * by);
-      if (byte < a.bytes) *reinterpret_cast<u32x2*>(out + byte) = __builtin_bit_cast(u32x2, v);
-    }
+  for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
+  float m = -INFINITY, l = 0.0f;
+  for (int p = 0; p < share.pieces; ++p) m = fmaxf(m, a.split.tops[((int64_t)p * gridDim.x + blockIdx.x) * kPatTile + wave * kRowGroup + (lane & 31)].x);
+  const float base = m == -INFINITY ? 0.0f : m;
+  for (int p = 0; p < share.pieces; ++p) {
+    const int64_t cell = (int64_t)p * gridDim.x + blockIdx.x;
+    const float2 top = a.split.tops[cell * kPatTile + wave * kRowGroup + (lane & 31)];
+    const float by = fast_exp2(top.x - base);
+    l = __builtin_fmaf(top.y, by, l);
+    add_sums<D>(a.split, cell, by, acc);
+  }
+  finish_rows<T, D>(a, head, row, half, acc, m, l);
 }
 
 }  // namespace spg

@@ -81,6 +81,7 @@ __global__ void __launch_bounds__(256) k_plan_rows(MaskView m, PlanView p) {
     if (threadIdx.x == 0) {
       *p.error = bad;
       *p.done = 0;
+      p.totals[0] = p.totals[1] = 0;
     }
   }
 }
@@ -136,22 +137,26 @@ __device__ __forceinline__ void order_by_work(int n, int* order, F work) {
 // behind its last.  And both kinds of tiles in order, the tiles of queries by a workgroup of its own, those of keys by the last one to
 // finish: the card holds a few workgroups a compute unit, and long rows that begin late are waited for (two documents of 4000 tokens, tiles
 // from the last row backwards: 1.3 waves a SIMD on average where two fit).  Few tiles all run at once and need no order.
-constexpr int kOrderFrom = 17;
+constexpr int kOrderQueries = 17, kOrderKeys = 48;   // (tiles of keys are ordered at the end, which costs 5 us)
 __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanView p) {
   const int q_tiles = ceil_div_d(q_len, kPatTile), k_tiles = ceil_div_d(k_len, kKeyTile);
   if (blockIdx.x == gridDim.x - 1) {
-    if (q_tiles < kOrderFrom) {
-      if ((int)threadIdx.x < q_tiles) p.q_order[threadIdx.x] = q_tiles - 1 - threadIdx.x;
-      return;
-    }
-    order_by_work(q_tiles, p.q_order, [&](int i) {
+    auto reach = [&](int i) {
       int lo = 0x7fffffff, hi = 0;
       for (int g = i * (kPatTile / kRowGroup); g < (i + 1) * (kPatTile / kRowGroup) && g < ceil_div_d(q_len, kRowGroup); ++g) {
         const GroupBound b = p.groups[g];
         if (b.hi > b.lo) { lo = min(lo, b.lo); hi = max(hi, b.hi); }
       }
-      return hi > lo ? hi - lo : 0;
-    });
+      return hi > lo ? make_int2(lo, hi) : make_int2(0, 0);
+    };
+    unsigned long long sum = 0;
+    for (int i = threadIdx.x; i < q_tiles; i += 256) {
+      const int2 r = reach(i);
+      sum += ceil_div_d(r.y, kKeyTile) - r.x / kKeyTile;
+      if (q_tiles < kOrderQueries) p.q_order[i] = q_tiles - 1 - i;
+    }
+    if (sum) atomicAdd(&p.totals[0], sum);
+    if (q_tiles >= kOrderQueries) order_by_work(q_tiles, p.q_order, [&](int i) { const int2 r = reach(i); return r.y - r.x; });
     return;
   }
   const int c = blockIdx.x * 4 + threadIdx.x / kWave;
@@ -161,10 +166,11 @@ __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanVie
     const int to = wave_count_below(q_len, last, [&](int i) { return p.rows[i].lo; });
     if (lane_id() == 0) {
       p.cols[c] = make_int2(from, to);
-      if (k_tiles < kOrderFrom) p.k_order[c] = c;
+      if (to > from) atomicAdd(&p.totals[1], (unsigned long long)(ceil_div_d(to, kQueryTile) - from / kQueryTile));
+      if (k_tiles < kOrderKeys) p.k_order[c] = c;
     }
   }
-  if (k_tiles < kOrderFrom) return;
+  if (k_tiles < kOrderKeys) return;
   __shared__ bool final;
   __threadfence();
   __syncthreads();
