@@ -76,15 +76,22 @@ def _dtype(t: torch.Tensor) -> int:
 
 def _tensor(t: torch.Tensor, name: str, tokens: Optional[int] = None, like: Optional[torch.Tensor] = None) -> TensorStruct:
     """[tokens, heads, head_dim] as the library sees it."""
-    if t.dim() != 3 or (t.numel() and t.stride(2) != 1):
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or (strides[2] != 1 and t.numel()):
         raise ValueError(f"{name}: [tokens, heads, head_dim] with a contiguous last dimension is wanted")
     if not t.is_cuda:
         raise ValueError(f"{name}: not on a GPU")
-    if tokens is not None and t.shape[0] != tokens:
-        raise ValueError(f"{name}: {t.shape[0]} tokens, not {tokens}")
+    if tokens is not None and shape[0] != tokens:
+        raise ValueError(f"{name}: {shape[0]} tokens, not {tokens}")
     if like is not None and t.dtype != like.dtype:
         raise TypeError(f"{name}: {t.dtype}, not {like.dtype}")
-    return TensorStruct(t.data_ptr() if t.numel() else None, t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+    return TensorStruct(t.data_ptr() or None, strides[0] if shape[0] > 1 else 0, strides[1] if shape[1] > 1 else 0)
+
+
+def _result(t: torch.Tensor) -> TensorStruct:
+    """A fresh contiguous tensor of this module's own."""
+    strides = t.stride()
+    return TensorStruct(t.data_ptr() or None, strides[0], strides[1])
 
 
 def _array(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: Optional[int] = None) -> Optional[int]:
@@ -94,7 +101,7 @@ def _array(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: Optional
         raise ValueError(f"{name}: a contiguous {dtype} tensor on the GPU is wanted")
     if n is not None and t.numel() != n:
         raise ValueError(f"{name}: {t.numel()} elements, not {n}")
-    return t.data_ptr() if t.numel() else None
+    return t.data_ptr() or None
 
 
 def _slopes(slopes: Optional[torch.Tensor], heads: int) -> Optional[int]:
@@ -156,7 +163,7 @@ def forward(handle: sg.Handle, plan: Plan, q, k, v, scale: Optional[float] = Non
     a = _args(plan, q, k, v, scale, cap, slopes)
     o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     lse = torch.empty((q.shape[1], plan.q_len), dtype=torch.float32, device=q.device)
-    handle._check(lib.spattn_forward(handle.ptr, C.byref(a), _tensor(o, "o"), lse.data_ptr() if lse.numel() else None))
+    handle._check(lib.spattn_forward(handle.ptr, C.byref(a), _result(o), lse.data_ptr() or None))
     return o, lse
 
 
@@ -168,7 +175,7 @@ def backward(handle: sg.Handle, plan: Plan, q, k, v, o, lse, d_o, scale: Optiona
         raise ValueError("o and d_o have q's shape")
     dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
     handle._check(lib.spattn_backward(handle.ptr, C.byref(a), _tensor(o, "o", plan.q_len, q), _array(lse, "lse", torch.float32, q.shape[1] * plan.q_len),
-                                      _tensor(d_o, "d_o", plan.q_len, q), _tensor(dq, "dq"), _tensor(dk, "dk"), _tensor(dv, "dv")))
+                                      _tensor(d_o, "d_o", plan.q_len, q), _result(dq), _result(dk), _result(dv)))
     return dq, dk, dv
 
 
@@ -256,7 +263,7 @@ def attend(handle: sg.Handle, cache: PagedCache, layer: int, table: PageTable, l
     o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     handle._check(lib.spcache_attend(handle.ptr, C.byref(cache._struct), int(layer), C.byref(table.struct(cache)), _array(lens, "lens", torch.int32, n), q_len, heads,
                                      _dtype(q), 1.0 / math.sqrt(d) if scale is None else float(scale), float(cap), _slopes(slopes, heads), int(window),
-                                     _tensor(rows, "q"), _tensor(o.view(n * q_len, heads, d), "o")))
+                                     _tensor(rows, "q"), TensorStruct(o.data_ptr() or None, heads * d, d)))
     return o
 
 

@@ -254,6 +254,27 @@ unsigned copy_grid(spgemm_context* h, const CopyArgs& a, int64_t most) {
   return (unsigned)(units < 1 ? 1 : units < cap ? units : cap);
 }
 
+// The copies, at most so many pages; with `out` their kernel also leaves for the host what the ones before it found, and the call waits.
+int copy_and_report(spgemm_context* h, CopyArgs& g, int64_t most, PageMoves* out) {
+  static_assert(sizeof(PageMoves) <= sizeof(Control), "fits a pinned block");
+  const dim3 grid(copy_grid(h, g, most));
+  if (!out) {
+    k_page_copy<<<grid, dim3(256), 0, h->stream>>>(g);
+    return launched(h);
+  }
+  PinnedLease lease(h->stream);
+  if (!lease.p) return fail(h, SPGEMM_ALLOC_FAILED, "pinned memory");
+  g.report = reinterpret_cast<PageMoves*>(lease.p);
+  lease.written();
+  k_page_copy<<<grid, dim3(256), 0, h->stream>>>(g);
+  int rc = launched(h);
+  if (rc) return rc;
+  HIP_TRY(h, hipStreamSynchronize(h->stream));
+  lease.waited();
+  std::memcpy(out, lease.p, sizeof(PageMoves));
+  return SPGEMM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -314,7 +335,14 @@ int spattn_forward(spgemm_handle h, const spattn_args* a, spattn_tensor o, float
     g.split = split_of(h, blocks, most, resident, room, mem);
     const dim3 grid((unsigned)blocks, (unsigned)most);
     dispatch(a->dtype, a->head_dim, a->cap > 0, a->slopes != nullptr, [&](auto type, auto dim, auto cap, auto bias) {
-      k_attn_fwd<decltype(type), dim(), cap(), bias()><<<grid, dim3(256), 0, h->stream>>>(g);
+      using T = decltype(type);
+      if constexpr (cap() && !bias() && std::is_same<T, bf16_t>::value) {
+        if (a->cap * kLog2e <= kBoundedCap2) {
+          k_attn_fwd<T, dim(), true, false, true><<<grid, dim3(256), 0, h->stream>>>(g);
+          return;
+        }
+      }
+      k_attn_fwd<T, dim(), cap(), bias(), false><<<grid, dim3(256), 0, h->stream>>>(g);
     });
     if (most > 1)
       dispatch(a->dtype, a->head_dim, false, false, [&](auto type, auto dim, auto, auto) {
@@ -400,7 +428,7 @@ int spcache_attend(spgemm_handle h, const spcache* c, int64_t layer, const spgem
     if (q_len >= kMaxTokens || n * q_len >= kMaxTokens) return fail(h, SPGEMM_UNSUPPORTED, "tokens must be below 2^30");
     if ((rc = check_tensor(h, q, n * q_len, "q")) || (rc = check_tensor(h, o, n * q_len, "o"))) return rc;
     const int64_t tiles = ceil_div(q_len * (heads / c->kv_heads), kRows);
-    if (tiles > 65535) return fail(h, SPGEMM_UNSUPPORTED, "too many query rows for a sequence");
+    if (q_len * heads > 65535) return fail(h, SPGEMM_UNSUPPORTED, "too many query rows for a sequence");
     if (n * q_len == 0) return SPGEMM_OK;
     if ((rc = ensure_device(h))) return rc;
     AttendArgs a{};
@@ -409,8 +437,9 @@ int spcache_attend(spgemm_handle h, const spcache* c, int64_t layer, const spgem
     a.tiles = (int)tiles;
     a.window = (int)(window < kMaxTokens ? window : 0);
     a.score = {scale, cap, slopes};
-    // Pages of a workgroup: so many that the workgroups fill the card three times (as many as are resident), at least one for every wave.
-    const int64_t want = (int64_t)h->num_cus * 3;
+    // Pages of a workgroup: so many that the workgroups fill the card twice (three are resident on a compute unit), at least one for every wave.  128
+    // sequences of 3 to 8192 tokens, us filling it once | twice: 51 | 47 and 7 to join; four of 131 071: 172 | 176 and 6.
+    const int64_t want = (int64_t)h->num_cus * 6;
     int64_t chunk = ceil_div(table->nnz * c->kv_heads * tiles, want);
     chunk = chunk < 4 ? 4 : ceil_div(chunk, 4) * 4;
     a.chunk = (int)chunk;
@@ -423,7 +452,7 @@ int spcache_attend(spgemm_handle h, const spcache* c, int64_t layer, const spgem
     if ((rc = scratch(h, part + ml, &mem))) return rc;
     a.part = static_cast<float*>(mem);
     a.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(mem) + part);
-    const dim3 grid((unsigned)slots, (unsigned)c->kv_heads, (unsigned)tiles), join((unsigned)n, (unsigned)c->kv_heads, (unsigned)tiles);
+    const dim3 grid((unsigned)slots, (unsigned)c->kv_heads, (unsigned)tiles), join((unsigned)n, (unsigned)(q_len * heads));
     dispatch(dtype, c->head_dim, cap > 0, slopes != nullptr, [&](auto type, auto dim, auto capped, auto bias) {
       k_cache_attend<decltype(type), dim(), capped(), bias()><<<grid, dim3(256), 0, h->stream>>>(a);
     });
@@ -452,7 +481,8 @@ int spcache_fork(spgemm_handle h, const spcache* c, const spgemm_csr* table, con
       a.out = w.take<PageMoves>(1);
       a.owner = w.take<int32_t>(c->pages);
       a.fresh = w.take<int64_t>(n_out);
-      a.moved = w.take<int2>(n_out);
+      a.src = w.take<int32_t>(n_out);
+      a.dst = w.take<int32_t>(n_out);
       a.used.words = w.take<unsigned>(blocks * (kPageBlock / 32));
       a.used.counts = w.take<unsigned>(blocks);
       return w.used;
@@ -471,13 +501,11 @@ int spcache_fork(spgemm_handle h, const spcache* c, const spgemm_csr* table, con
     k_fork_flags<<<dim3((unsigned)(blocks + 1)), dim3(1024), 0, h->stream>>>(a);
     k_fork_assign<<<dim3(rows4), dim3(256), 0, h->stream>>>(a);
     CopyArgs g = copy_args(c);
-    g.moved = a.moved;
+    g.src = a.src; g.dst = a.dst;
     g.in = a.out;
-    k_page_copy<<<dim3(copy_grid(h, g, n_out)), dim3(256), 0, h->stream>>>(g);
-    if ((rc = launched(h))) return rc;
-    if (!nnz_out) return SPGEMM_OK;
     PageMoves out{};
-    if ((rc = fetch(h, a.out, &out))) return rc;
+    if ((rc = copy_and_report(h, g, n_out, nnz_out ? &out : nullptr))) return rc;
+    if (!nnz_out) return SPGEMM_OK;
     *nnz_out = out.nnz;
     if (out.error == 2) return fail(h, SPGEMM_ALLOC_FAILED, "the cache has no page left");
     return out.error ? fail(h, SPGEMM_INVALID_INPUT, "a parent, length or page out of range, or too little room for the table") : SPGEMM_OK;
@@ -497,8 +525,9 @@ int spcache_compact(spgemm_handle h, const spcache* c, const spgemm_csr* table, 
     auto lay = [&](void* mem) {
       Carve w{static_cast<unsigned char*>(mem)};
       a.out = w.take<PageMoves>(1);
-      a.to = w.take<int32_t>(c->pages);
-      a.moved = w.take<int2>(c->pages / 2 + 1);
+      a.rank = w.take<int32_t>(c->pages);
+      a.movers = w.take<int32_t>(c->pages / 2 + 1);
+      a.holes = w.take<int32_t>(c->pages / 2 + 1);
       a.live.words = w.take<unsigned>(blocks * (kPageBlock / 32));
       a.live.counts = w.take<unsigned>(blocks);
       return w.used;
@@ -518,14 +547,12 @@ int spcache_compact(spgemm_handle h, const spcache* c, const spgemm_csr* table, 
       k_compact_map<<<dim3((unsigned)blocks), dim3(kPageBlock), 0, h->stream>>>(a);
     }
     CopyArgs g = copy_args(c);
-    g.moved = a.moved;
+    g.src = a.movers; g.dst = a.holes;
     g.in = a.out;
-    g.old_page = table->colidx; g.to = a.to; g.new_page = out_pages; g.nnz = table->nnz;
-    k_page_copy<<<dim3(copy_grid(h, g, c->pages / 2)), dim3(256), 0, h->stream>>>(g);
-    if ((rc = launched(h))) return rc;
-    if (!live) return SPGEMM_OK;
+    g.old_page = table->colidx; g.rank = a.rank; g.new_page = out_pages; g.nnz = table->nnz;
     PageMoves out{};
-    if ((rc = fetch(h, a.out, &out))) return rc;
+    if ((rc = copy_and_report(h, g, c->pages / 2, live ? &out : nullptr))) return rc;
+    if (!live) return SPGEMM_OK;
     *live = out.live;
     return out.error ? fail(h, SPGEMM_INVALID_INPUT, "a page of the table is out of range") : SPGEMM_OK;
   });
@@ -542,8 +569,7 @@ int spcache_copy(spgemm_handle h, const spcache* c, int64_t n, const int32_t* sr
     if ((rc = ensure_device(h))) return rc;
     CopyArgs g = copy_args(c);
     g.src = src; g.dst = dst; g.count = n;
-    k_page_copy<<<dim3(copy_grid(h, g, n)), dim3(256), 0, h->stream>>>(g);
-    return launched(h);
+    return copy_and_report(h, g, n, nullptr);
   });
 }
 

@@ -227,4 +227,20 @@ __device__ __forceinline__ void to_operand(const f32x16& v, vec8<T>* out) {
   for (int i = 0; i < 8; ++i) { out[0][i] = (T)v[i]; out[1][i] = (T)v[8 + i]; }
 }
 
+// How many of n ascending numbers at(0) .. at(n - 1) lie below `limit`, by the whole wave: 64 of them are looked at together.
+template <typename F>
+__device__ __forceinline__ int wave_count_below(int n, int64_t limit, F at) {
+  int a = 0;                                     // at(i) < limit for i < a
+  while (n - a > 0) {
+    const int step = ceil_div_d(n - a, kWave);   // lane l looks at the last of its share
+    const int i = a + (lane_id() + 1) * step - 1;
+    const bool below = (int64_t)a + (int64_t)(lane_id() + 1) * step - 1 < n && at(i) < limit;
+    const int shares = __popcll(__ballot(below));
+    a += shares * step;
+    if (step == 1) return a;
+    n = (int64_t)a + step < n ? a + step : n;    // the next share's last number is not below
+  }
+  return a;
+}
+
 }  // namespace spg

@@ -86,22 +86,6 @@ __global__ void __launch_bounds__(256) k_plan_rows(MaskView m, PlanView p) {
   }
 }
 
-// How many of n ascending numbers at(0) .. at(n - 1) lie below `limit`, by the whole wave: 64 of them are looked at together.
-template <typename F>
-__device__ __forceinline__ int wave_count_below(int n, int64_t limit, F at) {
-  int a = 0;                                     // at(i) < limit for i < a
-  while (n - a > 0) {
-    const int step = ceil_div_d(n - a, kWave);   // lane l looks at the last of its share
-    const int i = a + (lane_id() + 1) * step - 1;
-    const bool below = (int64_t)a + (int64_t)(lane_id() + 1) * step - 1 < n && at(i) < limit;
-    const int shares = __popcll(__ballot(below));
-    a += shares * step;
-    if (step == 1) return a;
-    n = (int64_t)a + step < n ? a + step : n;    // the next share's last number is not below
-  }
-  return a;
-}
-
 // Numbers 0 .. n - 1 by falling work(i), as far as 256 steps of the largest tell it, by one workgroup of 256 threads.  (Which of two alike comes first
 // may differ from call to call; it decides only when their workgroups run.)
 constexpr int kOrderKept = 2048;                 // works that LDS holds between the passes; with more tiles they are made again

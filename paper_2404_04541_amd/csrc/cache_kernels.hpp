@@ -29,15 +29,12 @@ struct TableView {        // pages of sequence s: page[ptr[s]] .. page[ptr[s + 1
   int64_t nnz;
 };
 
-// The last s with base(s) <= slot, base ascending, base(0) <= slot.
+// The last s with base(s) <= slot, base ascending; 0 where there is none.  By the whole wave: 64 places are looked at together, so that a table of 4096
+// sequences takes two dependent loads, not twelve.
 template <typename F>
 __device__ __forceinline__ int find_seq(int seqs, int64_t slot, F base) {
-  int a = 0, b = seqs;
-  while (b - a > 1) {
-    const int c = a + (b - a) / 2;
-    if (base(c) <= slot) a = c; else b = c;
-  }
-  return a;
+  const int n = wave_count_below(seqs, slot + 1, base);
+  return n > 0 ? n - 1 : 0;
 }
 
 // ---- append -----------------------------------------------------------------------------------
@@ -237,7 +234,7 @@ __device__ __forceinline__ float add_quarters(float v) {
 // A workgroup has `chunk` pages of a sequence, a key head and 16 query rows; its four waves take the pages in turn and are joined in LDS.
 // Places of chunks: sequence s has ptr[s] / chunk + s and on (as many as its pages can need, found without knowing the lengths on the host).
 template <typename T, int R, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256) k_cache_attend(AttendArgs a) {
+__global__ void __launch_bounds__(256, R == 128 ? 3 : 4) k_cache_attend(AttendArgs a) {
   constexpr int kSteps = R / 32, kOut = R / 16, kLoads = R / 64;
   const int64_t slot = blockIdx.x;
   const int kv = blockIdx.y, tile = blockIdx.z;
@@ -418,38 +415,54 @@ __global__ void __launch_bounds__(256) k_cache_attend(AttendArgs a) {
   }
 }
 
-// Joins a sequence's chunks in their order; rows that no chunk has (no tokens) become zero.  A workgroup has a sequence, a key head, 16 rows.
+// Joins a row's chunks; rows that no chunk has (no tokens) become zero.  A workgroup has a row of a sequence: R / 4 threads go over every
+// (1024 / R)-th chunk, four channels each, and their sums are joined in order.
 template <typename T, int R>
 __global__ void __launch_bounds__(256) k_cache_join(AttendArgs a) {
-  const int s = blockIdx.x, kv = blockIdx.y, tile = blockIdx.z;
+  constexpr int kThreads = R / 4, kLanes = 256 / kThreads;
+  const int s = blockIdx.x, tok = blockIdx.y / a.heads, head = blockIdx.y % a.heads, kv = head / a.group;
   const SeqPages sp = seq_pages(a, s);
   const bool none = sp.first >= sp.last;
   const int c0 = none ? 0 : sp.first / a.chunk, c1 = none ? 0 : (sp.last - 1) / a.chunk + 1;
   if (c1 - c0 == 1) return;
-  const int64_t base_slot = sp.at / a.chunk + s;
-  for (int i = threadIdx.x; i < kRows * R / 4; i += 256) {
-    const int row = i / (R / 4), d = i % (R / 4) * 4;
-    const int rr = tile * kRows + row, tok = rr / a.group;
-    if (tok >= a.q_len || d >= a.c.bytes8) continue;
-    float top = -INFINITY, sum = 0.0f;
-    f32x4 v = {0, 0, 0, 0};
-    for (int c = c0; c < c1; ++c) {
-      const int64_t cell = ((base_slot + c) * gridDim.y + kv) * gridDim.z + tile;
-      const float2 ml = a.part_ml[cell * kRows + row];
-      const f32x4 w = *reinterpret_cast<const f32x4*>(a.part + (cell * kRows + row) * R + d);
-      const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.0f : now;
-      const float f = fast_exp2(top - base), g = fast_exp2(ml.x - base);
-      v = v * f + w * g;
-      sum = sum * f + ml.y * g;
-      top = now;
-    }
-    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const RowSource dst = a.o.of(kv * a.group + rr % a.group);
-    T out[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) out[j] = (T)(v[j] * by);
-    *reinterpret_cast<u32x2*>(const_cast<unsigned char*>(dst.base) + ((int64_t)s * a.q_len + tok) * dst.stride + d * 2) = __builtin_bit_cast(u32x2, out);
+  const int rr = tok * a.group + head % a.group, d = threadIdx.x % kThreads * 4, mine = threadIdx.x / kThreads;
+  const int64_t slot = sp.at / a.chunk + s, kv_heads = a.heads / a.group;
+  float top = -INFINITY, sum = 0.0f;
+  f32x4 v = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int c = c0 + mine; c < c1; c += kLanes) {
+    const int64_t row = (((slot + c) * kv_heads + kv) * a.tiles + rr / kRows) * kRows + rr % kRows;
+    const float2 ml = a.part_ml[row];
+    const f32x4 w = *reinterpret_cast<const f32x4*>(a.part + row * R + d);
+    const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.0f : now;
+    const float f = fast_exp2(top - base), g = fast_exp2(ml.x - base);
+    v = v * f + w * g;
+    sum = sum * f + ml.y * g;
+    top = now;
   }
+  __shared__ __align__(16) f32x4 vs[256];
+  __shared__ float2 mls[kLanes];
+  vs[threadIdx.x] = v;
+  if (d == 0) mls[mine] = make_float2(top, sum);
+  __syncthreads();
+  if (mine || d >= a.c.bytes8) return;
+  float all = -INFINITY, total = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kLanes; ++i) all = fmaxf(all, mls[i].x);
+  all = all == -INFINITY ? 0.0f : all;
+  v = f32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < kLanes; ++i) {
+    const float f = fast_exp2(mls[i].x - all);
+    v += vs[i * kThreads + threadIdx.x] * f;
+    total += mls[i].y * f;
+  }
+  const float by = total == 0.0f ? 0.0f : 1.0f / total;
+  const RowSource dst = a.o.of(head);
+  T out[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) out[j] = (T)(v[j] * by);
+  *reinterpret_cast<u32x2*>(const_cast<unsigned char*>(dst.base) + ((int64_t)s * a.q_len + tok) * dst.stride + d * 2) = __builtin_bit_cast(u32x2, out);
 }
 
 }  // namespace spg

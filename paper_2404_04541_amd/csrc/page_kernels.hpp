@@ -36,7 +36,7 @@ struct ForkArgs {
   int32_t* owner;         // pages: the first row that ends inside the page, -1 where a row has it whole
   int64_t* fresh;         // rows: new pages of the rows before
   PageFlags used;
-  int2* moved;            // rows
+  int32_t *src, *dst;     // rows: the copies
   PageMoves* out;
 };
 
@@ -81,37 +81,35 @@ __device__ __forceinline__ int64_t block_scan(int64_t n, V value, S store) {
   return before;
 }
 
-// The new table's row pointer (the first workgroup); counters and owners cleared (the others).
-__global__ void __launch_bounds__(1024) k_fork_rows(ForkArgs a) {
-  if (blockIdx.x == 0) {
-    __shared__ int bad;
-    if (threadIdx.x == 0) bad = 0;
-    __syncthreads();
-    const int64_t nnz = block_scan(
-        a.rows,
-        [&](int64_t r) {
-          const Kept k = kept_of(a, (int)r);
-          if (!k.ok) bad = 1;
-          return k.need;
-        },
-        [&](int64_t r, int64_t sum) { a.ptr[r] = sum; });
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      a.ptr[a.rows] = nnz;
-      *a.out = PageMoves{bad || nnz > a.room ? 1 : 0, 0u, nnz, 0};
-    }
-    return;
+// The new table's row pointer, by one workgroup of 1024 threads.
+__device__ __forceinline__ void fork_rows(const ForkArgs& a) {
+  __shared__ int bad;
+  if (threadIdx.x == 0) bad = 0;
+  __syncthreads();
+  const int64_t nnz = block_scan(
+      a.rows,
+      [&](int64_t r) {
+        const Kept k = kept_of(a, (int)r);
+        if (!k.ok) bad = 1;
+        return k.need;
+      },
+      [&](int64_t r, int64_t sum) { a.ptr[r] = sum; });
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a.ptr[a.rows] = nnz;
+    *a.out = PageMoves{bad || nnz > a.room ? 1 : 0, 0u, nnz, 0};
   }
-  for (int64_t p = (int64_t)(blockIdx.x - 1) * 1024 + threadIdx.x; p < a.pages; p += (int64_t)(gridDim.x - 1) * 1024) {
+}
+
+__device__ __forceinline__ void fork_clear(const ForkArgs& a, int64_t first, int64_t step) {
+  for (int64_t p = first; p < a.pages; p += step) {
     a.refs[p] = 0;
     a.owner[p] = 0x7fffffff;
   }
 }
 
-// Pages that rows take over, a wave a row.
-__global__ void __launch_bounds__(256) k_fork_gather(ForkArgs a) {
-  const int r = blockIdx.x * 4 + threadIdx.x / kWave;
-  if (r >= a.rows || a.out->error) return;
+// Pages that a row takes over, by a wave.
+__device__ __forceinline__ void fork_gather(const ForkArgs& a, int r) {
   const Kept k = kept_of(a, r);
   const int64_t to = a.ptr[r];
   for (int j = lane_id(); j < k.pages; j += kWave) {
@@ -130,21 +128,21 @@ __device__ __forceinline__ bool copies_last(const ForkArgs& a, int r, const Kept
   return p >= 0 && p < a.pages && a.owner[p] != r;
 }
 
-// Flags of the pages in use, counts of their blocks; the last workgroup sums up how many new pages the rows before each row take.
-__global__ void __launch_bounds__(1024) k_fork_flags(ForkArgs a) {
-  if (a.out->error) return;                        // (set by earlier kernels only)
-  if (blockIdx.x == gridDim.x - 1) {
-    block_scan(
-        a.rows,
-        [&](int64_t r) {
-          const Kept k = kept_of(a, (int)r);
-          return k.need - k.pages + (copies_last(a, (int)r, k) ? 1 : 0);
-        },
-        [&](int64_t r, int64_t sum) { a.fresh[r] = sum; });
-    return;
-  }
+// How many new pages the rows before each row take, by one workgroup of 1024 threads.
+__device__ __forceinline__ void fork_fresh(const ForkArgs& a) {
+  block_scan(
+      a.rows,
+      [&](int64_t r) {
+        const Kept k = kept_of(a, (int)r);
+        return k.need - k.pages + (copies_last(a, (int)r, k) ? 1 : 0);
+      },
+      [&](int64_t r, int64_t sum) { a.fresh[r] = sum; });
+}
+
+// Flags and count of a block of pages in use, by 1024 threads.
+__device__ __forceinline__ void fork_flags(const ForkArgs& a, int64_t block) {
   __shared__ unsigned counts[16];
-  const int64_t p = (int64_t)blockIdx.x * kPageBlock + threadIdx.x;
+  const int64_t p = block * kPageBlock + threadIdx.x;
   const unsigned long long b = __ballot(p < a.pages && a.refs[p] > 0);
   if (lane_id() == 0) {
     const int64_t w = p / 32;
@@ -156,8 +154,9 @@ __global__ void __launch_bounds__(1024) k_fork_flags(ForkArgs a) {
   if (threadIdx.x == 0) {
     unsigned n = 0;
     for (int i = 0; i < 16; ++i) n += counts[i];
-    a.used.counts[blockIdx.x] = n;
+    a.used.counts[block] = n;
   }
+  __syncthreads();
 }
 
 // The k-th page (from 0) that is not in use, or -1.
@@ -178,11 +177,8 @@ __device__ __forceinline__ int64_t free_page(const PageFlags& f, int64_t k) {
   return -1;
 }
 
-// New pages: the k-th new one, rows in order, is the k-th page that no row of the new table kept.  A wave a row.
-__global__ void __launch_bounds__(256) k_fork_assign(ForkArgs a) {
-  const int r = blockIdx.x * 4 + threadIdx.x / kWave;
-  if (r >= a.rows) return;
-  if (a.out->error) return;                        // (set here only where pages run out: then every row that finds none sets it)
+// New pages of a row, by a wave: the k-th new one, rows in order, is the k-th page that no row of the new table kept.
+__device__ __forceinline__ void fork_assign(const ForkArgs& a, int r) {
   const Kept k = kept_of(a, r);
   const int copy = copies_last(a, r, k) ? 1 : 0;
   const int64_t to = a.ptr[r], rank = a.fresh[r];
@@ -193,11 +189,32 @@ __global__ void __launch_bounds__(256) k_fork_assign(ForkArgs a) {
     if (copy && j == 0) {
       const int old = a.t.page[k.at + at];
       atomicSub(&a.refs[old], 1);
-      a.moved[atomicAdd(&a.out->moves, 1u)] = make_int2(old, (int)p);
+      const unsigned i = atomicAdd(&a.out->moves, 1u);
+      a.src[i] = old;
+      a.dst[i] = (int)p;
     }
     a.page[to + at] = (int)p;
     a.refs[p] = 1;
   }
+}
+
+// The steps as kernels.  (An error is set by a step before, or in assigning, where every row that finds no page sets it.)
+__global__ void __launch_bounds__(1024) k_fork_rows(ForkArgs a) {
+  if (blockIdx.x == 0) fork_rows(a);
+  else fork_clear(a, (int64_t)(blockIdx.x - 1) * 1024 + threadIdx.x, (int64_t)(gridDim.x - 1) * 1024);
+}
+__global__ void __launch_bounds__(256) k_fork_gather(ForkArgs a) {
+  const int r = blockIdx.x * 4 + threadIdx.x / kWave;
+  if (r < a.rows && !a.out->error) fork_gather(a, r);
+}
+__global__ void __launch_bounds__(1024) k_fork_flags(ForkArgs a) {
+  if (a.out->error) return;
+  if (blockIdx.x == gridDim.x - 1) fork_fresh(a);
+  else fork_flags(a, blockIdx.x);
+}
+__global__ void __launch_bounds__(256) k_fork_assign(ForkArgs a) {
+  const int r = blockIdx.x * 4 + threadIdx.x / kWave;
+  if (r < a.rows && !a.out->error) fork_assign(a, r);
 }
 
 // ---- pages to the front -------------------------------------------------------------------------
@@ -205,8 +222,8 @@ __global__ void __launch_bounds__(256) k_fork_assign(ForkArgs a) {
 struct CompactArgs {
   TableView t;
   PageFlags live;
-  int32_t* to;            // pages: where a page that moves goes
-  int2* moved;
+  int32_t *movers, *holes;  // pages in use at or behind their number, and the places before it that are free: the i-th goes to the i-th
+  int32_t* rank;          // pages: of a mover, its place among them
   int32_t* page;          // the new table's entries
   PageMoves* out;
 };
@@ -236,22 +253,40 @@ __global__ void __launch_bounds__(256) k_compact_count(CompactArgs a) {
   }
 }
 
-// The i-th page in use at or behind `live` goes to the i-th page before it that is not.
+// Movers and holes in order, a workgroup a block of pages.  Page p has `before` pages in use before it, a hole so p - before holes; of the movers, those
+// before it are the ones in use before p but not before `live`.
 __global__ void __launch_bounds__(kPageBlock) k_compact_map(CompactArgs a) {
   if (a.out->error) return;                        // (set by earlier kernels only)
-  const int64_t live = a.out->live, p = (int64_t)blockIdx.x * kPageBlock + threadIdx.x;
-  if (p < live || p >= a.live.pages) return;
-  const unsigned w = a.live.words[p / 32];
-  if (!(w >> (p % 32) & 1)) return;
-  int64_t before = __popc(w & ((1u << (p % 32)) - 1));      // pages in use before p ...
-  for (int64_t b = 0; b < blockIdx.x; ++b) before += a.live.counts[b];
-  for (int64_t i = p / kPageBlock * (kPageBlock / 32); i < p / 32; ++i) before += __popc(a.live.words[i]);
-  for (int64_t b = 0; b < live / kPageBlock; ++b) before -= a.live.counts[b];   // ... at or behind `live`
-  for (int64_t i = live / kPageBlock * (kPageBlock / 32); i < live / 32; ++i) before -= __popc(a.live.words[i]);
-  if (live % 32) before -= __popc(a.live.words[live / 32] & ((1u << (live % 32)) - 1));
-  const int64_t hole = free_page(a.live, before);
-  a.to[p] = (int)hole;
-  a.moved[atomicAdd(&a.out->moves, 1u)] = make_int2((int)p, (int)hole);
+  __shared__ unsigned sums[2][16], ballots[16];
+  const int64_t live = a.out->live, first = (int64_t)blockIdx.x * kPageBlock, p = first + threadIdx.x;
+  const int wave = threadIdx.x / kWave;
+  // pages in use in all blocks before this one, and in all before `live`
+  unsigned here = 0, front = 0;
+  for (int64_t b = threadIdx.x; b < (int64_t)blockIdx.x || b < live / kPageBlock; b += kPageBlock) {
+    const unsigned n = a.live.counts[b];
+    here += b < (int64_t)blockIdx.x ? n : 0;
+    front += b < live / kPageBlock ? n : 0;
+  }
+  if (threadIdx.x < kPageBlock / 32) {             // the block that `live` cuts
+    const int64_t w = live / kPageBlock * (kPageBlock / 32) + threadIdx.x;
+    if (w * 32 < live) front += __popc(a.live.words[w] & (live - w * 32 < 32 ? (1u << (live - w * 32)) - 1 : ~0u));
+  }
+  for (int d = 1; d < kWave; d *= 2) { here += __shfl_xor(here, d); front += __shfl_xor(front, d); }
+  const bool used = p < a.live.pages && (a.live.words[p / 32] >> (p % 32) & 1);
+  const unsigned long long mask = __ballot(used);
+  if (lane_id() == 0) { sums[0][wave] = here; sums[1][wave] = front; ballots[wave] = __popcll(mask); }
+  __syncthreads();
+  int64_t before = __popcll(mask & ((1ULL << lane_id()) - 1)), in_front = 0;
+  for (int w = 0; w < 16; ++w) {
+    before += sums[0][w] + (w < wave ? ballots[w] : 0);
+    in_front += sums[1][w];
+  }
+  if (used && p >= live) {
+    a.movers[before - in_front] = (int)p;
+    a.rank[p] = (int)(before - in_front);
+  }
+  if (!used && p < live) a.holes[p - before] = (int)p;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.out->moves = (unsigned)(live - in_front);
 }
 
 // ---- copies --------------------------------------------------------------------------------------
@@ -262,12 +297,12 @@ struct CopyArgs {
   int64_t pages;
   int layers, heads;
   int64_t page_bytes;     // of keys (or values) in one layer
-  const int2* moved;      // (from, to), or null:
   const int32_t *src, *dst;
-  int64_t count;          // of src, dst
-  const PageMoves* in;    // of moved
-  // with it the table of k_compact_map's pages
-  const int32_t *old_page, *to;
+  int64_t count;          // of them, or
+  const PageMoves* in;    // ... what kernels before have found
+  PageMoves* report;      // pinned host memory that gets `in`, or null
+  // the table after k_compact_map's moves, or null
+  const int32_t *old_page, *rank;
   int32_t* new_page;
   int64_t nnz;
 };
@@ -276,13 +311,14 @@ constexpr int kCopyPiece = 16384;    // bytes that a workgroup copies at a time:
 
 // Destinations are distinct and no source, so the copies need no order.
 __global__ void __launch_bounds__(256) k_page_copy(CopyArgs a) {
+  if (a.report && blockIdx.x == 0 && threadIdx.x == 0) *a.report = *a.in;
   if (a.in && a.in->error) return;
   const int64_t moves = a.in ? a.in->moves : a.count;
   const int64_t pieces = (a.page_bytes + kCopyPiece - 1) / kCopyPiece, per = 2 * pieces;
   for (int64_t u = blockIdx.x; u < moves * a.layers * per; u += gridDim.x) {
     const int64_t move = u / (a.layers * per), layer = u / per % a.layers;
     const int piece = (int)(u % per);
-    const int64_t from = a.moved ? a.moved[move].x : a.src[move], to = a.moved ? a.moved[move].y : a.dst[move];
+    const int64_t from = a.src[move], to = a.dst[move];
     if (from < 0 || to < 0 || from >= a.pages || to >= a.pages) continue;
     unsigned char* base = piece < pieces ? a.k : a.v;
     const int64_t off = (int64_t)(piece % (int)pieces) * kCopyPiece;
@@ -306,7 +342,7 @@ __global__ void __launch_bounds__(256) k_page_copy(CopyArgs a) {
     const int64_t live = a.in->live;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.nnz; i += (int64_t)gridDim.x * 256) {
       const int p = a.old_page[i];
-      a.new_page[i] = p < live ? p : a.to[p];
+      a.new_page[i] = p < live ? p : a.dst[a.rank[p]];
     }
   }
 }
