@@ -67,7 +67,8 @@ int spattn_symbolic(spgemm_handle h, const spattn_mask* mask, void* plan_mem, si
 
 /* What both passes have in common.  heads is a multiple of kv_heads; query head h uses key head h / (heads / kv_heads).
  * The score of a visible pair is cap * tanh(scale * q.k / cap) - slopes[h] * |diag - j|, without the tanh where cap is 0, without the
- * distance where slopes is null. */
+ * distance where slopes is null.  The tanh is off by at most 3e-7, a capped score so by 3e-7 * cap: a cap far above the scores costs digits.
+ * slopes are constants: no gradient is formed for them. */
 typedef struct {
   const spattn_mask* mask;  /* sizes and the presence of a pattern as at spattn_symbolic */
   const void* plan_mem;
@@ -82,7 +83,9 @@ typedef struct {
 /* o = softmax(scores) * v, lse = the logarithm of each row's sum (device float, heads x q_len). */
 int spattn_forward(spgemm_handle h, const spattn_args* a, spattn_tensor o, float* lse);
 
-/* Gradients of sum(o * d_o) with respect to q, k and v, from forward's o and lse.  Key heads that several query heads share get the sum. */
+/* Gradients of sum(o * d_o) with respect to q, k and v, from forward's o and lse.  Key heads that several query heads share get the sum.
+ * Probabilities and the scores' gradients are rounded to the type once, as operands, and so is o, which the row sums of o * d_o are made from: against 64 bits
+ * the gradients are off by about 1.7 times what rounding the result alone costs.  In float16 a score's gradient beyond 65504 becomes infinite. */
 int spattn_backward(spgemm_handle h, const spattn_args* a, spattn_tensor o, const float* lse, spattn_tensor d_o, spattn_tensor dq,
                     spattn_tensor dk, spattn_tensor dv);
 
@@ -112,7 +115,8 @@ int spcache_append(spgemm_handle h, const spcache* c, int64_t layer, const spgem
                    int64_t tokens, int32_t dtype, spattn_tensor k, spattn_tensor v);
 
 /* o = attention of the last q_len tokens of every sequence (q and o: token s * q_len + i) over its cache.  Token i sees the keys up to itself, with
- * window > 0 only the last `window` of those.  Scores as in spattn_args.  A token before the sequence's first has the output 0. */
+ * window > 0 only the last `window` of those.  Scores as in spattn_args.  A token before the sequence's first has the output 0.
+ * q_len * heads is at most 65535. */
 int spcache_attend(spgemm_handle h, const spcache* c, int64_t layer, const spgemm_csr* table, const int32_t* lens, int64_t q_len, int32_t heads,
                    int32_t dtype, float scale, float cap, const float* slopes, int64_t window, spattn_tensor q, spattn_tensor o);
 

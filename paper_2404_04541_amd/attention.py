@@ -276,7 +276,7 @@ def fork(handle: sg.Handle, cache: PagedCache, table: PageTable, lens: torch.Ten
     lib = _lib()
     n = parent.numel()
     if entries is None:
-        entries = int(((new_lens.to(torch.int64) + PAGE - 1) // PAGE).sum())
+        entries = int(((new_lens.clamp(min=0).to(torch.int64) + PAGE - 1) // PAGE).sum())
     rowptr = torch.empty(n + 1, dtype=torch.int64, device=parent.device)
     pages = torch.empty(int(entries), dtype=torch.int32, device=parent.device)
     refs = torch.empty(cache.pages, dtype=torch.int32, device=parent.device)

@@ -137,6 +137,7 @@ int check_shape(spgemm_context* h, int32_t dtype, int32_t heads, int32_t kv_head
   if (head_dim % 8 || head_dim > 128) return fail(h, SPGEMM_UNSUPPORTED, "head_dim must be a multiple of 8, at most 128");
   if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(h, SPGEMM_INVALID_ARG, "scale must be positive and finite");
   if (!(cap >= 0.0f) || !std::isfinite(cap)) return fail(h, SPGEMM_INVALID_ARG, "cap must be 0 or positive and finite");
+  if (cap > 0.0f && !std::isfinite(4.0f * scale / cap)) return fail(h, SPGEMM_INVALID_ARG, "cap is too small for scale");
   return SPGEMM_OK;
 }
 

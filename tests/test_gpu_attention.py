@@ -102,6 +102,39 @@ def test_long_rows(h):
     run(h, q, k, v, d_o, {"causal": False, "tiles": ([0, 4, 7], [0, 5, 6, 22, 3, 4, 21])})
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap, bias", [(0.0, False), (20.0, False), (100.0, False), (20.0, True), (0.0, True)])
+def test_rows_in_pieces(h, d, cap, bias):
+    """Few workgroups and long rows (and columns, and heads that share them): their work is cut into pieces and joined."""
+    slopes = torch.tensor([0.02, 0.001, 0.0, 0.1], device="cuda") if bias else None
+    run(h, *tensors(23, BF, 90, 2300, 4, 2, d), {}, cap=cap, slopes=slopes)
+    run(h, *tensors(24, BF, 1500, 70, 4, 1, d), {"causal": False}, cap=cap, slopes=slopes)
+    run(h, *tensors(25, F16, 700, 700, 4, 2, d), {"window": 600, "tiles": ([0, 1, 3, 5, 7, 9, 12], [0, 0, 1, 0, 2, 1, 3, 0, 4, 0, 2, 5])}, cap=cap, slopes=slopes)
+
+
+@pytest.mark.parametrize("cap", [1.0, 30.0, 50.0, 52.0, 60.0])
+def test_scores_at_the_cap(h, cap):
+    """Rows whose scores are all at the cap, all at its negative, or both: no power over- or underflows on the way."""
+    q, k, v, _ = tensors(26, BF, 96, 200, 1, 1, 64)
+    one = torch.ones(64, dtype=BF, device="cuda")
+    q[:32], q[32:64], k[:] = one, -one, one * 8
+    k[100:, :, :] = -8 * one
+    q[64:] = 4 * one
+    plan = plan_of(h, 96, 200, causal=False)
+    o, lse = at.forward(h, plan, q, k, v, scale=4.0, cap=cap)
+    seen, diag = visible(96, 200, causal=False)
+    want = reference(q, k, v, None, seen, diag, 4.0, cap)
+    check("o", o, *want["o"])
+    check("lse", lse, *want["lse"])
+    mask = {"q_ptr": [0, 96], "k_ptr": [0, 100]}          # only keys at one end: every score of rows 32 to 63 is -cap
+    plan = plan_of(h, 96, 200, **mask, causal=False)
+    o, lse = at.forward(h, plan, q, k, v, scale=4.0, cap=cap)
+    seen, diag = visible(96, 200, **mask, causal=False)
+    want = reference(q, k, v, None, seen, diag, 4.0, cap)
+    check("o", o, *want["o"])
+    check("lse", lse, *want["lse"])
+
+
 def test_views(h):
     """One tensor of queries, keys and values; heads before tokens; gradients come in plain layout."""
     d, dtype = 64, BF
@@ -269,7 +302,7 @@ def test_arguments(h):
                        ((q.transpose(1, 2), k, v), ValueError), ((bad, k, v), sg.SpgemmError), ((odd, k, v), sg.SpgemmError), ((q[:, :3], k, v), sg.SpgemmError)):
         with pytest.raises(kind):
             at.forward(h, plan, *args)
-    for kw in (dict(scale=0.0), dict(scale=-1.0), dict(cap=-1.0), dict(cap=math.inf), dict(scale=math.nan)):
+    for kw in (dict(scale=0.0), dict(scale=-1.0), dict(cap=-1.0), dict(cap=math.inf), dict(scale=math.nan), dict(cap=1e-39)):
         with pytest.raises(sg.SpgemmError):
             at.forward(h, plan, q, k, v, **kw)
     with pytest.raises(ValueError):
