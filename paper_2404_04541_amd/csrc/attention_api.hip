@@ -105,8 +105,8 @@ PlanView carve_plan(const spattn_mask* m, void* mem, size_t* bytes) {
   p.rows = c.take<RowBound>(m->q_len);
   p.groups = c.take<GroupBound>(ceil_div(m->q_len, kRowGroup));
   p.cols = c.take<int2>(ceil_div(m->k_len, kKeyTile));
-  p.q_order = c.take<int>(q_tiles);
-  p.k_order = c.take<int>(ceil_div(m->k_len, kKeyTile));
+  p.q_order = c.take<int4>(q_tiles);
+  p.k_order = c.take<int4>(ceil_div(m->k_len, kKeyTile));
   if (m->tiles) {
     p.seen_words = (int)ceil_div(k_tiles > 0 ? k_tiles : 1, 32);
     p.seen_by_words = (int)ceil_div(q_tiles > 0 ? q_tiles : 1, 32);
@@ -347,7 +347,7 @@ int spattn_forward(spgemm_handle h, const spattn_args* a, spattn_tensor o, float
     });
     if (most > 1)
       dispatch(a->dtype, a->head_dim, false, false, [&](auto type, auto dim, auto, auto) {
-        k_attn_join<decltype(type), dim()><<<dim3((unsigned)blocks), dim3(256), 0, h->stream>>>(g);
+        k_attn_join<decltype(type), dim()><<<dim3((unsigned)blocks, dim() / 32), dim3(256), 0, h->stream>>>(g);
       });
     return launched(h);
   });
@@ -380,12 +380,12 @@ int spattn_backward(spgemm_handle h, const spattn_args* a, spattn_tensor o, cons
       if (q_blocks) {
         g.split = split_of(h, q_blocks, q_most, resident, room, part);
         k_attn_dq<T, dim(), cap(), bias()><<<dim3((unsigned)q_blocks, (unsigned)q_most), dim3(256), 0, h->stream>>>(g, r);
-        if (q_most > 1) k_attn_dq_join<T, dim(), cap()><<<dim3((unsigned)q_blocks), dim3(256), 0, h->stream>>>(g, r);
+        if (q_most > 1) k_attn_dq_join<T, dim(), cap()><<<dim3((unsigned)q_blocks, dim() / 32), dim3(256), 0, h->stream>>>(g, r);
       }
       if (k_blocks) {
         g.split = split_of(h, k_blocks, k_most, resident, room, part);
         k_attn_dkv<T, dim(), cap(), bias()><<<dim3((unsigned)k_blocks, (unsigned)k_most), dim3(256), 0, h->stream>>>(g, r);
-        if (k_most > 1) k_attn_dkv_join<T, dim(), cap()><<<dim3((unsigned)k_blocks), dim3(256), 0, h->stream>>>(g, r);
+        if (k_most > 1) k_attn_dkv_join<T, dim(), cap()><<<dim3((unsigned)k_blocks, dim() / 32), dim3(256), 0, h->stream>>>(g, r);
       }
     };
     dispatch(a->dtype, a->head_dim, a->cap > 0, a->slopes != nullptr, launch);

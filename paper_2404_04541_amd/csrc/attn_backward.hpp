@@ -15,14 +15,12 @@ template <typename T, int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
   using S = TileShape<D>;
   __shared__ __align__(16) unsigned char k_even[kKeyTile * D * 2], v_even[kKeyTile * D * 2], k_odd[kKeyTile * D * 2], v_odd[kKeyTile * D * 2];
-  int head, qt;
-  head_and_tile(blockIdx.x, a.heads, a.plan.q_order, &head, &qt);
+  const Place at = place_of(blockIdx.x, a.heads, a.plan.q_order);
+  const int head = at.head, qt = at.tile, lo = at.lo, hi = at.hi;
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
   const int row = qt * kPatTile + wave * kRowGroup + (lane & 31);
-  GroupBound mine;
-  const int2 reach = tile_reach(a, qt, wave, &mine);
-  const int lo = reach.x, hi = reach.y;
+  const GroupBound mine = wave_bound(a, qt, wave);
   const int begin = lo / kKeyTile;
   const Share share = share_of(a.split, ceil_div_d(hi, kKeyTile) - begin, a.split.most > 1 ? load_uniform(a.plan.totals) : 0, a.heads, kLeastTiles, blockIdx.y);
   if ((int)blockIdx.y >= share.pieces) return;
@@ -46,12 +44,12 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
   }
   if (half == 0 && blockIdx.y == 0) {
     RowFacts& facts = g.facts[((int64_t)head * a.q_tiles + qt) * (kPatTile / kQueryTile) + wave / 2];
-    const int at = row % kQueryTile;
-    facts.base[at] = f.add - lse2;
-    facts.less[at] = -delta;
-    facts.lo[at] = rb.lo;
-    facts.hi[at] = rb.hi;
-    facts.diag[at] = rb.diag;
+    const int i = row % kQueryTile;
+    facts.base[i] = f.add - lse2;
+    facts.less[i] = -delta;
+    facts.lo[i] = rb.lo;
+    facts.hi[i] = rb.hi;
+    facts.diag[i] = rb.diag;
   }
   const float base = f.add - lse2;
   load_row<T, D>(a.q.of(head), row, real, a.bytes, half, q);
@@ -118,27 +116,21 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
     c = next;
   }
 
-  if (share.pieces > 1) {
-    leave_sums<D>(a.split, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, acc);
-    return;
-  }
-  if (real) store_rows<T, D>(g.dq, head, row, half, a.bytes, acc, CAP ? 4.0f * a.score.scale : a.score.scale);
+  if (share.pieces > 1) leave_sums<D>(a.split, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, acc);
+  else if (real) store_rows<T, D>(g.dq, head, row, half, 0, a.bytes, acc, CAP ? 4.0f * a.score.scale : a.score.scale);
 }
 
 template <typename T, int D, bool CAP>
 __global__ void __launch_bounds__(256) k_attn_dq_join(AttnArgs a, AttnGrads g) {
-  int head, qt;
-  head_and_tile(blockIdx.x, a.heads, a.plan.q_order, &head, &qt);
-  const int lane = lane_id(), wave = uniform(threadIdx.x / kWave), row = qt * kPatTile + wave * kRowGroup + (lane & 31);
-  GroupBound mine;
-  const int2 reach = tile_reach(a, qt, wave, &mine);
-  const Share share = share_of(a.split, ceil_div_d(reach.y, kKeyTile) - reach.x / kKeyTile, load_uniform(a.plan.totals), a.heads, kLeastTiles, 0);
+  const Place at = place_of(blockIdx.x, a.heads, a.plan.q_order);
+  const Share share = share_of(a.split, ceil_div_d(at.hi, kKeyTile) - at.lo / kKeyTile, load_uniform(a.plan.totals), a.heads, kLeastTiles, 0);
   if (share.pieces == 1) return;
-  f32x16 acc[D / 32];
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
-  for (int p = 0; p < share.pieces; ++p) add_sums<D>(a.split, (int64_t)p * gridDim.x + blockIdx.x, 1.0f, acc);
-  if (row < a.q_len) store_rows<T, D>(g.dq, head, row, lane >> 5, a.bytes, acc, CAP ? 4.0f * a.score.scale : a.score.scale);
+  const int lane = lane_id(), row = at.tile * kPatTile + threadIdx.x / kWave * kRowGroup + (lane & 31);
+  const int c0 = blockIdx.y * 32;
+  f32x16 acc = {};
+#pragma unroll 4
+  for (int p = 0; p < share.pieces; ++p) add_sums<D>(a.split, (int64_t)p * gridDim.x + blockIdx.x, c0, 1.0f, acc);
+  if (row < a.q_len) store_rows<T, 32>(g.dq, at.head, row, lane >> 5, c0, a.bytes, &acc, CAP ? 4.0f * a.score.scale : a.score.scale);
 }
 
 // A workgroup has 64 keys of a key head and goes over their queries in tiles of 64 rows, head by head.  Wave w has keys 32 (w % 2) .. and of every
@@ -154,8 +146,8 @@ template <typename T, int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
   using S = TileShape<D>;
   __shared__ __align__(16) QueryTile<D> even, odd;
-  int kv, kt;
-  head_and_tile(blockIdx.x, a.heads / a.group, a.plan.k_order, &kv, &kt);
+  const Place at = place_of(blockIdx.x, a.heads / a.group, a.plan.k_order);
+  const int kv = at.head, kt = at.tile, lo = at.lo, hi = at.hi;
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave), part = wave >> 1;
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
   const int k0 = kt * kKeyTile + (wave & 1) * 32, key = k0 + (lane & 31);
@@ -167,8 +159,6 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) { dk[i] = f32x16{}; dv[i] = f32x16{}; }
 
-  const int2 span = load_uniform(a.plan.cols + kt);
-  const int lo = uniform(span.x), hi = uniform(span.y);
   const unsigned* flags = a.plan.seen_by_words ? a.plan.seen_by + (int64_t)(kt * kKeyTile / kPatTile) * a.plan.seen_by_words : nullptr;
   const int low = hi > lo ? lo / kQueryTile : 0, end = hi > lo ? ceil_div_d(hi, kQueryTile) : 0, tiles = end - low;
   const int begin = next_tile(flags, low, end, 1);
@@ -311,27 +301,22 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) sum[i][4 * r + j] = (part ? dv[i][4 * r + j] : dk[i][4 * r + j]) + x[j];
     }
-  if (share.pieces > 1) {
-    leave_sums<D>(a.split, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, sum);
-    return;
-  }
-  if (real) store_rows<T, D>(part ? g.dv : g.dk, kv, key, half, a.bytes, sum, part ? 1.0f : CAP ? 4.0f * a.score.scale : a.score.scale);
+  if (share.pieces > 1) leave_sums<D>(a.split, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, sum);
+  else if (real) store_rows<T, D>(part ? g.dv : g.dk, kv, key, half, 0, a.bytes, sum, part ? 1.0f : CAP ? 4.0f * a.score.scale : a.score.scale);
 }
 
 template <typename T, int D, bool CAP>
 __global__ void __launch_bounds__(256) k_attn_dkv_join(AttnArgs a, AttnGrads g) {
-  int kv, kt;
-  head_and_tile(blockIdx.x, a.heads / a.group, a.plan.k_order, &kv, &kt);
-  const int lane = lane_id(), wave = uniform(threadIdx.x / kWave), part = wave >> 1, key = kt * kKeyTile + (wave & 1) * 32 + (lane & 31);
-  const int2 span = load_uniform(a.plan.cols + kt);
-  const int tiles = span.y > span.x ? ceil_div_d(span.y, kQueryTile) - span.x / kQueryTile : 0;
+  const Place at = place_of(blockIdx.x, a.heads / a.group, a.plan.k_order);
+  const int tiles = at.hi > at.lo ? ceil_div_d(at.hi, kQueryTile) - at.lo / kQueryTile : 0;
   const Share share = share_of(a.split, tiles * a.group, load_uniform(a.plan.totals + 1), a.heads, kLeastTiles, 0);
   if (share.pieces == 1) return;
-  f32x16 sum[D / 32];
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) sum[i] = f32x16{};
-  for (int p = 0; p < share.pieces; ++p) add_sums<D>(a.split, (int64_t)p * gridDim.x + blockIdx.x, 1.0f, sum);
-  if (key < a.k_len) store_rows<T, D>(part ? g.dv : g.dk, kv, key, lane >> 5, a.bytes, sum, part ? 1.0f : CAP ? 4.0f * a.score.scale : a.score.scale);
+  const int lane = lane_id(), wave = uniform(threadIdx.x / kWave), part = wave >> 1, key = at.tile * kKeyTile + (wave & 1) * 32 + (lane & 31);
+  const int c0 = blockIdx.y * 32;
+  f32x16 sum = {};
+#pragma unroll 4
+  for (int p = 0; p < share.pieces; ++p) add_sums<D>(a.split, (int64_t)p * gridDim.x + blockIdx.x, c0, 1.0f, sum);
+  if (key < a.k_len) store_rows<T, 32>(part ? g.dv : g.dk, at.head, key, lane >> 5, c0, a.bytes, &sum, part ? 1.0f : CAP ? 4.0f * a.score.scale : a.score.scale);
 }
 
 }  // namespace spg

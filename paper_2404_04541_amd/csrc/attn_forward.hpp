@@ -19,8 +19,8 @@ struct HeadTensor {       // rows of a packed tensor with heads: token t of head
   __device__ __forceinline__ RowSource of(int h) const { return {base + (int64_t)h * head, stride}; }
 };
 
-// Long rows may be shared by several workgroups, each with a stretch of the tiles; their sums are joined by a kernel of their own.  A workgroup
-// leaves the registers of its accumulators as they are: float4 [piece][workgroup][4 D / 32][256], and for rows maximum and sum.
+// Long rows may be shared by several workgroups, each with a stretch of the tiles; their sums are joined, in order, by a kernel of their own (joined by the
+// last workgroup to finish, the fences that takes cost every workgroup more than the launch: 18 + 8 | 49 us).  A workgroup leaves the registers of its accumulators as they are: float4 [piece][workgroup][4 D / 32][256], and for rows maximum and sum.
 struct Split {
   int most;               // pieces that the grid has places for (1: nothing is shared)
   int slots;              // workgroups that the card holds at once
@@ -28,12 +28,12 @@ struct Split {
   float2* tops;           // [piece][workgroup][128]: maximum in units of log 2, sum
 };
 
-// The stretch of n tiles that a piece has.  A piece is as long as the average of what the card's places have to do, and at least `least`: shorter
-// ones cost more in joining than they save.
+// The stretch of n tiles that a piece has.  A piece is half as long again as the average of what the card's places have to do, and at least `least`:
+// shorter ones cost more in joining than they save.
 struct Share { int first, last, pieces; };
 __device__ __forceinline__ Share share_of(const Split& sp, int n, unsigned long long total, int heads, int least, int piece) {
   if (sp.most == 1) return {0, n, 1};
-  const long long even = (long long)((total * heads + sp.slots - 1) / sp.slots);
+  const long long even = (long long)((total * heads * 3 + 2 * sp.slots - 1) / (2 * sp.slots));
   int per = even > least ? (int)(even < n ? even : n) : least;
   per = max(per, ceil_div_d(n, sp.most));
   const int pieces = n > 2 * least ? ceil_div_d(n, per) : 1;
@@ -63,19 +63,21 @@ struct AttnGrads {
   RowFacts* facts;        // workspace [heads][ceil(q_len / 128) * 2]
 };
 
-// Which head and tile a workgroup has.  Workgroups go to the eight dies in turn: heads that share keys stay on one, whose L2 cache then
-// holds them once.  The tiles with the most to do come first.
-__device__ __forceinline__ void head_and_tile(int n, int heads, const int* order, int* head, int* tile) {
-  int rank;
+// Which head and tile a workgroup has, and what the tile reaches.  Workgroups go to the eight dies in turn: heads that share keys stay on one, whose
+// L2 cache then holds them once.  The tiles with the most to do come first.
+struct Place { int head, tile, lo, hi; };
+__device__ __forceinline__ Place place_of(int n, int heads, const int4* order) {
+  int head, rank;
   if (heads % 8 == 0) {
     const int per = heads / 8, j = n / 8;
-    *head = uniform(n % 8 * per + j % per);
-    rank = uniform(j / per);
+    head = n % 8 * per + j % per;
+    rank = j / per;
   } else {
-    *head = uniform(n % heads);
-    rank = uniform(n / heads);
+    head = n % heads;
+    rank = n / heads;
   }
-  *tile = load_uniform(order + rank);
+  const int4 o = load_uniform(order + uniform(rank));
+  return {uniform(head), o.x, o.y, o.z};
 }
 
 // The first tile at or behind c, before end, whose flag is set; 1 << shift tiles share a flag.
@@ -118,43 +120,32 @@ __device__ __forceinline__ float shaped(float s, const ScoreFactors& f, float d,
   return s;
 }
 
-// The keys that any query of a tile sees, and the bounds of a wave's rows.
-__device__ __forceinline__ int2 tile_reach(const AttnArgs& a, int tile, int wave, GroupBound* mine) {
-  const int groups = ceil_div_d(a.q_len, kRowGroup);
-  int lo = 0x7fffffff, hi = 0;
-  *mine = GroupBound{0, 0, 0, 0};
-#pragma unroll
-  for (int w = 0; w < kPatTile / kRowGroup; ++w) {
-    const int g = tile * (kPatTile / kRowGroup) + w;
-    if (g >= groups) break;
-    const GroupBound b = load_uniform(a.plan.groups + g);
-    if (b.hi > b.lo) { lo = min(lo, b.lo); hi = max(hi, b.hi); }
-    if (w == wave) *mine = b;
-  }
-  *mine = {uniform(mine->lo), uniform(mine->hi), uniform(mine->all_lo), uniform(mine->all_hi)};
-  return hi > lo ? make_int2(uniform(lo), uniform(hi)) : make_int2(0, 0);
+// The bounds of a wave's rows.
+__device__ __forceinline__ GroupBound wave_bound(const AttnArgs& a, int tile, int wave) {
+  const int g = tile * (kPatTile / kRowGroup) + wave;
+  return g < ceil_div_d(a.q_len, kRowGroup) ? load_uniform(a.plan.groups + g) : GroupBound{0, 0, 0, 0};
 }
 
-// What both the kernel and the joining one end with: a row's output and logarithm, from its lanes' accumulators.
-template <typename T, int D>
-__device__ __forceinline__ void store_rows(const HeadTensor& to, int head, int row, int half, int bytes, const f32x16* acc, float by) {
+// A row's output from its lanes' accumulators, N channels from c0 on; with its logarithm.
+template <typename T, int N>
+__device__ __forceinline__ void store_rows(const HeadTensor& to, int head, int row, int half, int c0, int bytes, const f32x16* acc, float by) {
   unsigned char* out = to.base + (int64_t)head * to.head + (int64_t)row * to.stride;
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i)
+  for (int i = 0; i < N / 32; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int byte = (32 * i + 8 * r + 4 * half) * 2;
+      const int byte = (c0 + 32 * i + 8 * r + 4 * half) * 2;
       T v[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] = (T)(acc[i][4 * r + j] * by);
       if (byte < bytes) *reinterpret_cast<u32x2*>(out + byte) = __builtin_bit_cast(u32x2, v);
     }
 }
-template <typename T, int D>
-__device__ __forceinline__ void finish_rows(const AttnArgs& a, int head, int row, int half, const f32x16* acc, float m, float l) {
+template <typename T, int N>
+__device__ __forceinline__ void finish_rows(const AttnArgs& a, int head, int row, int half, int c0, const f32x16* acc, float m, float l) {
   if (row >= a.q_len) return;
-  if (half == 0) a.lse[(int64_t)head * a.q_len + row] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-  store_rows<T, D>(a.o, head, row, half, a.bytes, acc, l == 0.0f ? 0.0f : 1.0f / l);
+  if (half == 0 && c0 == 0) a.lse[(int64_t)head * a.q_len + row] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  store_rows<T, N>(a.o, head, row, half, c0, a.bytes, acc, l == 0.0f ? 0.0f : 1.0f / l);
 }
 
 template <int D>
@@ -165,17 +156,16 @@ __device__ __forceinline__ void leave_sums(const Split& sp, int64_t cell, const 
 #pragma unroll
     for (int r = 0; r < 4; ++r) to[(4 * i + r) * 256] = f32x4{acc[i][4 * r], acc[i][4 * r + 1], acc[i][4 * r + 2], acc[i][4 * r + 3]};
 }
+// Adds the 32 channels from c0 on of a piece.
 template <int D>
-__device__ __forceinline__ void add_sums(const Split& sp, int64_t cell, float by, f32x16* acc) {
-  const f32x4* from = sp.sums + cell * (D / 8 * 256) + threadIdx.x;
+__device__ __forceinline__ void add_sums(const Split& sp, int64_t cell, int c0, float by, f32x16& acc) {
+  const f32x4* from = sp.sums + cell * (D / 8 * 256) + c0 / 8 * 256 + threadIdx.x;
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i)
+  for (int r = 0; r < 4; ++r) {
+    const f32x4 x = from[r * 256];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const f32x4 x = from[(4 * i + r) * 256];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][4 * r + j] = __builtin_fmaf(x[j], by, acc[i][4 * r + j]);
-    }
+    for (int j = 0; j < 4; ++j) acc[4 * r + j] = __builtin_fmaf(x[j], by, acc[4 * r + j]);
+  }
 }
 
 // With a cap and no distances |x| <= cap2, so that a fixed maximum will do: none is looked for, exchanged or raised (BOUNDED: 8192 tokens 216 -> 201 us).
@@ -190,14 +180,12 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
   using S = TileShape<D>;
   constexpr int KT = 64, kFlagShift = KT == 32 ? 2 : 1;
   __shared__ __align__(16) unsigned char k_even[KT * D * 2], v_even[KT * D * 2], k_odd[KT * D * 2], v_odd[KT * D * 2];
-  int head, qt;
-  head_and_tile(blockIdx.x, a.heads, a.plan.q_order, &head, &qt);
+  const Place at = place_of(blockIdx.x, a.heads, a.plan.q_order);
+  const int head = at.head, qt = at.tile, lo = at.lo, hi = at.hi;
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
   const int row = qt * kPatTile + wave * kRowGroup + (lane & 31);
-  GroupBound mine;
-  const int2 reach = tile_reach(a, qt, wave, &mine);
-  const int lo = reach.x, hi = reach.y;
+  const GroupBound mine = wave_bound(a, qt, wave);
   const ScoreFactors f = score_factors<CAP, BIAS>(a.score, head);
   const RowBound rb = row < a.q_len ? a.plan.rows[row] : RowBound{0, 0, 0, 0};
   vec8<T> q[D / 16];
@@ -304,34 +292,31 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
     if (half == 0) a.split.tops[cell * kPatTile + wave * kRowGroup + lane] = make_float2(m, l);
     return;
   }
-  finish_rows<T, D>(a, head, row, half, acc, m, l);
+  finish_rows<T, D>(a, head, row, half, 0, acc, m, l);
 }
 
-// Joins the pieces of rows that were shared, in their order.
+// A workgroup has 32 channels of a tile's rows.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
-  int head, qt;
-  head_and_tile(blockIdx.x, a.heads, a.plan.q_order, &head, &qt);
-  const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
-  const int row = qt * kPatTile + wave * kRowGroup + (lane & 31);
-  GroupBound mine;
-  const int2 reach = tile_reach(a, qt, wave, &mine);
-  const Share share = share_of(a.split, ceil_div_d(reach.y, kKeyTile) - reach.x / kKeyTile, load_uniform(a.plan.totals), a.heads, kLeastTiles, 0);
+  const Place at = place_of(blockIdx.x, a.heads, a.plan.q_order);
+  const Share share = share_of(a.split, ceil_div_d(at.hi, kKeyTile) - at.lo / kKeyTile, load_uniform(a.plan.totals), a.heads, kLeastTiles, 0);
   if (share.pieces == 1) return;
-  f32x16 acc[D / 32];
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
+  const int lane = lane_id(), row = threadIdx.x / kWave * kRowGroup + (lane & 31), c0 = blockIdx.y * 32;
+  const float2* tops = a.split.tops + (int64_t)blockIdx.x * kPatTile + row;
+  const int64_t step = (int64_t)gridDim.x * kPatTile;
+  f32x16 acc = {};
   float m = -INFINITY, l = 0.0f;
-  for (int p = 0; p < share.pieces; ++p) m = fmaxf(m, a.split.tops[((int64_t)p * gridDim.x + blockIdx.x) * kPatTile + wave * kRowGroup + (lane & 31)].x);
+#pragma unroll 4
+  for (int p = 0; p < share.pieces; ++p) m = fmaxf(m, tops[p * step].x);
   const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll 4
   for (int p = 0; p < share.pieces; ++p) {
-    const int64_t cell = (int64_t)p * gridDim.x + blockIdx.x;
-    const float2 top = a.split.tops[cell * kPatTile + wave * kRowGroup + (lane & 31)];
+    const float2 top = tops[p * step];
     const float by = fast_exp2(top.x - base);
     l = __builtin_fmaf(top.y, by, l);
-    add_sums<D>(a.split, cell, by, acc);
+    add_sums<D>(a.split, (int64_t)p * gridDim.x + blockIdx.x, c0, by, acc);
   }
-  finish_rows<T, D>(a, head, row, half, acc, m, l);
+  finish_rows<T, 32>(a, at.head, at.tile * kPatTile + row, lane >> 5, c0, &acc, m, l);
 }
 
 }  // namespace spg

@@ -86,11 +86,11 @@ __global__ void __launch_bounds__(256) k_plan_rows(MaskView m, PlanView p) {
   }
 }
 
-// Numbers 0 .. n - 1 by falling work(i), as far as 256 steps of the largest tell it, by one workgroup of 256 threads.  (Which of two alike comes first
+// Numbers 0 .. n - 1 by falling work(i), as far as 256 steps of the largest tell it, by one workgroup of 256 threads: store(place, i).  (Which of two alike comes first
 // may differ from call to call; it decides only when their workgroups run.)
 constexpr int kOrderKept = 2048;                 // works that LDS holds between the passes; with more tiles they are made again
-template <typename F>
-__device__ __forceinline__ void order_by_work(int n, int* order, F work) {
+template <typename F, typename S>
+__device__ __forceinline__ void order_by_work(int n, F work, S store) {
   __shared__ unsigned most, count[256];
   __shared__ int kept[kOrderKept];
   if (threadIdx.x == 0) most = 1;
@@ -114,7 +114,7 @@ __device__ __forceinline__ void order_by_work(int n, int* order, F work) {
     for (int j = 0; j < 4; ++j) { count[threadIdx.x * 4 + j] = before; before += v[j]; }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += 256) order[atomicAdd(&count[bucket(i)], 1u)] = i;
+  for (int i = threadIdx.x; i < n; i += 256) store((int)atomicAdd(&count[bucket(i)], 1u), i);
 }
 
 // The queries that can see any key of a tile, a wave a tile: from the first row that ends behind its first key to before the first that begins
@@ -137,10 +137,13 @@ __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanVie
     for (int i = threadIdx.x; i < q_tiles; i += 256) {
       const int2 r = reach(i);
       sum += ceil_div_d(r.y, kKeyTile) - r.x / kKeyTile;
-      if (q_tiles < kOrderQueries) p.q_order[i] = q_tiles - 1 - i;
+      if (q_tiles < kOrderQueries) p.q_order[q_tiles - 1 - i] = make_int4(i, r.x, r.y, 0);
     }
     if (sum) atomicAdd(&p.totals[0], sum);
-    if (q_tiles >= kOrderQueries) order_by_work(q_tiles, p.q_order, [&](int i) { const int2 r = reach(i); return r.y - r.x; });
+    if (q_tiles >= kOrderQueries)
+      order_by_work(
+          q_tiles, [&](int i) { const int2 r = reach(i); return r.y - r.x; },
+          [&](int place, int i) { const int2 r = reach(i); p.q_order[place] = make_int4(i, r.x, r.y, 0); });
     return;
   }
   const int c = blockIdx.x * 4 + threadIdx.x / kWave;
@@ -151,7 +154,7 @@ __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanVie
     if (lane_id() == 0) {
       p.cols[c] = make_int2(from, to);
       if (to > from) atomicAdd(&p.totals[1], (unsigned long long)(ceil_div_d(to, kQueryTile) - from / kQueryTile));
-      if (k_tiles < kOrderKeys) p.k_order[c] = c;
+      if (k_tiles < kOrderKeys) p.k_order[c] = to > from ? make_int4(c, from, to, 0) : make_int4(c, 0, 0, 0);
     }
   }
   if (k_tiles < kOrderKeys) return;
@@ -162,10 +165,10 @@ __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanVie
   __syncthreads();
   if (!final) return;
   __threadfence();
-  order_by_work(k_tiles, p.k_order, [&](int i) {
-    const int2 c = p.cols[i];
-    return c.y > c.x ? c.y - c.x : 0;
-  });
+  auto span = [&](int i) { const int2 c = p.cols[i]; return c.y > c.x ? c : make_int2(0, 0); };
+  order_by_work(
+      k_tiles, [&](int i) { const int2 c = span(i); return c.y - c.x; },
+      [&](int place, int i) { const int2 c = span(i); p.k_order[place] = make_int4(i, c.x, c.y, 0); });
 }
 
 // The pattern's flags, a wave a row of tiles.  Bits are only set, so neither the order of a row's columns nor repeated ones matter.
