@@ -97,7 +97,7 @@ def _result(t: torch.Tensor) -> TensorStruct:
 def _array(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: Optional[int] = None) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dtype} tensor on the GPU is wanted")
     if n is not None and t.numel() != n:
         raise ValueError(f"{name}: {t.numel()} elements, not {n}")
@@ -226,19 +226,16 @@ class PagedCache:
         return cls(head_dim, k, v, *scale)
 
 
-@dataclass
 class PageTable:
-    """Row s lists the pages of sequence s: pages[rowptr[s] : rowptr[s + 1]] (int64, int32)."""
-    rowptr: torch.Tensor
-    pages: torch.Tensor
+    """Row s lists the pages of sequence s: pages[rowptr[s] : rowptr[s + 1]] (int64, int32).  The tensors stay the table's for its life."""
+
+    def __init__(self, rowptr: torch.Tensor, pages: torch.Tensor):
+        self.rowptr, self.pages, self.rows = rowptr, pages, rowptr.numel() - 1
+        self._struct = sg.CsrStruct(self.rows, 0, pages.numel(), _array(rowptr, "table rowptr", torch.int64), _array(pages, "table pages", torch.int32), None, 0)
 
     def struct(self, cache: PagedCache) -> sg.CsrStruct:
-        return sg.CsrStruct(self.rowptr.numel() - 1, cache.pages, self.pages.numel(), _array(self.rowptr, "table rowptr", torch.int64),
-                            _array(self.pages, "table pages", torch.int32), None, 0)
-
-    @property
-    def rows(self) -> int:
-        return self.rowptr.numel() - 1
+        self._struct.cols = cache.pages
+        return self._struct
 
 
 def append(handle: sg.Handle, cache: PagedCache, layer: int, table: PageTable, lens: torch.Tensor, new_ptr: torch.Tensor, k, v) -> None:
@@ -257,13 +254,16 @@ def attend(handle: sg.Handle, cache: PagedCache, layer: int, table: PageTable, l
     if q.dim() != 4 or q.shape[0] != table.rows or q.shape[3] != cache.head_dim:
         raise ValueError("q: [sequences, q_len, heads, head_dim] is wanted")
     n, q_len, heads, d = q.shape
-    if n > 1 and q_len > 1 and q.stride(0) != q_len * q.stride(1):
-        raise ValueError("q: tokens of all sequences at one stride are wanted")
-    rows = q.reshape(n * q_len, heads, d) if q_len == 1 or n == 1 else q.flatten(0, 1)
+    per_sequence, per_token, per_head, per_channel = q.stride()
+    if (n > 1 and q_len > 1 and per_sequence != q_len * per_token) or (per_channel != 1 and q.numel()):
+        raise ValueError("q: tokens of all sequences at one stride and a contiguous last dimension are wanted")
+    if not q.is_cuda:
+        raise ValueError("q: not on a GPU")
     o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    rows = TensorStruct(q.data_ptr() or None, (per_sequence if q_len == 1 else per_token) if n * q_len > 1 else 0, per_head if heads > 1 else 0)
     handle._check(lib.spcache_attend(handle.ptr, C.byref(cache._struct), int(layer), C.byref(table.struct(cache)), _array(lens, "lens", torch.int32, n), q_len, heads,
                                      _dtype(q), 1.0 / math.sqrt(d) if scale is None else float(scale), float(cap), _slopes(slopes, heads), int(window),
-                                     _tensor(rows, "q"), TensorStruct(o.data_ptr() or None, heads * d, d)))
+                                     rows, TensorStruct(o.data_ptr() or None, heads * d, d)))
     return o
 
 
