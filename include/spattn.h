@@ -43,9 +43,9 @@ typedef struct {
  *   hi: the document's end or, with causal, max(k_ptr[d] + prefix[d], diag + 1);  lo: the document's begin or, with window > 0, diag - window + 1.
  * With a pattern, (i, j) is visible only if entry (i / SPATTN_TILE, j / SPATTN_TILE) is stored; its columns may be in any order and
  * repeat, values are not read.  Rows that see nothing have the output 0, the logarithm -inf and no gradient.
- * Queries and keys outside all documents see nothing and are seen by nobody; their elements are not used.  Keys inside one that a
- * query does not see have no weight, but a key or value that is not finite may make those rows NaN that share a tile of 128 with a row
- * that sees it (as 0 * inf does). */
+ * Queries and keys outside all documents see nothing and are seen by nobody; their elements are not used.  Inside one, what a
+ * query does not see has no weight.  But products go over tiles of 128 queries and 128 keys: an element that is not finite may make NaN (as 0 * inf
+ * does) the results of any row or key of a tile that it lies in, whether that sees it or not. */
 typedef struct {
   int64_t q_len, k_len;   /* below 2^30 */
   int64_t docs;           /* 0: one document of everything */

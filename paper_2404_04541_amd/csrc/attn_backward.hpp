@@ -4,7 +4,7 @@
 // delta_i = sum_d dO_id O_id:  dV = P^T dO,  dS = P (dP - delta) (1 - tanh^2),  dQ = scale dS K,  dK = scale dS^T Q.
 // Two kernels, each with a fixed order of its sums (no atomics: the same inputs give the same bits): k_attn_dq goes over the keys of 128
 // queries as the forward kernel does and leaves -delta and what exponents begin with for k_attn_dkv, which goes over the queries, of all heads that share
-// them, of 128 keys.  That computes S and dP twice, seven products where five would do with atomics on dQ in 32 bits.
+// them, of 64 keys.  That computes S and dP twice, seven products where five would do with atomics on dQ in 32 bits.
 // P, dS are rounded to 16 bits once, as operands; all sums are held in 32 bits.
 #pragma once
 #include "attn_forward.hpp"
@@ -100,16 +100,16 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
     load_tiles(load_k, ks.base, kt, load_v, vs.base, vt, k0, lo, hi, a.bytes);
   };
 
-  int c = next_tile(flags, begin + share.first, end, 1);
+  int c = next_tile(flags, begin + share.first, end);
   if (c < end) load(k_even, v_even, c * kKeyTile);
   while (c < end) {
-    int next = next_tile(flags, c + 1, end, 1);
+    int next = next_tile(flags, c + 1, end);
     tiles_ready();
     if (next < end) load(k_odd, v_odd, next * kKeyTile);
     compute(k_even, v_even, c * kKeyTile);
     c = next;
     if (c >= end) break;
-    next = next_tile(flags, c + 1, end, 1);
+    next = next_tile(flags, c + 1, end);
     tiles_ready();
     if (next < end) load(k_even, v_even, next * kKeyTile);
     compute(k_odd, v_odd, c * kKeyTile);
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
 
   const unsigned* flags = a.plan.seen_by_words ? a.plan.seen_by + (int64_t)(kt * kKeyTile / kPatTile) * a.plan.seen_by_words : nullptr;
   const int low = hi > lo ? lo / kQueryTile : 0, end = hi > lo ? ceil_div_d(hi, kQueryTile) : 0, tiles = end - low;
-  const int begin = next_tile(flags, low, end, 1);
+  const int begin = next_tile(flags, low, end);
   // the work is a list: all tiles of one head, then of the next
   const Share share = share_of(a.split, tiles * a.group, a.split.most > 1 ? load_uniform(a.plan.totals + 1) : 0, a.heads, kLeastTiles, blockIdx.y);
   if ((int)blockIdx.y >= share.pieces) return;
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
   const int head0 = kv * a.group;
   auto place = [&](int h, int tile) { return (h - head0) * tiles + tile - low; };
   auto settle = [&](int* h, int* tile) {              // the next tile that the pattern holds, of this head or the next one
-    *tile = next_tile(flags, *tile, end, 1);
+    *tile = next_tile(flags, *tile, end);
     if (*tile >= end) { *tile = begin; ++*h; }
   };
   if (begin < end && share.first < share.last) {

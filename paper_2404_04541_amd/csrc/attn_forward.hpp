@@ -80,14 +80,15 @@ __device__ __forceinline__ Place place_of(int n, int heads, const int4* order) {
   return {uniform(head), o.x, o.y, o.z};
 }
 
-// The first tile at or behind c, before end, whose flag is set; 1 << shift tiles share a flag.
-__device__ __forceinline__ int next_tile(const unsigned* flags, int c, int end, int shift) {
+// The first tile of 64 keys (queries) at or behind c, before end, whose flag is set; two of them share a flag.
+static_assert(kPatTile == 2 * kKeyTile && kPatTile == 2 * kQueryTile, "tiles of a flag");
+__device__ __forceinline__ int next_tile(const unsigned* flags, int c, int end) {
   if (!flags) return c;
   while (c < end) {
-    const int b = c >> shift;
+    const int b = c >> 1;
     const unsigned w = load_uniform(flags + (b >> 5)) >> (b & 31);
     if (w & 1) return c;
-    c = uniform(w ? (b + __ffs(w) - 1) << shift : ((b >> 5) + 1) << (5 + shift));
+    c = uniform(w ? (b + __ffs(w) - 1) << 1 : ((b >> 5) + 1) << 6);
   }
   return end;
 }
@@ -178,8 +179,7 @@ template <typename T, int D, bool CAP, bool BIAS, bool BOUNDED>
 __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
   static_assert(!BOUNDED || (CAP && !BIAS), "bounded scores");
   using S = TileShape<D>;
-  constexpr int KT = 64, kFlagShift = KT == 32 ? 2 : 1;
-  __shared__ __align__(16) unsigned char k_even[KT * D * 2], v_even[KT * D * 2], k_odd[KT * D * 2], v_odd[KT * D * 2];
+  __shared__ __align__(16) unsigned char k_even[kKeyTile * D * 2], v_even[kKeyTile * D * 2], k_odd[kKeyTile * D * 2], v_odd[kKeyTile * D * 2];
   const Place at = place_of(blockIdx.x, a.heads, a.plan.q_order);
   const int head = at.head, qt = at.tile, lo = at.lo, hi = at.hi;
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
@@ -192,34 +192,54 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
   load_row<T, D>(a.q.of(head), row, row < a.q_len, a.bytes, half, q);
   const int kv = uniform(head / a.group);
   const RowSource ks = a.k.of(kv), vs = a.v.of(kv);
-  const TileLoader<D, KT, 256> load_k(ks.stride, lane), load_v(vs.stride, lane);
+  const TileLoader<D, kKeyTile, 256> load_k(ks.stride, lane), load_v(vs.stride, lane);
   f32x16 acc[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
   float m = BOUNDED ? fixed_maximum(f.cap2) : -INFINITY, l = 0.0f;
 
   const unsigned* flags = a.plan.seen_words ? a.plan.seen + (int64_t)qt * a.plan.seen_words : nullptr;
-  const int begin = lo / KT;
-  const Share share = share_of(a.split, ceil_div_d(hi, KT) - begin, a.split.most > 1 ? load_uniform(a.plan.totals) : 0, a.heads, kLeastTiles, blockIdx.y);
+  const int begin = lo / kKeyTile;
+  const Share share = share_of(a.split, ceil_div_d(hi, kKeyTile) - begin, a.split.most > 1 ? load_uniform(a.plan.totals) : 0, a.heads, kLeastTiles, blockIdx.y);
   if ((int)blockIdx.y >= share.pieces) return;
   const int end = begin + share.last;
 
+  float key_part[16];                                // slope2 times a key's place among a lane's
+  int least_diag = 0;                                // of the wave's rows
+  if constexpr (BIAS && !CAP) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) key_part[i] = f.slope2 * (float)(8 * (i / 4) + i % 4);
+    least_diag = row < a.q_len ? rb.diag : 0x7fffffff;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) least_diag = min(least_diag, __shfl_xor(least_diag, d));
+    least_diag = uniform(least_diag);
+  }
   constexpr bool kFalls = CAP && !BIAS;              // the smallest s is the largest score
   const float hidden = kFalls ? INFINITY : -INFINITY;
   auto compute = [&](const unsigned char* kt, const unsigned char* vt, int k0) {
-    if (mine.lo >= k0 + KT || mine.hi <= k0) return;
-    const bool whole = mine.all_lo <= k0 && mine.all_hi >= k0 + KT;
-    f32x16 s[KT / 32];
+    if (mine.lo >= k0 + kKeyTile || mine.hi <= k0) return;
+    const bool whole = mine.all_lo <= k0 && mine.all_hi >= k0 + kKeyTile;
+    f32x16 s[kKeyTile / 32];
 #pragma unroll
-    for (int t = 0; t < KT / 32; ++t) {
+    for (int t = 0; t < kKeyTile / 32; ++t) {
       s[t] = f32x16{};
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) s[t] = mma(S::template row<T>(kt, row_base, 32 * t, i), q[i], s[t]);
     }
-    if constexpr (CAP || BIAS) {
+    // Where every key of a tile is at or before every row, a distance is a row's part less a key's: the key's goes into the product's scaling, the row's
+    // into the exponent, and an entry costs two operations less (5003 queries through a pattern: 174 -> 169.5 us).
+    float row_part[kKeyTile / 32] = {};
+    if (BIAS && !CAP && whole && k0 + kKeyTile - 1 <= least_diag) {
+#pragma unroll
+      for (int t = 0; t < kKeyTile / 32; ++t) {
+        row_part[t] = f.slope2 * (float)(k0 + 4 * half + 32 * t - rb.diag);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[t][i] = __builtin_fmaf(s[t][i], f.scale2, key_part[i]);
+      }
+    } else if constexpr (CAP || BIAS) {
       const float away = (float)(rb.diag - k0 - 4 * half);
 #pragma unroll
-      for (int t = 0; t < KT / 32; ++t)
+      for (int t = 0; t < kKeyTile / 32; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[t][i] = shaped<CAP, BIAS>(s[t][i], f, f.slope2 * fabsf(away - (float)(32 * t + 8 * (i / 4) + i % 4)), nullptr);
     }
@@ -227,17 +247,20 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
       const unsigned span = rb.hi > rb.lo ? rb.hi - rb.lo : 0;
       const int off = k0 + 4 * half - rb.lo;
 #pragma unroll
-      for (int t = 0; t < KT / 32; ++t)
+      for (int t = 0; t < kKeyTile / 32; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[t][i] = (unsigned)(off + 32 * t + 8 * (i / 4) + i % 4) < span ? s[t][i] : hidden;
     }
     if constexpr (!BOUNDED) {
-      float top = hidden;
+      float tops[kKeyTile / 32];
 #pragma unroll
-      for (int t = 0; t < KT / 32; ++t)
+      for (int t = 0; t < kKeyTile / 32; ++t) {
+        tops[t] = hidden;
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) top = kFalls ? min3(top, s[t][i], s[t][i + 1]) : max3(top, s[t][i], s[t][i + 1]);
-      top = max_halves(__builtin_fmaf(top, f.mul, f.add));
+        for (int i = 0; i < 16; i += 2) tops[t] = kFalls ? min3(tops[t], s[t][i], s[t][i + 1]) : max3(tops[t], s[t][i], s[t][i + 1]);
+        tops[t] = __builtin_fmaf(tops[t], f.mul, f.add + row_part[t]);
+      }
+      const float top = max_halves(fmaxf(tops[0], tops[1]));
       if (__any(top > m + kLazyMax)) {
         const float now = fmaxf(m, top);
         const float by = m == now ? 1.0f : fast_exp2(m - now);
@@ -250,10 +273,10 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
     const float base = f.add - (m == -INFINITY ? 0.0f : m);
     float sum = 0.0f;
 #pragma unroll
-    for (int t = 0; t < KT / 32; ++t) {
+    for (int t = 0; t < kKeyTile / 32; ++t) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[t][i] = fast_exp2(__builtin_fmaf(s[t][i], f.mul, base));
+        s[t][i] = fast_exp2(__builtin_fmaf(s[t][i], f.mul, base + row_part[t]));
         sum += s[t][i];
       }
       vec8<T> p[2];
@@ -269,19 +292,19 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
     load_tiles(load_k, ks.base, kt, load_v, vs.base, vt, k0, lo, hi, a.bytes);
   };
 
-  int c = next_tile(flags, begin + share.first, end, kFlagShift);
-  if (c < end) load(k_even, v_even, c * KT);
+  int c = next_tile(flags, begin + share.first, end);
+  if (c < end) load(k_even, v_even, c * kKeyTile);
   while (c < end) {
-    int next = next_tile(flags, c + 1, end, kFlagShift);
+    int next = next_tile(flags, c + 1, end);
     tiles_ready();                                  // the tile is there, and nobody reads the other one any more
-    if (next < end) load(k_odd, v_odd, next * KT);
-    compute(k_even, v_even, c * KT);
+    if (next < end) load(k_odd, v_odd, next * kKeyTile);
+    compute(k_even, v_even, c * kKeyTile);
     c = next;
     if (c >= end) break;
-    next = next_tile(flags, c + 1, end, kFlagShift);
+    next = next_tile(flags, c + 1, end);
     tiles_ready();
-    if (next < end) load(k_even, v_even, next * KT);
-    compute(k_odd, v_odd, c * KT);
+    if (next < end) load(k_even, v_even, next * kKeyTile);
+    compute(k_odd, v_odd, c * kKeyTile);
     c = next;
   }
 
