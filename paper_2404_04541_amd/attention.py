@@ -88,6 +88,11 @@ def _tensor(t: torch.Tensor, name: str, tokens: Optional[int] = None, like: Opti
     return TensorStruct(t.data_ptr() or None, strides[0] if shape[0] > 1 else 0, strides[1] if shape[1] > 1 else 0)
 
 
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """A contiguous tensor of its shape (in a third of the time that naming shape, type and device takes)."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _result(t: torch.Tensor) -> TensorStruct:
     """A fresh contiguous tensor of this module's own."""
     strides = t.stride()
@@ -140,8 +145,11 @@ def symbolic(handle: sg.Handle, q_len: int, k_len: int, q_ptr: Optional[torch.Te
                             _array(colidx, "pattern colidx", torch.int32), None, 0)
         m.tiles = C.pointer(held)
     nbytes = lib.spattn_plan_bytes(C.byref(m))
-    with torch.cuda.stream(handle.stream) if handle.stream is not None else sg._nullctx():
-        memory = torch.empty(max(nbytes, 1), dtype=torch.uint8, device="cuda")
+    if handle.stream is None and q_ptr is not None:
+        memory = q_ptr.new_empty(max(nbytes, 1), dtype=torch.uint8)
+    else:
+        with torch.cuda.stream(handle.stream) if handle.stream is not None else sg._nullctx():
+            memory = torch.empty(max(nbytes, 1), dtype=torch.uint8, device="cuda")
     checked = C.c_int32(0)
     handle._check(lib.spattn_symbolic(handle.ptr, C.byref(m), memory.data_ptr(), nbytes, C.byref(checked) if check else None))
     m.q_ptr = m.k_ptr = None          # (what follows needs the sizes only)
@@ -161,8 +169,8 @@ def forward(handle: sg.Handle, plan: Plan, q, k, v, scale: Optional[float] = Non
     """-> (o [q_len, heads, head_dim], lse float32 [heads, q_len]).  scale: 1 / sqrt(head_dim) unless given."""
     lib = _lib()
     a = _args(plan, q, k, v, scale, cap, slopes)
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty((q.shape[1], plan.q_len), dtype=torch.float32, device=q.device)
+    o = _like(q)
+    lse = q.new_empty((q.shape[1], plan.q_len), dtype=torch.float32)
     handle._check(lib.spattn_forward(handle.ptr, C.byref(a), _result(o), lse.data_ptr() or None))
     return o, lse
 
@@ -173,7 +181,7 @@ def backward(handle: sg.Handle, plan: Plan, q, k, v, o, lse, d_o, scale: Optiona
     a = _args(plan, q, k, v, scale, cap, slopes)
     if o.shape != q.shape or d_o.shape != q.shape:
         raise ValueError("o and d_o have q's shape")
-    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    dq, dk, dv = _like(q), _like(k), _like(v)
     handle._check(lib.spattn_backward(handle.ptr, C.byref(a), _tensor(o, "o", plan.q_len, q), _array(lse, "lse", torch.float32, q.shape[1] * plan.q_len),
                                       _tensor(d_o, "d_o", plan.q_len, q), _result(dq), _result(dk), _result(dv)))
     return dq, dk, dv
@@ -259,7 +267,7 @@ def attend(handle: sg.Handle, cache: PagedCache, layer: int, table: PageTable, l
         raise ValueError("q: tokens of all sequences at one stride and a contiguous last dimension are wanted")
     if not q.is_cuda:
         raise ValueError("q: not on a GPU")
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    o = _like(q)
     rows = TensorStruct(q.data_ptr() or None, (per_sequence if q_len == 1 else per_token) if n * q_len > 1 else 0, per_head if heads > 1 else 0)
     handle._check(lib.spcache_attend(handle.ptr, C.byref(cache._struct), int(layer), C.byref(table.struct(cache)), _array(lens, "lens", torch.int32, n), q_len, heads,
                                      _dtype(q), 1.0 / math.sqrt(d) if scale is None else float(scale), float(cap), _slopes(slopes, heads), int(window),
@@ -277,9 +285,9 @@ def fork(handle: sg.Handle, cache: PagedCache, table: PageTable, lens: torch.Ten
     n = parent.numel()
     if entries is None:
         entries = int(((new_lens.clamp(min=0).to(torch.int64) + PAGE - 1) // PAGE).sum())
-    rowptr = torch.empty(n + 1, dtype=torch.int64, device=parent.device)
-    pages = torch.empty(int(entries), dtype=torch.int32, device=parent.device)
-    refs = torch.empty(cache.pages, dtype=torch.int32, device=parent.device)
+    rowptr = parent.new_empty(n + 1, dtype=torch.int64)
+    pages = parent.new_empty(int(entries), dtype=torch.int32)
+    refs = parent.new_empty(cache.pages, dtype=torch.int32)
     nnz = C.c_int64(0)
     handle._check(lib.spcache_fork(handle.ptr, C.byref(cache._struct), C.byref(table.struct(cache)), _array(lens, "lens", torch.int32, table.rows), n,
                                    _array(parent, "parent", torch.int32), _array(new_lens, "new_lens", torch.int32, n), rowptr.data_ptr(),

@@ -1,5 +1,5 @@
 // The structure of a mask: bounds of its rows, of groups of rows and of columns, and a pattern's flags.  Bandwidth does not matter here (28 bytes a row);
-// what a plan costs is its launches: two without a pattern, three with one.
+// what a plan costs is its launches: two, or one where the mask is small, and one more with a pattern.
 #pragma once
 #include "attn_common.hpp"
 
@@ -46,12 +46,8 @@ __device__ inline RowBound row_bound(const MaskView& m, int i) {
   return {lo, hi, diag, 0};
 }
 
-// One thread a row, groups from their lanes; the first workgroup checks the documents too.  The flags of a pattern are cleared here.
-__global__ void __launch_bounds__(256) k_plan_rows(MaskView m, PlanView p) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  const int64_t words = (int64_t)ceil_div_d(m.q_len, kPatTile) * p.seen_words, by_words = (int64_t)ceil_div_d(m.k_len, kPatTile) * p.seen_by_words;
-  for (int64_t w = i; w < words; w += (int64_t)gridDim.x * 256) p.seen[w] = 0;
-  for (int64_t w = i; w < by_words; w += (int64_t)gridDim.x * 256) p.seen_by[w] = 0;
+// Row i of the mask by a thread, its group from the lanes of a half wave.
+__device__ __forceinline__ void plan_row(const MaskView& m, const PlanView& p, int i) {
   RowBound r{0, 0, 0, 0};
   if (i < m.q_len) {
     r = row_bound(m, i);
@@ -64,27 +60,65 @@ __global__ void __launch_bounds__(256) k_plan_rows(MaskView m, PlanView p) {
     g.all_lo = max(g.all_lo, __shfl_xor(g.all_lo, d)); g.all_hi = min(g.all_hi, __shfl_xor(g.all_hi, d));
   }
   if (i % kRowGroup == 0 && i < m.q_len) p.groups[i / kRowGroup] = {g.hi ? g.lo : 0, g.hi, g.all_lo, g.all_hi};
-  if (blockIdx.x == 0) {
-    __shared__ int bad;
-    if (threadIdx.x == 0) bad = 0;
-    __syncthreads();
-    if (m.q_ptr) {
-      for (int d = threadIdx.x; d < m.docs; d += 256) {
-        const int64_t a = m.q_ptr[d], b = m.q_ptr[d + 1], c = m.k_ptr[d], e = m.k_ptr[d + 1];
-        if (a < 0 || b < a || b > m.q_len || c < 0 || e < c || e > m.k_len) bad = 1;
-        if (m.prefix && m.prefix[d] < 0) bad = 1;
-      }
-    } else if (m.prefix && threadIdx.x == 0 && m.prefix[0] < 0) {
-      bad = 1;
+}
+
+// The flags of a pattern, before k_plan_pattern sets them.
+__device__ __forceinline__ void clear_flags(const MaskView& m, const PlanView& p, int first, int64_t step) {
+  const int64_t words = (int64_t)ceil_div_d(m.q_len, kPatTile) * p.seen_words, by_words = (int64_t)ceil_div_d(m.k_len, kPatTile) * p.seen_by_words;
+  for (int64_t w = first; w < words; w += step) p.seen[w] = 0;
+  for (int64_t w = first; w < by_words; w += step) p.seen_by[w] = 0;
+}
+
+// By one workgroup.
+__device__ __forceinline__ void check_documents(const MaskView& m, const PlanView& p) {
+  __shared__ int bad;
+  if (threadIdx.x == 0) bad = 0;
+  __syncthreads();
+  if (m.q_ptr) {
+    for (int d = threadIdx.x; d < m.docs; d += blockDim.x) {
+      const int64_t a = m.q_ptr[d], b = m.q_ptr[d + 1], c = m.k_ptr[d], e = m.k_ptr[d + 1];
+      if (a < 0 || b < a || b > m.q_len || c < 0 || e < c || e > m.k_len) bad = 1;
+      if (m.prefix && m.prefix[d] < 0) bad = 1;
     }
-    __syncthreads();
+  } else if (m.prefix && threadIdx.x == 0 && m.prefix[0] < 0) {
+    bad = 1;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) *p.error = bad;
+}
+
+__global__ void __launch_bounds__(256) k_plan_rows(MaskView m, PlanView p) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  clear_flags(m, p, i, (int64_t)gridDim.x * 256);
+  plan_row(m, p, i);
+  if (blockIdx.x == 0) {
+    check_documents(m, p);
     if (threadIdx.x == 0) {
-      *p.error = bad;
       *p.done = 0;
       p.totals[0] = p.totals[1] = 0;
     }
   }
 }
+
+// The keys that the rows of tile i see: from .x to before .y; nothing is 0, 0.
+__device__ __forceinline__ int2 query_tile_reach(const PlanView& p, int q_len, int i) {
+  int lo = 0x7fffffff, hi = 0;
+  for (int g = i * (kPatTile / kRowGroup); g < (i + 1) * (kPatTile / kRowGroup) && g < ceil_div_d(q_len, kRowGroup); ++g) {
+    const GroupBound b = p.groups[g];
+    if (b.hi > b.lo) { lo = min(lo, b.lo); hi = max(hi, b.hi); }
+  }
+  return hi > lo ? make_int2(lo, hi) : make_int2(0, 0);
+}
+
+// The queries that can see any key of tile c, by a wave: from the first row that ends behind its first key to before the first that begins behind its last.
+__device__ __forceinline__ int2 key_tile_reach(const PlanView& p, int q_len, int k_len, int c) {
+  const int first = c * kKeyTile, last = k_len - first > kKeyTile ? first + kKeyTile : k_len;
+  const int from = wave_count_below(q_len, (int64_t)first + 1, [&](int i) { return p.rows[i].hi; });
+  const int to = wave_count_below(q_len, last, [&](int i) { return p.rows[i].lo; });
+  return to > from ? make_int2(from, to) : make_int2(0, 0);
+}
+__device__ __forceinline__ unsigned query_tiles(int2 r) { return ceil_div_d(r.y, kQueryTile) - r.x / kQueryTile; }
+__device__ __forceinline__ unsigned key_tiles(int2 r) { return ceil_div_d(r.y, kKeyTile) - r.x / kKeyTile; }
 
 // Numbers 0 .. n - 1 by falling work(i), as far as 256 steps of the largest tell it, by one workgroup of 256 threads: store(place, i).  (Which of two alike comes first
 // may differ from call to call; it decides only when their workgroups run.)
@@ -117,26 +151,18 @@ __device__ __forceinline__ void order_by_work(int n, F work, S store) {
   for (int i = threadIdx.x; i < n; i += 256) store((int)atomicAdd(&count[bucket(i)], 1u), i);
 }
 
-// The queries that can see any key of a tile, a wave a tile: from the first row that ends behind its first key to before the first that begins
-// behind its last.  And both kinds of tiles in order, the tiles of queries by a workgroup of its own, those of keys by the last one to
-// finish: the card holds a few workgroups a compute unit, and long rows that begin late are waited for (two documents of 4000 tokens, tiles
+// Both kinds of tiles and what they reach, in order of work, the tiles of queries by a workgroup of its own, those of keys a wave a tile, ordered by the last
+// workgroup to finish: the card holds a few workgroups a compute unit, and long rows that begin late are waited for (two documents of 4000 tokens, tiles
 // from the last row backwards: 1.3 waves a SIMD on average where two fit).  Few tiles all run at once and need no order.
 constexpr int kOrderQueries = 17, kOrderKeys = 48;   // (tiles of keys are ordered at the end, which costs 5 us)
 __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanView p) {
   const int q_tiles = ceil_div_d(q_len, kPatTile), k_tiles = ceil_div_d(k_len, kKeyTile);
   if (blockIdx.x == gridDim.x - 1) {
-    auto reach = [&](int i) {
-      int lo = 0x7fffffff, hi = 0;
-      for (int g = i * (kPatTile / kRowGroup); g < (i + 1) * (kPatTile / kRowGroup) && g < ceil_div_d(q_len, kRowGroup); ++g) {
-        const GroupBound b = p.groups[g];
-        if (b.hi > b.lo) { lo = min(lo, b.lo); hi = max(hi, b.hi); }
-      }
-      return hi > lo ? make_int2(lo, hi) : make_int2(0, 0);
-    };
+    auto reach = [&](int i) { return query_tile_reach(p, q_len, i); };
     unsigned long long sum = 0;
     for (int i = threadIdx.x; i < q_tiles; i += 256) {
       const int2 r = reach(i);
-      sum += ceil_div_d(r.y, kKeyTile) - r.x / kKeyTile;
+      sum += key_tiles(r);
       if (q_tiles < kOrderQueries) p.q_order[q_tiles - 1 - i] = make_int4(i, r.x, r.y, 0);
     }
     if (sum) atomicAdd(&p.totals[0], sum);
@@ -148,13 +174,11 @@ __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanVie
   }
   const int c = blockIdx.x * 4 + threadIdx.x / kWave;
   if (c < k_tiles) {
-    const int first = c * kKeyTile, last = k_len - first > kKeyTile ? first + kKeyTile : k_len;
-    const int from = wave_count_below(q_len, (int64_t)first + 1, [&](int i) { return p.rows[i].hi; });
-    const int to = wave_count_below(q_len, last, [&](int i) { return p.rows[i].lo; });
+    const int2 r = key_tile_reach(p, q_len, k_len, c);
     if (lane_id() == 0) {
-      p.cols[c] = make_int2(from, to);
-      if (to > from) atomicAdd(&p.totals[1], (unsigned long long)(ceil_div_d(to, kQueryTile) - from / kQueryTile));
-      if (k_tiles < kOrderKeys) p.k_order[c] = to > from ? make_int4(c, from, to, 0) : make_int4(c, 0, 0, 0);
+      p.cols[c] = r;
+      atomicAdd(&p.totals[1], (unsigned long long)query_tiles(r));
+      if (k_tiles < kOrderKeys) p.k_order[c] = make_int4(c, r.x, r.y, 0);
     }
   }
   if (k_tiles < kOrderKeys) return;
@@ -165,10 +189,38 @@ __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanVie
   __syncthreads();
   if (!final) return;
   __threadfence();
-  auto span = [&](int i) { const int2 c = p.cols[i]; return c.y > c.x ? c : make_int2(0, 0); };
   order_by_work(
-      k_tiles, [&](int i) { const int2 c = span(i); return c.y - c.x; },
-      [&](int place, int i) { const int2 c = span(i); p.k_order[place] = make_int4(i, c.x, c.y, 0); });
+      k_tiles, [&](int i) { const int2 c = p.cols[i]; return c.y - c.x; },
+      [&](int place, int i) { const int2 c = p.cols[i]; p.k_order[place] = make_int4(i, c.x, c.y, 0); });
+}
+
+// The same for a small mask, whose tiles need no order, by one workgroup: a thread a row, a wave a tile of keys.  us in one launch | in two: 257 tokens 4.6 | 5.0,
+// and 4 less on the host; 2003 tokens by the same kernel 8.5 | 7.5.
+constexpr int kSmallMask = 1024;
+static_assert(kSmallMask / kPatTile < kOrderQueries && kSmallMask / kKeyTile < kOrderKeys && kSmallMask / kKeyTile <= kSmallMask / kWave, "no order, a wave a tile");
+__global__ void __launch_bounds__(kSmallMask) k_plan_small(MaskView m, PlanView p) {
+  __shared__ unsigned totals[2];
+  if (threadIdx.x < 2) totals[threadIdx.x] = 0;
+  clear_flags(m, p, threadIdx.x, kSmallMask);
+  plan_row(m, p, threadIdx.x);
+  check_documents(m, p);
+  __syncthreads();
+  const int q_tiles = ceil_div_d(m.q_len, kPatTile), k_tiles = ceil_div_d(m.k_len, kKeyTile);
+  const int i = threadIdx.x, c = threadIdx.x / kWave;
+  if (i < q_tiles) {
+    const int2 r = query_tile_reach(p, m.q_len, i);
+    atomicAdd(&totals[0], key_tiles(r));
+    p.q_order[q_tiles - 1 - i] = make_int4(i, r.x, r.y, 0);
+  }
+  if (c < k_tiles) {
+    const int2 r = key_tile_reach(p, m.q_len, m.k_len, c);
+    if (lane_id() == 0) {
+      atomicAdd(&totals[1], query_tiles(r));
+      p.k_order[c] = make_int4(c, r.x, r.y, 0);
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < 2) p.totals[threadIdx.x] = totals[threadIdx.x];
 }
 
 // The pattern's flags, a wave a row of tiles.  Bits are only set, so neither the order of a row's columns nor repeated ones matter.
