@@ -102,13 +102,13 @@ def test_long_rows(h):
     run(h, q, k, v, d_o, {"causal": False, "tiles": ([0, 4, 7], [0, 5, 6, 22, 3, 4, 21])})
 
 
-@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("tq, tk", [(1024, 1024), (1025, 1024), (1024, 1025), (1, 1025), (1030, 1)])
 def test_around_a_small_plan(h, tq, tk):
     """Masks of at most 1024 queries and keys are planned by one workgroup."""
     run(h, *tensors(41, BF, tq, tk, 2, 1, 64), {"q_ptr": [0, tq // 3, tq], "k_ptr": [0, tk // 2, tk], "window": 500})
 
 
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("cap, bias", [(0.0, False), (20.0, False), (100.0, False), (20.0, True), (0.0, True)])
 def test_rows_in_pieces(h, d, cap, bias):
     """Few workgroups and long rows (and columns, and heads that share them): their work is cut into pieces and joined."""
