@@ -150,7 +150,7 @@ int check_args(spgemm_context* h, const spattn_args* a) {
   if ((rc = check_tensor(h, a->q, a->mask->q_len, "q"))) return rc;
   if ((rc = check_tensor(h, a->k, a->mask->k_len, "k"))) return rc;
   if ((rc = check_tensor(h, a->v, a->mask->k_len, "v"))) return rc;
-  if (ceil_div(a->mask->q_len, kPatTile) * a->heads > 0x7fffffffLL || ceil_div(a->mask->k_len, kKeyTile) * a->kv_heads > 0x7fffffffLL)
+  if (ceil_div(a->mask->q_len, kPatTile) * a->heads + ceil_div(a->mask->k_len, kKeyTile) * a->kv_heads > 0xffffff)   // (2^32 threads are a launch's limit)
     return fail(h, SPGEMM_UNSUPPORTED, "too many tiles");
   return SPGEMM_OK;
 }
@@ -170,9 +170,9 @@ AttnArgs attn_args(const spattn_args* a, const spattn_tensor& o, const float* ls
 
 // How a pass over `blocks` workgroups, each with at most `tiles` tiles, may be shared: the card holds `resident` of them a compute unit; where the
 // workgroups fill it nothing is shared, nor where the longest is short, else there are places for pieces until it is filled twice.
-int split_pieces(spgemm_context* h, int64_t blocks, int64_t tiles, int resident) {
+int split_pieces(spgemm_context* h, int64_t blocks, int64_t all, int64_t tiles, int resident) {
   const int64_t slots = (int64_t)h->num_cus * resident;
-  if (blocks == 0 || blocks >= slots || tiles <= 2 * kLeastTiles) return 1;
+  if (blocks == 0 || all >= 2 * slots || tiles <= 2 * kLeastTiles) return 1;
   const int64_t most = ceil_div(2 * slots, blocks) + 1;
   return (int)(most < 64 ? most : 64);
 }
@@ -334,7 +334,7 @@ int spattn_forward(spgemm_handle h, const spattn_args* a, spattn_tensor o, float
     AttnArgs g = attn_args(a, o, lse);
     const int64_t blocks = (int64_t)g.q_tiles * g.heads;
     const int room = a->head_dim <= 64 ? 64 : 128, resident = room == 64 ? 4 : 2;
-    const int most = split_pieces(h, blocks, ceil_div(a->mask->k_len, kKeyTile), resident);
+    const int most = split_pieces(h, blocks, 2 * blocks, ceil_div(a->mask->k_len, kKeyTile), resident);
     void* mem = nullptr;
     if (most > 1 && (rc = scratch(h, split_bytes(blocks, most, room), &mem))) return rc;
     g.split = split_of(h, blocks, most, resident, room, mem);
@@ -372,25 +372,23 @@ int spattn_backward(spgemm_handle h, const spattn_args* a, spattn_tensor o, cons
     const int64_t q_blocks = ceil_div(q_len, kPatTile) * a->heads, k_blocks = ceil_div(k_len, kKeyTile) * a->kv_heads;
     const int room = a->head_dim <= 64 ? 64 : 128, resident = room == 64 ? 3 : 2;
     const int64_t g_heads = a->heads / a->kv_heads;
-    const int q_most = split_pieces(h, q_blocks, ceil_div(k_len, kKeyTile), resident), k_most = split_pieces(h, k_blocks, ceil_div(q_len, kQueryTile) * g_heads, resident);
+    const int64_t both = q_blocks + k_blocks;
+    const int q_most = split_pieces(h, q_blocks, both, ceil_div(k_len, kKeyTile), resident);
+    const int k_most = split_pieces(h, k_blocks, both, ceil_div(q_len, kQueryTile) * g_heads, resident);
     const size_t q_part = split_bytes(q_blocks, q_most, room), k_part = split_bytes(k_blocks, k_most, room);
     void* mem = nullptr;
-    if ((rc = scratch(h, facts + (q_part > k_part ? q_part : k_part), &mem))) return rc;
-    unsigned char* part = static_cast<unsigned char*>(mem) + facts;      // (one kernel's pieces are joined before the next one's come)
+    if ((rc = scratch(h, facts + q_part + k_part, &mem))) return rc;
+    unsigned char* part = static_cast<unsigned char*>(mem) + facts;
     AttnArgs g = attn_args(a, o, lse);
-    AttnGrads r{view(d_o), view(dq), view(dk), view(dv), static_cast<RowFacts*>(mem)};
+    AttnGrads r{view(d_o), view(dq), view(dk), view(dv), static_cast<RowFacts*>(mem), (int)q_blocks, (int)k_blocks,
+                split_of(h, k_blocks, k_most, resident, room, part + q_part)};
+    g.split = split_of(h, q_blocks, q_most, resident, room, part);
+    if (both == 0) return SPGEMM_OK;
     auto launch = [&](auto type, auto dim, auto cap, auto bias) {
       using T = decltype(type);
-      if (q_blocks) {
-        g.split = split_of(h, q_blocks, q_most, resident, room, part);
-        k_attn_dq<T, dim(), cap(), bias()><<<dim3((unsigned)q_blocks, (unsigned)q_most), dim3(256), 0, h->stream>>>(g, r);
-        if (q_most > 1) k_attn_dq_join<T, dim(), cap()><<<dim3((unsigned)q_blocks, dim() / 32), dim3(256), 0, h->stream>>>(g, r);
-      }
-      if (k_blocks) {
-        g.split = split_of(h, k_blocks, k_most, resident, room, part);
-        k_attn_dkv<T, dim(), cap(), bias()><<<dim3((unsigned)k_blocks, (unsigned)k_most), dim3(256), 0, h->stream>>>(g, r);
-        if (k_most > 1) k_attn_dkv_join<T, dim(), cap()><<<dim3((unsigned)k_blocks, dim() / 32), dim3(256), 0, h->stream>>>(g, r);
-      }
+      if (q_len) k_attn_facts<T, dim()><<<dim3((unsigned)g.q_tiles * (kPatTile / kQueryTile), (unsigned)a->heads), dim3(256), 0, h->stream>>>(g, r);
+      k_attn_back<T, dim(), cap(), bias()><<<dim3((unsigned)(q_blocks * q_most + k_blocks * k_most)), dim3(256), 0, h->stream>>>(g, r);
+      if (q_most > 1 || k_most > 1) k_attn_back_join<T, dim(), cap()><<<dim3((unsigned)both, dim() / 32), dim3(256), 0, h->stream>>>(g, r);
     };
     dispatch(a->dtype, a->head_dim, a->cap > 0, a->slopes != nullptr, launch);
     return launched(h);

@@ -2,57 +2,81 @@
 //
 // With P = 2^(x - lse2) (x: the shaped scores in units of log 2, lse2 the row's logarithm from the forward pass), dP = dO V^T and
 // delta_i = sum_d dO_id O_id:  dV = P^T dO,  dS = P (dP - delta) (1 - tanh^2),  dQ = scale dS K,  dK = scale dS^T Q.
-// Two kernels, each with a fixed order of its sums (no atomics: the same inputs give the same bits): k_attn_dq goes over the keys of 128
-// queries as the forward kernel does and leaves -delta and what exponents begin with for k_attn_dkv, which goes over the queries, of all heads that share
-// them, of 64 keys.  That computes S and dP twice, seven products where five would do with atomics on dQ in 32 bits.
+// k_attn_facts sums up what the rows' exponents begin with and -delta; after it workgroups of two kinds run in one launch, each with a fixed order of its
+// sums (no atomics: the same inputs give the same bits): for dQ they go over the keys of 128 queries as the forward kernel does, for dK and dV over
+// the queries, of all heads that share them, of 64 keys.  That computes S and dP twice, seven products where five would do with atomics on dQ in 32 bits.
 // P, dS are rounded to 16 bits once, as operands; all sums are held in 32 bits.
 #pragma once
 #include "attn_forward.hpp"
 
 namespace spg {
 
+// Tiles that all workgroups go over together, of one head.
+__device__ __forceinline__ unsigned long long all_work(const AttnArgs& a) { return load_uniform(a.plan.totals) + load_uniform(a.plan.totals + 1); }
+
+// A workgroup has 64 rows of a head: D / 8 lanes a row, 16 bytes of O and dO each.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) k_attn_facts(AttnArgs a, AttnGrads g) {
+  constexpr int kLanes = D / 8, kStep = 256 / kLanes;
+  const int n = blockIdx.x, head = blockIdx.y, chunk = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
+  const HeadTensor &o = a.o, &d_o = g.d_o;
+  __shared__ float deltas[kQueryTile];
+  u32x4 x[kQueryTile / kStep], y[kQueryTile / kStep];
+#pragma unroll
+  for (int i = 0; i < kQueryTile / kStep; ++i) {
+    const int64_t row = (int64_t)n * kQueryTile + i * kStep + mine;
+    x[i] = y[i] = u32x4{0, 0, 0, 0};
+    if (row < a.q_len && chunk * 16 < a.bytes) {
+      x[i] = *reinterpret_cast<const u32x4*>(o.of(head).base + row * o.stride + chunk * 16);
+      y[i] = *reinterpret_cast<const u32x4*>(d_o.of(head).base + row * d_o.stride + chunk * 16);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kQueryTile / kStep; ++i) {
+    const vec8<T> u = __builtin_bit_cast(vec8<T>, x[i]), v = __builtin_bit_cast(vec8<T>, y[i]);
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum = __builtin_fmaf((float)u[j], (float)v[j], sum);
+#pragma unroll
+    for (int d = 1; d < kLanes; d *= 2) sum += __shfl_xor(sum, d);
+    if (chunk == 0) deltas[i * kStep + mine] = sum;
+  }
+  __syncthreads();
+  if (threadIdx.x >= kQueryTile) return;
+  const int i = threadIdx.x, row = n * kQueryTile + i;
+  const bool real = row < a.q_len;
+  const RowBound rb = real ? a.plan.rows[row] : RowBound{0, 0, 0, 0};
+  const float lse = real ? a.lse[(int64_t)head * a.q_len + row] : -INFINITY;
+  RowFacts& facts = g.facts[(int64_t)head * a.q_tiles * (kPatTile / kQueryTile) + n];
+  facts.base[i] = lse == -INFINITY ? -INFINITY : (a.score.cap > 0.0f && !a.score.slopes ? a.score.cap * kLog2e : 0.0f) - lse * kLog2e;   // (a row that sees nothing: every power is 0)
+  facts.less[i] = -deltas[i];
+  facts.lo[i] = rb.lo;
+  facts.hi[i] = rb.hi;
+  facts.diag[i] = rb.diag;
+}
+
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
+__device__ __forceinline__ void dq_tile(const AttnArgs& a, const AttnGrads& g, unsigned char* lds, int n, int piece) {
   using S = TileShape<D>;
-  __shared__ __align__(16) unsigned char k_even[kKeyTile * D * 2], v_even[kKeyTile * D * 2], k_odd[kKeyTile * D * 2], v_odd[kKeyTile * D * 2];
-  const Place at = place_of(blockIdx.x, a.heads, a.plan.q_order);
+  constexpr int kTile = kKeyTile * D * 2;
+  unsigned char *k_even = lds, *v_even = lds + kTile, *k_odd = lds + 2 * kTile, *v_odd = lds + 3 * kTile;
+  const Place at = place_of(n, a.heads, a.plan.q_order);
   const int head = at.head, qt = at.tile, lo = at.lo, hi = at.hi;
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
   const int row = qt * kPatTile + wave * kRowGroup + (lane & 31);
   const GroupBound mine = wave_bound(a, qt, wave);
   const int begin = lo / kKeyTile;
-  const Share share = share_of(a.split, ceil_div_d(hi, kKeyTile) - begin, a.split.most > 1 ? load_uniform(a.plan.totals) : 0, a.heads, kLeastTiles, blockIdx.y);
-  if ((int)blockIdx.y >= share.pieces) return;
+  const Share share = share_of(a.split, ceil_div_d(hi, kKeyTile) - begin, a.split.most > 1 ? all_work(a) : 0, a.heads, kLeastTiles, piece);
+  if (piece >= share.pieces) return;
   const ScoreFactors f = score_factors<CAP, BIAS>(a.score, head);
   const bool real = row < a.q_len;
   const RowBound rb = real ? a.plan.rows[row] : RowBound{0, 0, 0, 0};
+  const RowFacts& facts = g.facts[((int64_t)head * a.q_tiles + qt) * (kPatTile / kQueryTile) + wave / 2];
+  const float base = facts.base[row % kQueryTile], less = facts.less[row % kQueryTile];
   vec8<T> q[D / 16], d_o[D / 16];
-  load_row<T, D>(g.d_o.of(head), row, real, a.bytes, half, d_o);
-  float delta = 0.0f, lse2 = INFINITY;   // (a row that sees nothing: every power is 0)
-  {
-    load_row<T, D>(a.o.of(head), row, real, a.bytes, half, q);   // (O for the moment)
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)d_o[i][j], (float)q[i][j], delta);
-    delta = add_halves(delta);
-  }
-  if (real) {
-    const float v = a.lse[(int64_t)head * a.q_len + row];
-    lse2 = v == -INFINITY ? INFINITY : v * kLog2e;
-  }
-  if (half == 0 && blockIdx.y == 0) {
-    RowFacts& facts = g.facts[((int64_t)head * a.q_tiles + qt) * (kPatTile / kQueryTile) + wave / 2];
-    const int i = row % kQueryTile;
-    facts.base[i] = f.add - lse2;
-    facts.less[i] = -delta;
-    facts.lo[i] = rb.lo;
-    facts.hi[i] = rb.hi;
-    facts.diag[i] = rb.diag;
-  }
-  const float base = f.add - lse2;
   load_row<T, D>(a.q.of(head), row, real, a.bytes, half, q);
+  load_row<T, D>(g.d_o.of(head), row, real, a.bytes, half, d_o);
   const int kv = uniform(head / a.group);
   const RowSource ks = a.k.of(kv), vs = a.v.of(kv);
   const TileLoader<D, kKeyTile, 256> load_k(ks.stride, lane), load_v(vs.stride, lane);
@@ -81,7 +105,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
       for (int i = 0; i < 16; ++i) {
         float back;
         const float x = shaped<CAP, BIAS>(s[i], f, f.slope2 * fabsf(away - (float)(8 * (i / 4) + i % 4)), &back);
-        s[i] = fast_exp2(__builtin_fmaf(x, f.mul, base)) * (dp[i] - delta);
+        s[i] = fast_exp2(__builtin_fmaf(x, f.mul, base)) * (dp[i] + less);
         if constexpr (CAP) s[i] *= back;
       }
       if (!whole) {
@@ -116,21 +140,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnArgs a, AttnGrads g) {
     c = next;
   }
 
-  if (share.pieces > 1) leave_sums<D>(a.split, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, acc);
+  if (share.pieces > 1) leave_sums<D>(a.split, (int64_t)piece * g.q_blocks + n, acc);
   else if (real) store_rows<T, D>(g.dq, head, row, half, 0, a.bytes, acc, CAP ? 4.0f * a.score.scale : a.score.scale);
-}
-
-template <typename T, int D, bool CAP>
-__global__ void __launch_bounds__(256) k_attn_dq_join(AttnArgs a, AttnGrads g) {
-  const Place at = place_of(blockIdx.x, a.heads, a.plan.q_order);
-  const Share share = share_of(a.split, ceil_div_d(at.hi, kKeyTile) - at.lo / kKeyTile, load_uniform(a.plan.totals), a.heads, kLeastTiles, 0);
-  if (share.pieces == 1) return;
-  const int lane = lane_id(), row = at.tile * kPatTile + threadIdx.x / kWave * kRowGroup + (lane & 31);
-  const int c0 = blockIdx.y * 32;
-  f32x16 acc = {};
-#pragma unroll 4
-  for (int p = 0; p < share.pieces; ++p) add_sums<D>(a.split, (int64_t)p * gridDim.x + blockIdx.x, c0, 1.0f, acc);
-  if (row < a.q_len) store_rows<T, 32>(g.dq, at.head, row, lane >> 5, c0, a.bytes, &acc, CAP ? 4.0f * a.score.scale : a.score.scale);
 }
 
 // A workgroup has 64 keys of a key head and goes over their queries in tiles of 64 rows, head by head.  Wave w has keys 32 (w % 2) .. and of every
@@ -143,10 +154,10 @@ struct QueryTile {
 };
 
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
+__device__ __forceinline__ void dkv_tile(const AttnArgs& a, const AttnGrads& g, unsigned char* lds, int n, int piece) {
   using S = TileShape<D>;
-  __shared__ __align__(16) QueryTile<D> even, odd;
-  const Place at = place_of(blockIdx.x, a.heads / a.group, a.plan.k_order);
+  QueryTile<D>&even = reinterpret_cast<QueryTile<D>*>(lds)[0], &odd = reinterpret_cast<QueryTile<D>*>(lds)[1];
+  const Place at = place_of(n, a.heads / a.group, a.plan.k_order);
   const int kv = at.head, kt = at.tile, lo = at.lo, hi = at.hi;
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave), part = wave >> 1;
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
@@ -163,8 +174,8 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
   const int low = hi > lo ? lo / kQueryTile : 0, end = hi > lo ? ceil_div_d(hi, kQueryTile) : 0, tiles = end - low;
   const int begin = next_tile(flags, low, end);
   // the work is a list: all tiles of one head, then of the next
-  const Share share = share_of(a.split, tiles * a.group, a.split.most > 1 ? load_uniform(a.plan.totals + 1) : 0, a.heads, kLeastTiles, blockIdx.y);
-  if ((int)blockIdx.y >= share.pieces) return;
+  const Share share = share_of(g.k_split, tiles * a.group, g.k_split.most > 1 ? all_work(a) : 0, a.heads, kLeastTiles, piece);
+  if (piece >= share.pieces) return;
 
   auto load = [&](QueryTile<D>& t, int head, int tile) {
     const int first = tile * kQueryTile;
@@ -301,22 +312,43 @@ __global__ void __launch_bounds__(256, 2) k_attn_dkv(AttnArgs a, AttnGrads g) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) sum[i][4 * r + j] = (part ? dv[i][4 * r + j] : dk[i][4 * r + j]) + x[j];
     }
-  if (share.pieces > 1) leave_sums<D>(a.split, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, sum);
+  if (share.pieces > 1) leave_sums<D>(g.k_split, (int64_t)piece * g.k_blocks + n, sum);
   else if (real) store_rows<T, D>(part ? g.dv : g.dk, kv, key, half, 0, a.bytes, sum, part ? 1.0f : CAP ? 4.0f * a.score.scale : a.score.scale);
 }
 
+// Keys' workgroups come first, for their chains are the longer ones.
+template <typename T, int D, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(256, 2) k_attn_back(AttnArgs a, AttnGrads g) {
+  static_assert(sizeof(QueryTile<D>) >= 2 * kKeyTile * D * 2, "both kinds fit");
+  __shared__ __align__(16) unsigned char lds[2 * sizeof(QueryTile<D>)];
+  const int n = blockIdx.x, keys = g.k_blocks * g.k_split.most;
+  if (n < keys) dkv_tile<T, D, CAP, BIAS>(a, g, lds, n % g.k_blocks, n / g.k_blocks);
+  else dq_tile<T, D, CAP, BIAS>(a, g, lds, (n - keys) % g.q_blocks, (n - keys) / g.q_blocks);
+}
+
+// A workgroup has 32 channels of a tile's rows (keys).
 template <typename T, int D, bool CAP>
-__global__ void __launch_bounds__(256) k_attn_dkv_join(AttnArgs a, AttnGrads g) {
-  const Place at = place_of(blockIdx.x, a.heads / a.group, a.plan.k_order);
-  const int tiles = at.hi > at.lo ? ceil_div_d(at.hi, kQueryTile) - at.lo / kQueryTile : 0;
-  const Share share = share_of(a.split, tiles * a.group, load_uniform(a.plan.totals + 1), a.heads, kLeastTiles, 0);
+__global__ void __launch_bounds__(256) k_attn_back_join(AttnArgs a, AttnGrads g) {
+  const int c0 = blockIdx.y * 32, lane = lane_id(), wave = uniform(threadIdx.x / kWave);
+  const float by = CAP ? 4.0f * a.score.scale : a.score.scale;
+  const bool keys = (int)blockIdx.x < g.k_blocks;
+  const int n = keys ? blockIdx.x : blockIdx.x - g.k_blocks;
+  const Split& sp = keys ? g.k_split : a.split;
+  if (sp.most == 1) return;
+  const Place at = keys ? place_of(n, a.heads / a.group, a.plan.k_order) : place_of(n, a.heads, a.plan.q_order);
+  const int tiles = keys ? (at.hi > at.lo ? ceil_div_d(at.hi, kQueryTile) - at.lo / kQueryTile : 0) * a.group : ceil_div_d(at.hi, kKeyTile) - at.lo / kKeyTile;
+  const Share share = share_of(sp, tiles, all_work(a), a.heads, kLeastTiles, 0);
   if (share.pieces == 1) return;
-  const int lane = lane_id(), wave = uniform(threadIdx.x / kWave), part = wave >> 1, key = at.tile * kKeyTile + (wave & 1) * 32 + (lane & 31);
-  const int c0 = blockIdx.y * 32;
   f32x16 sum = {};
 #pragma unroll 4
-  for (int p = 0; p < share.pieces; ++p) add_sums<D>(a.split, (int64_t)p * gridDim.x + blockIdx.x, c0, 1.0f, sum);
-  if (key < a.k_len) store_rows<T, 32>(part ? g.dv : g.dk, at.head, key, lane >> 5, c0, a.bytes, &sum, part ? 1.0f : CAP ? 4.0f * a.score.scale : a.score.scale);
+  for (int p = 0; p < share.pieces; ++p) add_sums<D>(sp, (int64_t)p * (keys ? g.k_blocks : g.q_blocks) + n, c0, 1.0f, sum);
+  if (keys) {
+    const int part = wave >> 1, key = at.tile * kKeyTile + (wave & 1) * 32 + (lane & 31);
+    if (key < a.k_len) store_rows<T, 32>(part ? g.dv : g.dk, at.head, key, lane >> 5, c0, a.bytes, &sum, part ? 1.0f : by);
+  } else {
+    const int row = at.tile * kPatTile + wave * kRowGroup + (lane & 31);
+    if (row < a.q_len) store_rows<T, 32>(g.dq, at.head, row, lane >> 5, c0, a.bytes, &sum, by);
+  }
 }
 
 }  // namespace spg

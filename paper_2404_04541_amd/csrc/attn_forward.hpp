@@ -51,7 +51,7 @@ struct AttnArgs {
   Split split;
 };
 
-// What the kernel of dK and dV needs to know of 64 rows of a head: what their exponents add to s * mul (ScoreFactors; -inf for a row that sees nothing or
+// What the gradients need to know of 64 rows of a head: what their exponents add to s * mul (ScoreFactors; -inf for a row that sees nothing or
 // does not exist), minus the sums of dO * O, and their bounds.
 struct RowFacts {
   float base[kQueryTile], less[kQueryTile];
@@ -61,6 +61,8 @@ struct RowFacts {
 struct AttnGrads {
   HeadTensor d_o, dq, dk, dv;
   RowFacts* facts;        // workspace [heads][ceil(q_len / 128) * 2]
+  int q_blocks, k_blocks; // workgroups for dQ, for dK and dV, not counting pieces
+  Split k_split;
 };
 
 // Which head and tile a workgroup has, and what the tile reaches.  Workgroups go to the eight dies in turn: heads that share keys stay on one, whose
