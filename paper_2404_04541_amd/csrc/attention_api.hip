@@ -100,13 +100,11 @@ PlanView carve_plan(const spattn_mask* m, void* mem, size_t* bytes) {
   Carve c{static_cast<unsigned char*>(mem)};
   PlanView p{};
   p.error = c.take<int>(1);
-  p.done = c.take<unsigned>(1);
   p.totals = c.take<unsigned long long>(2);
   p.rows = c.take<RowBound>(m->q_len);
   p.groups = c.take<GroupBound>(ceil_div(m->q_len, kRowGroup));
   p.cols = c.take<int2>(ceil_div(m->k_len, kKeyTile));
   p.q_order = c.take<int4>(q_tiles);
-  p.k_order = c.take<int4>(ceil_div(m->k_len, kKeyTile));
   if (m->tiles) {
     p.seen_words = (int)ceil_div(k_tiles > 0 ? k_tiles : 1, 32);
     p.seen_by_words = (int)ceil_div(q_tiles > 0 ? q_tiles : 1, 32);
@@ -368,7 +366,7 @@ int spattn_backward(spgemm_handle h, const spattn_args* a, spattn_tensor o, cons
       return rc;
     if (q_len > 0 && !lse) return fail(h, SPGEMM_INVALID_ARG, "lse is null");
     if ((rc = ensure_device(h))) return rc;
-    const size_t facts = align_up((size_t)a->heads * ceil_div(q_len, kPatTile) * (kPatTile / kQueryTile) * sizeof(RowFacts));
+    const size_t order = align_up((size_t)ceil_div(k_len, kKeyTile) * sizeof(int4)), facts = align_up((size_t)a->heads * ceil_div(q_len, kPatTile) * (kPatTile / kQueryTile) * sizeof(RowFacts));
     const int64_t q_blocks = ceil_div(q_len, kPatTile) * a->heads, k_blocks = ceil_div(k_len, kKeyTile) * a->kv_heads;
     const int room = a->head_dim <= 64 ? 64 : 128, resident = room == 64 ? 3 : 2;
     const int64_t g_heads = a->heads / a->kv_heads;
@@ -377,16 +375,16 @@ int spattn_backward(spgemm_handle h, const spattn_args* a, spattn_tensor o, cons
     const int k_most = split_pieces(h, k_blocks, both, ceil_div(q_len, kQueryTile) * g_heads, resident);
     const size_t q_part = split_bytes(q_blocks, q_most, room), k_part = split_bytes(k_blocks, k_most, room);
     void* mem = nullptr;
-    if ((rc = scratch(h, facts + q_part + k_part, &mem))) return rc;
-    unsigned char* part = static_cast<unsigned char*>(mem) + facts;
+    if ((rc = scratch(h, order + facts + q_part + k_part, &mem))) return rc;
+    unsigned char *rows = static_cast<unsigned char*>(mem) + order, *part = rows + facts;
     AttnArgs g = attn_args(a, o, lse);
-    AttnGrads r{view(d_o), view(dq), view(dk), view(dv), static_cast<RowFacts*>(mem), (int)q_blocks, (int)k_blocks,
-                split_of(h, k_blocks, k_most, resident, room, part + q_part)};
+    AttnGrads r{view(d_o), view(dq), view(dk), view(dv), reinterpret_cast<RowFacts*>(rows), (int)q_blocks, (int)k_blocks,
+                split_of(h, k_blocks, k_most, resident, room, part + q_part), static_cast<int4*>(mem)};
     g.split = split_of(h, q_blocks, q_most, resident, room, part);
     if (both == 0) return SPGEMM_OK;
     auto launch = [&](auto type, auto dim, auto cap, auto bias) {
       using T = decltype(type);
-      if (q_len) k_attn_facts<T, dim()><<<dim3((unsigned)g.q_tiles * (kPatTile / kQueryTile), (unsigned)a->heads), dim3(256), 0, h->stream>>>(g, r);
+      k_attn_facts<T, dim()><<<dim3((unsigned)g.q_tiles * (kPatTile / kQueryTile) + 1, (unsigned)a->heads), dim3(256), 0, h->stream>>>(g, r);
       k_attn_back<T, dim(), cap(), bias()><<<dim3((unsigned)(q_blocks * q_most + k_blocks * k_most)), dim3(256), 0, h->stream>>>(g, r);
       if (q_most > 1 || k_most > 1) k_attn_back_join<T, dim(), cap()><<<dim3((unsigned)both, dim() / 32), dim3(256), 0, h->stream>>>(g, r);
     };

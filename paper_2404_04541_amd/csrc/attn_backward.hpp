@@ -8,17 +8,22 @@
 // P, dS are rounded to 16 bits once, as operands; all sums are held in 32 bits.
 #pragma once
 #include "attn_forward.hpp"
+#include "attn_plan_kernels.hpp"
 
 namespace spg {
 
 // Tiles that all workgroups go over together, of one head.
 __device__ __forceinline__ unsigned long long all_work(const AttnArgs& a) { return load_uniform(a.plan.totals) + load_uniform(a.plan.totals + 1); }
 
-// A workgroup has 64 rows of a head: D / 8 lanes a row, 16 bytes of O and dO each.
+// A workgroup has 64 rows of a head: D / 8 lanes a row, 16 bytes of O and dO each.  The first one brings the tiles of keys into order meanwhile.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_attn_facts(AttnArgs a, AttnGrads g) {
   constexpr int kLanes = D / 8, kStep = 256 / kLanes;
-  const int n = blockIdx.x, head = blockIdx.y, chunk = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
+  if (blockIdx.x == 0) {
+    if (blockIdx.y == 0) order_key_tiles(a.plan, a.k_len, g.k_order);
+    return;
+  }
+  const int n = blockIdx.x - 1, head = blockIdx.y, chunk = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
   const HeadTensor &o = a.o, &d_o = g.d_o;
   __shared__ float deltas[kQueryTile];
   u32x4 x[kQueryTile / kStep], y[kQueryTile / kStep];
@@ -157,7 +162,7 @@ template <typename T, int D, bool CAP, bool BIAS>
 __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const AttnGrads& g, unsigned char* lds, int n, int piece) {
   using S = TileShape<D>;
   QueryTile<D>&even = reinterpret_cast<QueryTile<D>*>(lds)[0], &odd = reinterpret_cast<QueryTile<D>*>(lds)[1];
-  const Place at = place_of(n, a.heads / a.group, a.plan.k_order);
+  const Place at = place_of(n, a.heads / a.group, g.k_order);
   const int kv = at.head, kt = at.tile, lo = at.lo, hi = at.hi;
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave), part = wave >> 1;
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
@@ -335,7 +340,7 @@ __global__ void __launch_bounds__(256) k_attn_back_join(AttnArgs a, AttnGrads g)
   const int n = keys ? blockIdx.x : blockIdx.x - g.k_blocks;
   const Split& sp = keys ? g.k_split : a.split;
   if (sp.most == 1) return;
-  const Place at = keys ? place_of(n, a.heads / a.group, a.plan.k_order) : place_of(n, a.heads, a.plan.q_order);
+  const Place at = keys ? place_of(n, a.heads / a.group, g.k_order) : place_of(n, a.heads, a.plan.q_order);
   const int tiles = keys ? (at.hi > at.lo ? ceil_div_d(at.hi, kQueryTile) - at.lo / kQueryTile : 0) * a.group : ceil_div_d(at.hi, kKeyTile) - at.lo / kKeyTile;
   const Share share = share_of(sp, tiles, all_work(a), a.heads, kLeastTiles, 0);
   if (share.pieces == 1) return;

@@ -48,9 +48,7 @@ struct PlanView {
   RowBound* rows;          // q_len
   GroupBound* groups;      // ceil(q_len / kRowGroup)
   int2* cols;              // per kKeyTile keys: the queries that can see any of them
-  int4 *q_order, *k_order; // tiles of kPatTile queries and of kKeyTile keys, the ones with the most to do first: the tile, and the keys (queries) from y to
-                           // before z that any of its queries sees (that can see any of its keys)
-  unsigned* done;          // workgroups of k_plan_cols that are through
+  int4* q_order;           // tiles of kPatTile queries, the ones with the most to do first: the tile, and the keys from y to before z that its queries see
   unsigned long long* totals;   // tiles of kKeyTile keys that the tiles of queries go over, tiles of kQueryTile queries that those of keys go over
   unsigned* seen;          // ceil(q_len / kPatTile) rows of seen_words
   unsigned* seen_by;       // ceil(k_len / kPatTile) rows of seen_by_words

@@ -63,6 +63,7 @@ struct AttnGrads {
   RowFacts* facts;        // workspace [heads][ceil(q_len / 128) * 2]
   int q_blocks, k_blocks; // workgroups for dQ, for dK and dV, not counting pieces
   Split k_split;
+  int4* k_order;          // workspace: tiles of keys, the ones with the most to do first: the tile, and the queries from y to before z that can see its keys
 };
 
 // Which head and tile a workgroup has, and what the tile reaches.  Workgroups go to the eight dies in turn: heads that share keys stay on one, whose

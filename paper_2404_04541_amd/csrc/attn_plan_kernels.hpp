@@ -93,10 +93,7 @@ __global__ void __launch_bounds__(256) k_plan_rows(MaskView m, PlanView p) {
   plan_row(m, p, i);
   if (blockIdx.x == 0) {
     check_documents(m, p);
-    if (threadIdx.x == 0) {
-      *p.done = 0;
-      p.totals[0] = p.totals[1] = 0;
-    }
+    if (threadIdx.x == 0) p.totals[0] = p.totals[1] = 0;
   }
 }
 
@@ -151,10 +148,11 @@ __device__ __forceinline__ void order_by_work(int n, F work, S store) {
   for (int i = threadIdx.x; i < n; i += 256) store((int)atomicAdd(&count[bucket(i)], 1u), i);
 }
 
-// Both kinds of tiles and what they reach, in order of work, the tiles of queries by a workgroup of its own, those of keys a wave a tile, ordered by the last
-// workgroup to finish: the card holds a few workgroups a compute unit, and long rows that begin late are waited for (two documents of 4000 tokens, tiles
-// from the last row backwards: 1.3 waves a SIMD on average where two fit).  Few tiles all run at once and need no order.
-constexpr int kOrderQueries = 17, kOrderKeys = 48;   // (tiles of keys are ordered at the end, which costs 5 us)
+// What both kinds of tiles reach, a wave a tile of keys; those of queries by a workgroup of its own, which also brings them into order of work: the card
+// holds a few workgroups a compute unit, and long rows that begin late are waited for (two documents of 4000 tokens, tiles from the last row
+// backwards: 1.3 waves a SIMD on average where two fit).  Few tiles all run at once and need no order.  (Tiles of keys are ordered beside
+// k_attn_facts: here that would have to wait for all waves, and a forward pass does not need it; 4096 tokens 8.0 -> FIGURE us.)
+constexpr int kOrderQueries = 17, kOrderKeys = 48;
 __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanView p) {
   const int q_tiles = ceil_div_d(q_len, kPatTile), k_tiles = ceil_div_d(k_len, kKeyTile);
   if (blockIdx.x == gridDim.x - 1) {
@@ -173,31 +171,29 @@ __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanVie
     return;
   }
   const int c = blockIdx.x * 4 + threadIdx.x / kWave;
-  if (c < k_tiles) {
-    const int2 r = key_tile_reach(p, q_len, k_len, c);
-    if (lane_id() == 0) {
-      p.cols[c] = r;
-      atomicAdd(&p.totals[1], (unsigned long long)query_tiles(r));
-      if (k_tiles < kOrderKeys) p.k_order[c] = make_int4(c, r.x, r.y, 0);
-    }
+  if (c >= k_tiles) return;
+  const int2 r = key_tile_reach(p, q_len, k_len, c);
+  if (lane_id() == 0) {
+    p.cols[c] = r;
+    atomicAdd(&p.totals[1], (unsigned long long)query_tiles(r));
   }
-  if (k_tiles < kOrderKeys) return;
-  __shared__ bool final;
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) final = atomicAdd(p.done, 1u) == gridDim.x - 2;
-  __syncthreads();
-  if (!final) return;
-  __threadfence();
-  order_by_work(
-      k_tiles, [&](int i) { const int2 c = p.cols[i]; return c.y - c.x; },
-      [&](int place, int i) { const int2 c = p.cols[i]; p.k_order[place] = make_int4(i, c.x, c.y, 0); });
+}
+
+// Tiles of keys in order of work, by a workgroup of 256 threads.
+__device__ __forceinline__ void order_key_tiles(const PlanView& p, int k_len, int4* order) {
+  const int n = ceil_div_d(k_len, kKeyTile);
+  auto store = [&](int place, int i) { const int2 c = p.cols[i]; order[place] = make_int4(i, c.x, c.y, 0); };
+  if (n < kOrderKeys) {
+    if ((int)threadIdx.x < n) store(threadIdx.x, threadIdx.x);
+  } else {
+    order_by_work(n, [&](int i) { const int2 c = p.cols[i]; return c.y - c.x; }, store);
+  }
 }
 
 // The same for a small mask, whose tiles need no order, by one workgroup: a thread a row, a wave a tile of keys.  us in one launch | in two: 257 tokens 4.6 | 5.0,
 // and 4 less on the host; 2003 tokens by the same kernel 8.5 | 7.5.
 constexpr int kSmallMask = 1024;
-static_assert(kSmallMask / kPatTile < kOrderQueries && kSmallMask / kKeyTile < kOrderKeys && kSmallMask / kKeyTile <= kSmallMask / kWave, "no order, a wave a tile");
+static_assert(kSmallMask / kPatTile < kOrderQueries && kSmallMask / kKeyTile <= kSmallMask / kWave, "no order, a wave a tile");
 __global__ void __launch_bounds__(kSmallMask) k_plan_small(MaskView m, PlanView p) {
   __shared__ unsigned totals[2];
   if (threadIdx.x < 2) totals[threadIdx.x] = 0;
@@ -216,7 +212,7 @@ __global__ void __launch_bounds__(kSmallMask) k_plan_small(MaskView m, PlanView 
     const int2 r = key_tile_reach(p, m.q_len, m.k_len, c);
     if (lane_id() == 0) {
       atomicAdd(&totals[1], query_tiles(r));
-      p.k_order[c] = make_int4(c, r.x, r.y, 0);
+      p.cols[c] = r;
     }
   }
   __syncthreads();
