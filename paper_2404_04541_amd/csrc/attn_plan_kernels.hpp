@@ -117,13 +117,26 @@ __device__ __forceinline__ int2 key_tile_reach(const PlanView& p, int q_len, int
 __device__ __forceinline__ unsigned query_tiles(int2 r) { return ceil_div_d(r.y, kQueryTile) - r.x / kQueryTile; }
 __device__ __forceinline__ unsigned key_tiles(int2 r) { return ceil_div_d(r.y, kKeyTile) - r.x / kKeyTile; }
 
-// Numbers 0 .. n - 1 by falling work(i), as far as 256 steps of the largest tell it, by one workgroup of 256 threads: store(place, i).  (Which of two alike comes first
-// may differ from call to call; it decides only when their workgroups run.)
+// Tiles 0 .. n - 1 by falling work, by one workgroup of 256 threads: order[place] = tile and what reach(tile) says.  Up to 256 of them count how many come before
+// each; more are sorted as far as 256 steps of the largest tell them apart.  (Which of two alike comes first may then differ from call to call; it
+// decides only when their workgroups run.)
 constexpr int kOrderKept = 2048;                 // works that LDS holds between the passes; with more tiles they are made again
-template <typename F, typename S>
-__device__ __forceinline__ void order_by_work(int n, F work, S store) {
+template <typename F>
+__device__ __forceinline__ void order_by_work(int n, F reach, int4* order) {
   __shared__ unsigned most, count[256];
   __shared__ int kept[kOrderKept];
+  if (n <= 256) {
+    const int i = threadIdx.x;
+    const int2 r = i < n ? reach(i) : make_int2(0, 0);
+    const int mine = r.y - r.x;
+    kept[i] = mine;
+    __syncthreads();
+    int place = 0;
+    for (int k = 0; k < n; ++k) place += kept[k] > mine || (kept[k] == mine && k < i);
+    if (i < n) order[place] = make_int4(i, r.x, r.y, 0);
+    return;
+  }
+  auto work = [&](int i) { const int2 r = reach(i); return r.y - r.x; };
   if (threadIdx.x == 0) most = 1;
   count[threadIdx.x] = 0;
   __syncthreads();
@@ -145,13 +158,16 @@ __device__ __forceinline__ void order_by_work(int n, F work, S store) {
     for (int j = 0; j < 4; ++j) { count[threadIdx.x * 4 + j] = before; before += v[j]; }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += 256) store((int)atomicAdd(&count[bucket(i)], 1u), i);
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int2 r = reach(i);
+    order[atomicAdd(&count[bucket(i)], 1u)] = make_int4(i, r.x, r.y, 0);
+  }
 }
 
 // What both kinds of tiles reach, a wave a tile of keys; those of queries by a workgroup of its own, which also brings them into order of work: the card
 // holds a few workgroups a compute unit, and long rows that begin late are waited for (two documents of 4000 tokens, tiles from the last row
 // backwards: 1.3 waves a SIMD on average where two fit).  Few tiles all run at once and need no order.  (Tiles of keys are ordered beside
-// k_attn_facts: here that would have to wait for all waves, and a forward pass does not need it; 4096 tokens 8.0 -> FIGURE us.)
+// k_attn_facts: here that would have to wait for all waves, and a forward pass does not need it; 4096 tokens 8.0 -> 6.7 us, by counting 5.2.)
 constexpr int kOrderQueries = 17, kOrderKeys = 48;
 __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanView p) {
   const int q_tiles = ceil_div_d(q_len, kPatTile), k_tiles = ceil_div_d(k_len, kKeyTile);
@@ -164,10 +180,7 @@ __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanVie
       if (q_tiles < kOrderQueries) p.q_order[q_tiles - 1 - i] = make_int4(i, r.x, r.y, 0);
     }
     if (sum) atomicAdd(&p.totals[0], sum);
-    if (q_tiles >= kOrderQueries)
-      order_by_work(
-          q_tiles, [&](int i) { const int2 r = reach(i); return r.y - r.x; },
-          [&](int place, int i) { const int2 r = reach(i); p.q_order[place] = make_int4(i, r.x, r.y, 0); });
+    if (q_tiles >= kOrderQueries) order_by_work(q_tiles, reach, p.q_order);
     return;
   }
   const int c = blockIdx.x * 4 + threadIdx.x / kWave;
@@ -182,11 +195,12 @@ __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanVie
 // Tiles of keys in order of work, by a workgroup of 256 threads.
 __device__ __forceinline__ void order_key_tiles(const PlanView& p, int k_len, int4* order) {
   const int n = ceil_div_d(k_len, kKeyTile);
-  auto store = [&](int place, int i) { const int2 c = p.cols[i]; order[place] = make_int4(i, c.x, c.y, 0); };
-  if (n < kOrderKeys) {
-    if ((int)threadIdx.x < n) store(threadIdx.x, threadIdx.x);
-  } else {
-    order_by_work(n, [&](int i) { const int2 c = p.cols[i]; return c.y - c.x; }, store);
+  auto reach = [&](int i) { return p.cols[i]; };
+  if (n >= kOrderKeys) {
+    order_by_work(n, reach, order);
+  } else if ((int)threadIdx.x < n) {
+    const int2 r = reach(threadIdx.x);
+    order[threadIdx.x] = make_int4(threadIdx.x, r.x, r.y, 0);
   }
 }
 

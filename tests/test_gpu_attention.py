@@ -108,6 +108,15 @@ def test_around_a_small_plan(h, tq, tk):
     run(h, *tensors(41, BF, tq, tk, 2, 1, 64), {"q_ptr": [0, tq // 3, tq], "k_ptr": [0, tk // 2, tk], "window": 500})
 
 
+@pytest.mark.parametrize("tq, tk", [(33100, 90), (262200, 70), (90, 16500), (70, 131200)])
+def test_many_tiles_in_order(h, tq, tk):
+    """Tiles are ordered by their work: up to 256 of them by counting, more by sorting, whose works LDS holds or does not.  Documents of a few thousand tokens, so that
+    sums stay as short as the bounds take them to be."""
+    docs = min(tq, tk) // 2
+    cut = lambda n: [int(n * (i / docs) ** 1.2) for i in range(docs + 1)]  # noqa: E731
+    run(h, *tensors(42, BF, tq, tk, 1, 1, 8), {"q_ptr": cut(tq), "k_ptr": cut(tk), "causal": False})
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("cap, bias", [(0.0, False), (20.0, False), (100.0, False), (20.0, True), (0.0, True)])
 def test_rows_in_pieces(h, d, cap, bias):
