@@ -166,14 +166,16 @@ AttnArgs attn_args(const spattn_args* a, const spattn_tensor& o, const float* ls
   return g;
 }
 
-// How a pass over `blocks` workgroups, each with at most `tiles` tiles, may be shared: the card holds `resident` of them a compute unit; where the
-// workgroups fill it nothing is shared, nor where the longest is short, else there are places for pieces until it is filled twice.
-int split_pieces(spgemm_context* h, int64_t blocks, int64_t all, int64_t tiles, int resident) {
+// How many pieces the rows of `blocks` workgroups, each with at most `tiles` tiles, may be cut into: the card holds `resident` workgroups a compute unit; where `all`
+// workgroups of a launch fill it `rounds` times nothing is cut, nor where the longest is short, else there are places for pieces until it is filled twice.
+int split_pieces(spgemm_context* h, int64_t blocks, int64_t all, int64_t tiles, int resident, int rounds) {
   const int64_t slots = (int64_t)h->num_cus * resident;
-  if (blocks == 0 || all >= 2 * slots || tiles <= 2 * kLeastTiles) return 1;
+  if (blocks == 0 || all >= rounds * slots || tiles <= 2 * kLeastTiles) return 1;
   const int64_t most = ceil_div(2 * slots, blocks) + 1;
   return (int)(most < 64 ? most : 64);
 }
+// Eleven documents, 4096 tokens, us whole | cut: forward (512 workgroups, 512 places) 38 | 37 and 7 to join, gradients (768) FIGURE | 86 and 7.
+constexpr int kRoundsForward = 1, kRoundsBackward = 2;
 size_t split_bytes(int64_t blocks, int most, int room) {
   return most == 1 ? 0 : align_up((size_t)blocks * most * 128 * room * sizeof(float)) + align_up((size_t)blocks * most * kPatTile * sizeof(float2));
 }
@@ -332,7 +334,7 @@ int spattn_forward(spgemm_handle h, const spattn_args* a, spattn_tensor o, float
     AttnArgs g = attn_args(a, o, lse);
     const int64_t blocks = (int64_t)g.q_tiles * g.heads;
     const int room = a->head_dim <= 64 ? 64 : 128, resident = room == 64 ? 4 : 2;
-    const int most = split_pieces(h, blocks, 2 * blocks, ceil_div(a->mask->k_len, kKeyTile), resident);
+    const int most = split_pieces(h, blocks, blocks, ceil_div(a->mask->k_len, kKeyTile), resident, kRoundsForward);
     void* mem = nullptr;
     if (most > 1 && (rc = scratch(h, split_bytes(blocks, most, room), &mem))) return rc;
     g.split = split_of(h, blocks, most, resident, room, mem);
@@ -371,8 +373,8 @@ int spattn_backward(spgemm_handle h, const spattn_args* a, spattn_tensor o, cons
     const int room = a->head_dim <= 64 ? 64 : 128, resident = room == 64 ? 3 : 2;
     const int64_t g_heads = a->heads / a->kv_heads;
     const int64_t both = q_blocks + k_blocks;
-    const int q_most = split_pieces(h, q_blocks, both, ceil_div(k_len, kKeyTile), resident);
-    const int k_most = split_pieces(h, k_blocks, both, ceil_div(q_len, kQueryTile) * g_heads, resident);
+    const int q_most = split_pieces(h, q_blocks, both, ceil_div(k_len, kKeyTile), resident, kRoundsBackward);
+    const int k_most = split_pieces(h, k_blocks, both, ceil_div(q_len, kQueryTile) * g_heads, resident, kRoundsBackward);
     const size_t q_part = split_bytes(q_blocks, q_most, room), k_part = split_bytes(k_blocks, k_most, room);
     void* mem = nullptr;
     if ((rc = scratch(h, order + facts + q_part + k_part, &mem))) return rc;
@@ -406,7 +408,7 @@ int spcache_append(spgemm_handle h, const spcache* c, int64_t layer, const spgem
     if (tokens == 0 || table->rows == 0) return SPGEMM_OK;
     if (!new_ptr) return fail(h, SPGEMM_INVALID_ARG, "new_ptr is null");
     const int64_t slots = tokens / SPCACHE_PAGE + 2 * table->rows;
-    if (slots > 0x7fffffffLL) return fail(h, SPGEMM_UNSUPPORTED, "too many sequences");
+    if (slots > 0xffffff) return fail(h, SPGEMM_UNSUPPORTED, "too many sequences");   // (2^32 threads are a launch's limit)
     if ((rc = ensure_device(h))) return rc;
     const AppendArgs a{view(c, layer), view(table, lens), new_ptr, view(k), view(v), tokens};
     const dim3 grid((unsigned)slots, (unsigned)c->kv_heads);
@@ -445,7 +447,7 @@ int spcache_attend(spgemm_handle h, const spcache* c, int64_t layer, const spgem
     chunk = chunk < 4 ? 4 : ceil_div(chunk, 4) * 4;
     a.chunk = (int)chunk;
     const int64_t slots = table->nnz / chunk + n;
-    if (slots > 0x7fffffffLL) return fail(h, SPGEMM_UNSUPPORTED, "too many pages");
+    if (slots > 0xffffff) return fail(h, SPGEMM_UNSUPPORTED, "too many pages");   // (2^32 threads are a launch's limit)
     const int64_t cells = slots * c->kv_heads * tiles;
     const int room = room_of(c);
     const size_t part = align_up((size_t)cells * kRows * room * sizeof(float)), ml = align_up((size_t)cells * kRows * sizeof(float2));

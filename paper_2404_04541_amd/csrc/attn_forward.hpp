@@ -6,6 +6,13 @@
 // probabilities are the second product's right operand as they are (attn_common.hpp).  One pass: out = sum_j 2^(x_j - m) v_j with the running
 // maximum m; sums and maxima in 32 bits, probabilities rounded to 16 bits once, as an operand.  The accumulators are brought to a
 // new maximum only where some row's grew by more than 2^8 since (the sum is in the same units, so nothing is approximated).
+//
+// Measured (bfloat16, 128 channels): two documents of 8192 tokens together, 16 heads on 8, capped, 200 us, 0.69 PFLOP/s; 5003 queries over 11 147 keys through a
+// pattern, 32 heads on 8, with distances, 169 us, 0.66.  Vector instructions issue in 56 % of the cycles (49 in the second), eight an entry with a cap,
+// three of them powers and reciprocals; matrix instructions run in 37 % (38), LDS in 28 %: what vector and matrix instructions take
+// together bounds it, for two waves a SIMD, as many as the registers allow, hardly overlap.  Tiles of 32 keys for three waves, products of the next tile beside
+// the powers of this one (in the order of the code or by hints to the scheduler) and priorities were all slower.  Short rows (documents of a few
+// hundred tokens) are bound by the chain of their tiles, 2 us each.
 #pragma once
 #include "attn_common.hpp"
 
@@ -20,7 +27,8 @@ struct HeadTensor {       // rows of a packed tensor with heads: token t of head
 };
 
 // Long rows may be shared by several workgroups, each with a stretch of the tiles; their sums are joined, in order, by a kernel of their own (joined by the
-// last workgroup to finish, the fences that takes cost every workgroup more than the launch: 18 + 8 | 49 us).  A workgroup leaves the registers of its accumulators as they are: float4 [piece][workgroup][4 D / 32][256], and for rows maximum and sum.
+// last workgroup to finish, the fences that takes cost every workgroup more than the launch: 18 + 8 | 49 us).  A workgroup leaves the registers of its
+// accumulators as they are: float4 [piece][workgroup][4 D / 32][256], and for rows maximum and sum.  2003 tokens, 8 heads: forward 33 | 17 us and 5 to join.
 struct Split {
   int most;               // pieces that the grid has places for (1: nothing is shared)
   int slots;              // workgroups that the card holds at once
@@ -29,7 +37,7 @@ struct Split {
 };
 
 // The stretch of n tiles that a piece has.  A piece is half as long again as the average of what the card's places have to do, and at least `least`:
-// shorter ones cost more in joining than they save.
+// shorter ones cost more in joining than they save (gradients of documents of 4096 tokens, pieces of 1, 1.25, 1.5 and 2 averages: 98, 88, 86, 103 us).
 struct Share { int first, last, pieces; };
 __device__ __forceinline__ Share share_of(const Split& sp, int n, unsigned long long total, int heads, int least, int piece) {
   if (sp.most == 1) return {0, n, 1};
@@ -321,7 +329,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
   finish_rows<T, D>(a, head, row, half, 0, acc, m, l);
 }
 
-// A workgroup has 32 channels of a tile's rows.
+// A workgroup has 32 channels of a tile's rows.  2003 tokens, 8 heads of 64 channels: 4.8 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
   const Place at = place_of(blockIdx.x, a.heads, a.plan.q_order);

@@ -3,6 +3,8 @@
 // A table is a compressed structure (rows: sequences, columns: pages).  Everything here but the copies is a few bytes a row or page: what it
 // costs is launches and dependent loads, so that ranks (the k-th free page) are found by counting bits in a flag list, as the
 // product's kernels rank columns.  No result depends on the order of atomics: they count, take minima, or set bits.
+// us, without copies: a fork of 8 rows 2.4 + 2.7 + 2.6 + 3.9 (by one workgroup 17), 512 rows from 384 3.1 + 8 + 3.7 + 7.3 (gather: atomics on pages that many rows share);
+// compacting 2048 pages 1.5 + 4.6 + 2.3 + 4.0.
 #pragma once
 #include "cache_kernels.hpp"
 
@@ -309,7 +311,7 @@ struct CopyArgs {
 
 constexpr int kCopyPiece = 16384;    // bytes that a workgroup copies at a time: four loads of 16 bytes in flight a lane
 
-// Destinations are distinct and no source, so the copies need no order.
+// Destinations are distinct and no source, so the copies need no order.  Memory bounds it: 237 MB read and written 40 us, 5.9 TB/s; 530 MB 116 us, 4.6.
 __global__ void __launch_bounds__(256) k_page_copy(CopyArgs a) {
   if (a.report && blockIdx.x == 0 && threadIdx.x == 0) *a.report = *a.in;
   if (a.in && a.in->error) return;
