@@ -166,16 +166,15 @@ AttnArgs attn_args(const spattn_args* a, const spattn_tensor& o, const float* ls
   return g;
 }
 
-// How many pieces the rows of `blocks` workgroups, each with at most `tiles` tiles, may be cut into: the card holds `resident` workgroups a compute unit; where `all`
-// workgroups of a launch fill it `rounds` times nothing is cut, nor where the longest is short, else there are places for pieces until it is filled twice.
-int split_pieces(spgemm_context* h, int64_t blocks, int64_t all, int64_t tiles, int resident, int rounds) {
+// How many pieces the forward pass's rows may be cut into, with at most `tiles` tiles each: the card holds `resident` workgroups a compute unit; where `blocks` fill it
+// nothing is cut (eleven documents, 4096 tokens, 512 workgroups for 512 places, us whole | cut: 38 | 37 and 7 to join), nor where the longest is
+// short, else there are places for pieces until it is filled twice.
+int split_pieces(spgemm_context* h, int64_t blocks, int64_t tiles, int resident) {
   const int64_t slots = (int64_t)h->num_cus * resident;
-  if (blocks == 0 || all >= rounds * slots || tiles <= 2 * kLeastTiles) return 1;
+  if (blocks == 0 || blocks >= slots || tiles <= 2 * kLeastTiles) return 1;
   const int64_t most = ceil_div(2 * slots, blocks) + 1;
   return (int)(most < 64 ? most : 64);
 }
-// Eleven documents, 4096 tokens, us whole | cut: forward (512 workgroups, 512 places) 38 | 37 and 7 to join, gradients (768) FIGURE | 86 and 7.
-constexpr int kRoundsForward = 1, kRoundsBackward = 2;
 size_t split_bytes(int64_t blocks, int most, int room) {
   return most == 1 ? 0 : align_up((size_t)blocks * most * 128 * room * sizeof(float)) + align_up((size_t)blocks * most * kPatTile * sizeof(float2));
 }
@@ -334,7 +333,7 @@ int spattn_forward(spgemm_handle h, const spattn_args* a, spattn_tensor o, float
     AttnArgs g = attn_args(a, o, lse);
     const int64_t blocks = (int64_t)g.q_tiles * g.heads;
     const int room = a->head_dim <= 64 ? 64 : 128, resident = room == 64 ? 4 : 2;
-    const int most = split_pieces(h, blocks, blocks, ceil_div(a->mask->k_len, kKeyTile), resident, kRoundsForward);
+    const int most = split_pieces(h, blocks, ceil_div(a->mask->k_len, kKeyTile), resident);
     void* mem = nullptr;
     if (most > 1 && (rc = scratch(h, split_bytes(blocks, most, room), &mem))) return rc;
     g.split = split_of(h, blocks, most, resident, room, mem);
@@ -368,27 +367,37 @@ int spattn_backward(spgemm_handle h, const spattn_args* a, spattn_tensor o, cons
       return rc;
     if (q_len > 0 && !lse) return fail(h, SPGEMM_INVALID_ARG, "lse is null");
     if ((rc = ensure_device(h))) return rc;
-    const size_t order = align_up((size_t)ceil_div(k_len, kKeyTile) * sizeof(int4)), facts = align_up((size_t)a->heads * ceil_div(q_len, kPatTile) * (kPatTile / kQueryTile) * sizeof(RowFacts));
-    const int64_t q_blocks = ceil_div(q_len, kPatTile) * a->heads, k_blocks = ceil_div(k_len, kKeyTile) * a->kv_heads;
-    const int room = a->head_dim <= 64 ? 64 : 128, resident = room == 64 ? 3 : 2;
-    const int64_t g_heads = a->heads / a->kv_heads;
-    const int64_t both = q_blocks + k_blocks;
-    const int q_most = split_pieces(h, q_blocks, both, ceil_div(k_len, kKeyTile), resident, kRoundsBackward);
-    const int k_most = split_pieces(h, k_blocks, both, ceil_div(q_len, kQueryTile) * g_heads, resident, kRoundsBackward);
-    const size_t q_part = split_bytes(q_blocks, q_most, room), k_part = split_bytes(k_blocks, k_most, room);
-    void* mem = nullptr;
-    if ((rc = scratch(h, order + facts + q_part + k_part, &mem))) return rc;
-    unsigned char *rows = static_cast<unsigned char*>(mem) + order, *part = rows + facts;
-    AttnArgs g = attn_args(a, o, lse);
-    AttnGrads r{view(d_o), view(dq), view(dk), view(dv), reinterpret_cast<RowFacts*>(rows), (int)q_blocks, (int)k_blocks,
-                split_of(h, k_blocks, k_most, resident, room, part + q_part), static_cast<int4*>(mem)};
-    g.split = split_of(h, q_blocks, q_most, resident, room, part);
+    const int64_t q_tiles = ceil_div(q_len, kPatTile), k_tiles = ceil_div(k_len, kKeyTile), both = q_tiles * a->heads + k_tiles * a->kv_heads;
     if (both == 0) return SPGEMM_OK;
+    const int room = a->head_dim <= 64 ? 64 : 128, resident = room == 64 ? 3 : 2;
+    // Where the card's places are filled less than four times, long tiles are cut: pieces_of bounds how many more workgroups that makes, and how many
+    // pieces have to be joined.  us whole | cut, 16 heads on 4: 32 documents of 128 tokens and one of 4096 478 | 331, eleven of 4096 together 179 | 97; 16 heads on 16 of 64 channels,
+    // 4096 tokens in two documents 107 | 111.
+    int64_t slots = (int64_t)h->num_cus * resident;
+    if (both >= 4 * slots || (ceil_div(q_len, kQueryTile) * (a->heads / a->kv_heads) <= 2 * kLeastTiles && ceil_div(k_len, kKeyTile) <= 2 * kLeastTiles)) slots = 0;
+    const int64_t more = 2 * slots / 3 + 1, cells = slots ? 2 * more : 0;
+    Carve c{nullptr};
+    AttnGrads r{view(d_o), view(dq), view(dk), view(dv)};
+    auto carve = [&] {
+      r.facts = c.take<RowFacts>(a->heads * q_tiles * (kPatTile / kQueryTile));
+      r.k_list = c.take<int4>(k_tiles + more);
+      r.q_list = c.take<int4>(q_tiles + more);
+      r.counts = c.take<Counts>(1);
+      r.sums = c.take<f32x4>(cells * 32 * room);
+    };
+    carve();
+    void* mem = nullptr;
+    if ((rc = scratch(h, c.used, &mem))) return rc;
+    c = Carve{static_cast<unsigned char*>(mem)};
+    carve();
+    r.slots = (int)slots;
+    r.more = (int)more;
+    AttnArgs g = attn_args(a, o, lse);
     auto launch = [&](auto type, auto dim, auto cap, auto bias) {
       using T = decltype(type);
-      k_attn_facts<T, dim()><<<dim3((unsigned)g.q_tiles * (kPatTile / kQueryTile) + 1, (unsigned)a->heads), dim3(256), 0, h->stream>>>(g, r);
-      k_attn_back<T, dim(), cap(), bias()><<<dim3((unsigned)(q_blocks * q_most + k_blocks * k_most)), dim3(256), 0, h->stream>>>(g, r);
-      if (q_most > 1 || k_most > 1) k_attn_back_join<T, dim(), cap()><<<dim3((unsigned)both, dim() / 32), dim3(256), 0, h->stream>>>(g, r);
+      k_attn_facts<T, dim()><<<dim3((unsigned)g.q_tiles * (kPatTile / kQueryTile) + 2, (unsigned)a->heads), dim3(256), 0, h->stream>>>(g, r);
+      k_attn_back<T, dim(), cap(), bias()><<<dim3((unsigned)(slots ? both + more : both)), dim3(256), 0, h->stream>>>(BackArgs{g, r});
+      if (slots) k_attn_back_join<T, dim(), cap()><<<dim3((unsigned)cells, dim() / 32), dim3(256), 0, h->stream>>>(g, r);
     };
     dispatch(a->dtype, a->head_dim, a->cap > 0, a->slopes != nullptr, launch);
     return launched(h);

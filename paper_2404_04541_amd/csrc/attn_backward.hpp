@@ -7,8 +7,8 @@
 // the queries, of all heads that share them, of 64 keys.  That computes S and dP twice, seven products where five would do with atomics on dQ in 32 bits.
 // P, dS are rounded to 16 bits once, as operands; all sums are held in 32 bits.
 //
-// Measured (bfloat16, 128 channels, capped): two documents of 8192 tokens together, 16 heads on 8, 655 us, 0.74 PFLOP/s for the seven products (vector instructions issue in
-// 52 % of the cycles, matrix instructions run in 39 %, LDS in 31 %: as the forward kernel); eleven documents of 4096 tokens, 16 heads on 4, 86 us and 6.6 to join, where two launches, one after
+// Measured (bfloat16, 128 channels, capped): two documents of 8192 tokens together, 16 heads on 8, 647 us, 0.75 PFLOP/s for the seven products (vector instructions issue in
+// 52 % of the cycles, matrix instructions run in 39 %, LDS in 31 %: as the forward kernel); eleven documents of 4096 tokens, 16 heads on 4, 82 us and 5.3 to join, where two launches, one after
 // the other, took 126 and 8.6: the long chains of one kind fill the places that the other leaves.
 #pragma once
 #include "attn_forward.hpp"
@@ -16,19 +16,49 @@
 
 namespace spg {
 
-// Tiles that all workgroups go over together, of one head.
-__device__ __forceinline__ unsigned long long all_work(const AttnArgs& a) { return load_uniform(a.plan.totals) + load_uniform(a.plan.totals + 1); }
+// The work of n tiles as a list, most first, by one workgroup of 256 threads; tiles of up to 256 are cut into pieces where there are places for them (more
+// fill the card).  counts: the list's length, and how many of its entries belong to cut tiles: they come first.
+template <typename F, typename W>
+__device__ __forceinline__ void list_work(int n, F reach, W tiles, unsigned long long total, const AttnGrads& g, int4* list, int* counts) {
+  if (n > 256) {
+    order_by_work(n, reach, list);
+    if (threadIdx.x == 0) { counts[0] = n; counts[1] = 0; }
+    return;
+  }
+  __shared__ int2 of[256];                       // tiles, pieces
+  const int i = threadIdx.x;
+  const int2 r = i < n ? reach(i) : make_int2(0, 0);
+  const int mine = tiles(r), cut = i < n && g.slots ? pieces_of(mine, g.slots, total) : 1;
+  of[i] = i < n ? make_int2(mine, cut) : make_int2(0, 0);
+  __syncthreads();
+  int place = 0, all = 0, front = 0;
+#pragma unroll 16
+  for (int k = 0; k < ceil_div_d(n, 16) * 16; ++k) {
+    const int2 x = of[k];
+    place += (x.x > mine) | ((x.x == mine) & (k < i)) ? x.y : 0;
+    all += x.y;
+    front += x.y > 1 ? x.y : 0;
+  }
+  if (i < n)
+    for (int p = 0; p < cut && place + p < n + g.more; ++p) list[place + p] = make_int4(i, r.x, r.y, cut + 65536 * p);
+  if (i == 0) { counts[0] = min(all, n + g.more); counts[1] = min(front, n + g.more); }
+}
 
-// A workgroup has 64 rows of a head: D / 8 lanes a row, 16 bytes of O and dO each.  The first one brings the tiles of keys into order meanwhile.
-// Memory bounds it: 8192 tokens, 16 heads of 128 channels 14.2 us, 4.7 TB/s; 4096 tokens 8.2 us.
+// A workgroup has 64 rows of a head: D / 8 lanes a row, 16 bytes of O and dO each.  The first two make the lists of work meanwhile.
+// Memory bounds it: 8192 tokens, 16 heads of 128 channels 14.2 us, 4.7 TB/s; 4096 tokens 8.2 us, with lists of cut work 9.5.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_attn_facts(AttnArgs a, AttnGrads g) {
   constexpr int kLanes = D / 8, kStep = 256 / kLanes;
-  if (blockIdx.x == 0) {
-    if (blockIdx.y == 0) order_key_tiles(a.plan, a.k_len, g.k_order);
+  if (blockIdx.x < 2) {
+    if (blockIdx.y > 0) return;
+    const unsigned long long total = (load_uniform(a.plan.totals) + load_uniform(a.plan.totals + 1)) * a.heads;
+    if (blockIdx.x == 0)
+      list_work(ceil_div_d(a.k_len, kKeyTile), [&](int i) { return a.plan.cols[i]; }, [&](int2 r) { return (int)query_tiles(r) * a.group; }, total, g, g.k_list, &g.counts->keys);
+    else
+      list_work(a.q_tiles, [&](int i) { return query_tile_reach(a.plan, a.q_len, i); }, [](int2 r) { return (int)key_tiles(r); }, total, g, g.q_list, &g.counts->queries);
     return;
   }
-  const int n = blockIdx.x - 1, head = blockIdx.y, chunk = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
+  const int n = blockIdx.x - 2, head = blockIdx.y, chunk = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
   const HeadTensor &o = a.o, &d_o = g.d_o;
   __shared__ float deltas[kQueryTile];
   u32x4 x[kQueryTile / kStep], y[kQueryTile / kStep];
@@ -65,20 +95,32 @@ __global__ void __launch_bounds__(256) k_attn_facts(AttnArgs a, AttnGrads g) {
   facts.diag[i] = rb.diag;
 }
 
+// k_attn_back's arguments, read where they are wanted: the compiler loads all arguments of a kernel at its begin, and with those of both kinds of work the scalar
+// registers did not do (70 of them kept in lanes of vector registers; 8192 tokens 682 -> 647 us).
+struct BackArgs { AttnArgs a; AttnGrads g; };
+__device__ __forceinline__ BackArgs back_args() {
+  typedef const __attribute__((address_space(4))) BackArgs Memory;
+  Memory* p = (Memory*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const BackArgs*)p;
+}
+
 template <typename T, int D, bool CAP, bool BIAS>
-__device__ __forceinline__ void dq_tile(const AttnArgs& a, const AttnGrads& g, unsigned char* lds, int n, int piece) {
+__device__ __forceinline__ void dq_tile(unsigned char* lds, int n) {
+  const BackArgs args = back_args();
+  const AttnArgs& a = args.a;
+  const AttnGrads& g = args.g;
   using S = TileShape<D>;
   constexpr int kTile = kKeyTile * D * 2;
   unsigned char *k_even = lds, *v_even = lds + kTile, *k_odd = lds + 2 * kTile, *v_odd = lds + 3 * kTile;
-  const Place at = place_of(n, a.heads, a.plan.q_order);
+  const Place at = place_of(n, a.heads, g.q_list);
   const int head = at.head, qt = at.tile, lo = at.lo, hi = at.hi;
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave);
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
   const int row = qt * kPatTile + wave * kRowGroup + (lane & 31);
   const GroupBound mine = wave_bound(a, qt, wave);
   const int begin = lo / kKeyTile;
-  const Share share = share_of(a.split, ceil_div_d(hi, kKeyTile) - begin, a.split.most > 1 ? all_work(a) : 0, a.heads, kLeastTiles, piece);
-  if (piece >= share.pieces) return;
+  const Share share = share_of(ceil_div_d(hi, kKeyTile) - begin, at.piece & 0xffff, at.piece >> 16);
   const ScoreFactors f = score_factors<CAP, BIAS>(a.score, head);
   const bool real = row < a.q_len;
   const RowBound rb = real ? a.plan.rows[row] : RowBound{0, 0, 0, 0};
@@ -150,8 +192,9 @@ __device__ __forceinline__ void dq_tile(const AttnArgs& a, const AttnGrads& g, u
     c = next;
   }
 
-  if (share.pieces > 1) leave_sums<D>(a.split, (int64_t)piece * g.q_blocks + n, acc);
-  else if (real) store_rows<T, D>(g.dq, head, row, half, 0, a.bytes, acc, CAP ? 4.0f * a.score.scale : a.score.scale);
+  const BackArgs end_args = back_args();
+  if (share.pieces > 1) leave_sums<D>(end_args.g.sums, load_uniform(&end_args.g.counts->cut_keys) * (end_args.a.heads / end_args.a.group) + n, acc);
+  else if (row < end_args.a.q_len) store_rows<T, D>(end_args.g.dq, head, row, half, 0, end_args.a.bytes, acc, (CAP ? 4.0f : 1.0f) * end_args.a.score.scale);
 }
 
 // A workgroup has 64 keys of a key head and goes over their queries in tiles of 64 rows, head by head.  Wave w has keys 32 (w % 2) .. and of every
@@ -164,10 +207,13 @@ struct QueryTile {
 };
 
 template <typename T, int D, bool CAP, bool BIAS>
-__device__ __forceinline__ void dkv_tile(const AttnArgs& a, const AttnGrads& g, unsigned char* lds, int n, int piece) {
+__device__ __forceinline__ void dkv_tile(unsigned char* lds, int n) {
+  const BackArgs args = back_args();
+  const AttnArgs& a = args.a;
+  const AttnGrads& g = args.g;
   using S = TileShape<D>;
   QueryTile<D>&even = reinterpret_cast<QueryTile<D>*>(lds)[0], &odd = reinterpret_cast<QueryTile<D>*>(lds)[1];
-  const Place at = place_of(n, a.heads / a.group, g.k_order);
+  const Place at = place_of(n, a.heads / a.group, g.k_list);
   const int kv = at.head, kt = at.tile, lo = at.lo, hi = at.hi;
   const int lane = lane_id(), half = lane >> 5, wave = uniform(threadIdx.x / kWave), part = wave >> 1;
   const int row_base = S::row_base(lane), across_base = S::across_base(lane);
@@ -184,8 +230,7 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const AttnGrads& g, 
   const int low = hi > lo ? lo / kQueryTile : 0, end = hi > lo ? ceil_div_d(hi, kQueryTile) : 0, tiles = end - low;
   const int begin = next_tile(flags, low, end);
   // the work is a list: all tiles of one head, then of the next
-  const Share share = share_of(g.k_split, tiles * a.group, g.k_split.most > 1 ? all_work(a) : 0, a.heads, kLeastTiles, piece);
-  if (piece >= share.pieces) return;
+  const Share share = share_of(tiles * a.group, at.piece & 0xffff, at.piece >> 16);
 
   auto load = [&](QueryTile<D>& t, int head, int tile) {
     const int first = tile * kQueryTile;
@@ -322,37 +367,40 @@ __device__ __forceinline__ void dkv_tile(const AttnArgs& a, const AttnGrads& g, 
 #pragma unroll
       for (int j = 0; j < 4; ++j) sum[i][4 * r + j] = (part ? dv[i][4 * r + j] : dk[i][4 * r + j]) + x[j];
     }
-  if (share.pieces > 1) leave_sums<D>(g.k_split, (int64_t)piece * g.k_blocks + n, sum);
-  else if (real) store_rows<T, D>(part ? g.dv : g.dk, kv, key, half, 0, a.bytes, sum, part ? 1.0f : CAP ? 4.0f * a.score.scale : a.score.scale);
+  const BackArgs end_args = back_args();
+  if (share.pieces > 1) leave_sums<D>(end_args.g.sums, n, sum);
+  else if (key < end_args.a.k_len)
+    store_rows<T, D>(part ? end_args.g.dv : end_args.g.dk, kv, key, half, 0, end_args.a.bytes, sum, part ? 1.0f : (CAP ? 4.0f : 1.0f) * end_args.a.score.scale);
 }
 
-// Keys' workgroups come first, for their chains are the longer ones.
+// Keys' workgroups come first, for their chains are the longer ones.  How many there are only the lists know: the last ones have nothing.
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, 2) k_attn_back(AttnArgs a, AttnGrads g) {
+__global__ void __launch_bounds__(256, 2) k_attn_back(BackArgs) {
   static_assert(sizeof(QueryTile<D>) >= 2 * kKeyTile * D * 2, "both kinds fit");
   __shared__ __align__(16) unsigned char lds[2 * sizeof(QueryTile<D>)];
-  const int n = blockIdx.x, keys = g.k_blocks * g.k_split.most;
-  if (n < keys) dkv_tile<T, D, CAP, BIAS>(a, g, lds, n % g.k_blocks, n / g.k_blocks);
-  else dq_tile<T, D, CAP, BIAS>(a, g, lds, (n - keys) % g.q_blocks, (n - keys) / g.q_blocks);
+  const BackArgs args = back_args();
+  const Counts c = load_uniform(args.g.counts);
+  const int n = blockIdx.x, keys = uniform(c.keys * (args.a.heads / args.a.group)), queries = uniform(c.queries * args.a.heads);
+  if (n < keys) dkv_tile<T, D, CAP, BIAS>(lds, n);
+  else if (n - keys < queries) dq_tile<T, D, CAP, BIAS>(lds, n - keys);
 }
 
 // A workgroup has 32 channels of a tile's rows (keys).
 template <typename T, int D, bool CAP>
 __global__ void __launch_bounds__(256) k_attn_back_join(AttnArgs a, AttnGrads g) {
+  const Counts c = load_uniform(g.counts);
+  const int kv_heads = a.heads / a.group, keys = c.cut_keys * kv_heads, n = blockIdx.x;
+  if (n >= keys + c.cut_queries * a.heads) return;
+  const bool of_keys = n < keys;
+  const int heads = of_keys ? kv_heads : a.heads;
+  const Place at = place_of(of_keys ? n : n - keys, heads, of_keys ? g.k_list : g.q_list);
+  if (at.piece >> 16) return;
   const int c0 = blockIdx.y * 32, lane = lane_id(), wave = uniform(threadIdx.x / kWave);
   const float by = CAP ? 4.0f * a.score.scale : a.score.scale;
-  const bool keys = (int)blockIdx.x < g.k_blocks;
-  const int n = keys ? blockIdx.x : blockIdx.x - g.k_blocks;
-  const Split& sp = keys ? g.k_split : a.split;
-  if (sp.most == 1) return;
-  const Place at = keys ? place_of(n, a.heads / a.group, g.k_order) : place_of(n, a.heads, a.plan.q_order);
-  const int tiles = keys ? (at.hi > at.lo ? ceil_div_d(at.hi, kQueryTile) - at.lo / kQueryTile : 0) * a.group : ceil_div_d(at.hi, kKeyTile) - at.lo / kKeyTile;
-  const Share share = share_of(sp, tiles, all_work(a), a.heads, kLeastTiles, 0);
-  if (share.pieces == 1) return;
   f32x16 sum = {};
 #pragma unroll 4
-  for (int p = 0; p < share.pieces; ++p) add_sums<D>(sp, (int64_t)p * (keys ? g.k_blocks : g.q_blocks) + n, c0, 1.0f, sum);
-  if (keys) {
+  for (int p = 0; p < (at.piece & 0xffff); ++p) add_sums<D>(g.sums, n + (int64_t)p * heads, c0, 1.0f, sum);   // (a head's next piece is so many places on)
+  if (of_keys) {
     const int part = wave >> 1, key = at.tile * kKeyTile + (wave & 1) * 32 + (lane & 31);
     if (key < a.k_len) store_rows<T, 32>(part ? g.dv : g.dk, at.head, key, lane >> 5, c0, a.bytes, &sum, part ? 1.0f : by);
   } else {

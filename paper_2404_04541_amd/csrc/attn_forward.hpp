@@ -36,19 +36,25 @@ struct Split {
   float2* tops;           // [piece][workgroup][128]: maximum in units of log 2, sum
 };
 
-// The stretch of n tiles that a piece has.  A piece is half as long again as the average of what the card's places have to do, and at least `least`:
-// shorter ones cost more in joining than they save (gradients of documents of 4096 tokens, pieces of 1, 1.25, 1.5 and 2 averages: 98, 88, 86, 103 us).
+// How many pieces n tiles are cut into.  A piece is half as long again as the average of what the card's `slots` places have to do (total: what
+// all workgroups have), and at least kLeastTiles: shorter ones cost more in joining than they save (gradients of documents of 4096 tokens, pieces
+// of 1, 1.25, 1.5 and 2 averages: 98, 88, 86, 103 us).  So all together are cut into at most 2/3 slots more than they are.
+constexpr int kLeastTiles = 4;
+__device__ __forceinline__ int pieces_of(int n, int slots, unsigned long long total) {
+  const float even = fminf((float)total * 1.5f / (float)slots, (float)n);   // (a large number in 24 bits: less than one tile off)
+  const int per = max((int)even + 1, kLeastTiles);
+  return n > 2 * kLeastTiles ? ceil_div_d(n, per) : 1;
+}
+// The stretch of n tiles that a piece has.
 struct Share { int first, last, pieces; };
-__device__ __forceinline__ Share share_of(const Split& sp, int n, unsigned long long total, int heads, int least, int piece) {
-  if (sp.most == 1) return {0, n, 1};
-  const long long even = (long long)((total * heads * 3 + 2 * sp.slots - 1) / (2 * sp.slots));
-  int per = even > least ? (int)(even < n ? even : n) : least;
-  per = max(per, ceil_div_d(n, sp.most));
-  const int pieces = n > 2 * least ? ceil_div_d(n, per) : 1;
-  per = ceil_div_d(n, pieces);
+__device__ __forceinline__ Share share_of(int n, int pieces, int piece) {
+  const int per = ceil_div_d(n, pieces);
   return {uniform(min(piece * per, n)), uniform(min((piece + 1) * per, n)), uniform(pieces)};
 }
-constexpr int kLeastTiles = 4;
+__device__ __forceinline__ Share share_of(const Split& sp, int n, unsigned long long total, int piece) {
+  if (sp.most == 1) return {0, n, 1};
+  return share_of(n, uniform(min(pieces_of(n, sp.slots, total), sp.most)), piece);
+}
 
 struct AttnArgs {
   HeadTensor q, k, v, o;
@@ -66,17 +72,21 @@ struct RowFacts {
   int lo[kQueryTile], hi[kQueryTile], diag[kQueryTile];
 };
 
+struct Counts { int keys, cut_keys, queries, cut_queries; };
 struct AttnGrads {
   HeadTensor d_o, dq, dk, dv;
-  RowFacts* facts;        // workspace [heads][ceil(q_len / 128) * 2]
-  int q_blocks, k_blocks; // workgroups for dQ, for dK and dV, not counting pieces
-  Split k_split;
-  int4* k_order;          // workspace: tiles of keys, the ones with the most to do first: the tile, and the queries from y to before z that can see its keys
+  // in the workspace:
+  RowFacts* facts;        // [heads][ceil(q_len / 128) * 2]
+  int4 *k_list, *q_list;  // work, most first: tile, what it reaches from y to before z, pieces of it + 65536 * this piece; for every (key) head
+  Counts* counts;         // entries of both lists, and how many of them, all in front, are pieces of cut tiles
+  f32x4* sums;            // [pieces and heads of keys, then of queries][4 D / 32][256]
+  int more;               // entries that a list can hold beside its tiles
+  int slots;              // workgroups that the card holds at once; 0: nothing is cut
 };
 
 // Which head and tile a workgroup has, and what the tile reaches.  Workgroups go to the eight dies in turn: heads that share keys stay on one, whose
 // L2 cache then holds them once.  The tiles with the most to do come first.
-struct Place { int head, tile, lo, hi; };
+struct Place { int head, tile, lo, hi, piece; };
 __device__ __forceinline__ Place place_of(int n, int heads, const int4* order) {
   int head, rank;
   if (heads % 8 == 0) {
@@ -88,7 +98,7 @@ __device__ __forceinline__ Place place_of(int n, int heads, const int4* order) {
     rank = n / heads;
   }
   const int4 o = load_uniform(order + uniform(rank));
-  return {uniform(head), o.x, o.y, o.z};
+  return {uniform(head), o.x, o.y, o.z, o.w};
 }
 
 // The first tile of 64 keys (queries) at or behind c, before end, whose flag is set; two of them share a flag.
@@ -161,8 +171,8 @@ __device__ __forceinline__ void finish_rows(const AttnArgs& a, int head, int row
 }
 
 template <int D>
-__device__ __forceinline__ void leave_sums(const Split& sp, int64_t cell, const f32x16* acc) {
-  f32x4* to = sp.sums + cell * (D / 8 * 256) + threadIdx.x;
+__device__ __forceinline__ void leave_sums(f32x4* sums, int64_t cell, const f32x16* acc) {
+  f32x4* to = sums + cell * (D / 8 * 256) + threadIdx.x;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -170,8 +180,8 @@ __device__ __forceinline__ void leave_sums(const Split& sp, int64_t cell, const 
 }
 // Adds the 32 channels from c0 on of a piece.
 template <int D>
-__device__ __forceinline__ void add_sums(const Split& sp, int64_t cell, int c0, float by, f32x16& acc) {
-  const f32x4* from = sp.sums + cell * (D / 8 * 256) + c0 / 8 * 256 + threadIdx.x;
+__device__ __forceinline__ void add_sums(const f32x4* sums, int64_t cell, int c0, float by, f32x16& acc) {
+  const f32x4* from = sums + cell * (D / 8 * 256) + c0 / 8 * 256 + threadIdx.x;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const f32x4 x = from[r * 256];
@@ -211,7 +221,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
 
   const unsigned* flags = a.plan.seen_words ? a.plan.seen + (int64_t)qt * a.plan.seen_words : nullptr;
   const int begin = lo / kKeyTile;
-  const Share share = share_of(a.split, ceil_div_d(hi, kKeyTile) - begin, a.split.most > 1 ? load_uniform(a.plan.totals) : 0, a.heads, kLeastTiles, blockIdx.y);
+  const Share share = share_of(a.split, ceil_div_d(hi, kKeyTile) - begin, a.split.most > 1 ? load_uniform(a.plan.totals) * a.heads : 0, blockIdx.y);
   if ((int)blockIdx.y >= share.pieces) return;
   const int end = begin + share.last;
 
@@ -322,7 +332,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
   l = add_halves(l);
   if (share.pieces > 1) {
     const int64_t cell = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    leave_sums<D>(a.split, cell, acc);
+    leave_sums<D>(a.split.sums, cell, acc);
     if (half == 0) a.split.tops[cell * kPatTile + wave * kRowGroup + lane] = make_float2(m, l);
     return;
   }
@@ -333,7 +343,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
   const Place at = place_of(blockIdx.x, a.heads, a.plan.q_order);
-  const Share share = share_of(a.split, ceil_div_d(at.hi, kKeyTile) - at.lo / kKeyTile, load_uniform(a.plan.totals), a.heads, kLeastTiles, 0);
+  const Share share = share_of(a.split, ceil_div_d(at.hi, kKeyTile) - at.lo / kKeyTile, load_uniform(a.plan.totals) * a.heads, 0);
   if (share.pieces == 1) return;
   const int lane = lane_id(), row = threadIdx.x / kWave * kRowGroup + (lane & 31), c0 = blockIdx.y * 32;
   const float2* tops = a.split.tops + (int64_t)blockIdx.x * kPatTile + row;
@@ -348,7 +358,7 @@ __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
     const float2 top = tops[p * step];
     const float by = fast_exp2(top.x - base);
     l = __builtin_fmaf(top.y, by, l);
-    add_sums<D>(a.split, (int64_t)p * gridDim.x + blockIdx.x, c0, by, acc);
+    add_sums<D>(a.split.sums, (int64_t)p * gridDim.x + blockIdx.x, c0, by, acc);
   }
   finish_rows<T, 32>(a, at.head, at.tile * kPatTile + row, lane >> 5, c0, &acc, m, l);
 }

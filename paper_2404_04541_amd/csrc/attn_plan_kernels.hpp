@@ -130,11 +130,12 @@ __device__ __forceinline__ void order_by_work(int n, F reach, int4* order) {
     const int i = threadIdx.x;
     const int2 r = i < n ? reach(i) : make_int2(0, 0);
     const int mine = r.y - r.x;
-    kept[i] = mine;
+    kept[i] = i < n ? mine : -1;
     __syncthreads();
     int place = 0;
-    for (int k = 0; k < n; ++k) place += kept[k] > mine || (kept[k] == mine && k < i);
-    if (i < n) order[place] = make_int4(i, r.x, r.y, 0);
+#pragma unroll 16
+    for (int k = 0; k < ceil_div_d(n, 16) * 16; ++k) place += (kept[k] > mine) | ((kept[k] == mine) & (k < i));
+    if (i < n) order[place] = make_int4(i, r.x, r.y, 1);
     return;
   }
   auto work = [&](int i) { const int2 r = reach(i); return r.y - r.x; };
@@ -161,7 +162,7 @@ __device__ __forceinline__ void order_by_work(int n, F reach, int4* order) {
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += 256) {
     const int2 r = reach(i);
-    order[atomicAdd(&count[bucket(i)], 1u)] = make_int4(i, r.x, r.y, 0);
+    order[atomicAdd(&count[bucket(i)], 1u)] = make_int4(i, r.x, r.y, 1);
   }
 }
 
@@ -169,7 +170,7 @@ __device__ __forceinline__ void order_by_work(int n, F reach, int4* order) {
 // holds a few workgroups a compute unit, and long rows that begin late are waited for (two documents of 4000 tokens, tiles from the last row
 // backwards: 1.3 waves a SIMD on average where two fit).  Few tiles all run at once and need no order.  (Tiles of keys are ordered beside
 // k_attn_facts: here that would have to wait for all waves, and a forward pass does not need it; 4096 tokens 8.0 -> 6.7 us, by counting 5.2.)
-constexpr int kOrderQueries = 17, kOrderKeys = 48;
+constexpr int kOrderQueries = 17;
 __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanView p) {
   const int q_tiles = ceil_div_d(q_len, kPatTile), k_tiles = ceil_div_d(k_len, kKeyTile);
   if (blockIdx.x == gridDim.x - 1) {
@@ -178,7 +179,7 @@ __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanVie
     for (int i = threadIdx.x; i < q_tiles; i += 256) {
       const int2 r = reach(i);
       sum += key_tiles(r);
-      if (q_tiles < kOrderQueries) p.q_order[q_tiles - 1 - i] = make_int4(i, r.x, r.y, 0);
+      if (q_tiles < kOrderQueries) p.q_order[q_tiles - 1 - i] = make_int4(i, r.x, r.y, 1);
     }
     if (sum) atomicAdd(&p.totals[0], sum);
     if (q_tiles >= kOrderQueries) order_by_work(q_tiles, reach, p.q_order);
@@ -190,18 +191,6 @@ __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanVie
   if (lane_id() == 0) {
     p.cols[c] = r;
     atomicAdd(&p.totals[1], (unsigned long long)query_tiles(r));
-  }
-}
-
-// Tiles of keys in order of work, by a workgroup of 256 threads.
-__device__ __forceinline__ void order_key_tiles(const PlanView& p, int k_len, int4* order) {
-  const int n = ceil_div_d(k_len, kKeyTile);
-  auto reach = [&](int i) { return p.cols[i]; };
-  if (n >= kOrderKeys) {
-    order_by_work(n, reach, order);
-  } else if ((int)threadIdx.x < n) {
-    const int2 r = reach(threadIdx.x);
-    order[threadIdx.x] = make_int4(threadIdx.x, r.x, r.y, 0);
   }
 }
 
@@ -221,7 +210,7 @@ __global__ void __launch_bounds__(kSmallMask) k_plan_small(MaskView m, PlanView 
   if (i < q_tiles) {
     const int2 r = query_tile_reach(p, m.q_len, i);
     atomicAdd(&totals[0], key_tiles(r));
-    p.q_order[q_tiles - 1 - i] = make_int4(i, r.x, r.y, 0);
+    p.q_order[q_tiles - 1 - i] = make_int4(i, r.x, r.y, 1);
   }
   if (c < k_tiles) {
     const int2 r = key_tile_reach(p, m.q_len, m.k_len, c);
