@@ -7,8 +7,8 @@
 // the queries, of all heads that share them, of 64 keys.  That computes S and dP twice, seven products where five would do with atomics on dQ in 32 bits.
 // P, dS are rounded to 16 bits once, as operands; all sums are held in 32 bits.
 //
-// Measured (bfloat16, 128 channels, capped): two documents of 8192 tokens together, 16 heads on 8, 647 us, 0.75 PFLOP/s for the seven products (vector instructions issue in
-// 52 % of the cycles, matrix instructions run in 39 %, LDS in 31 %: as the forward kernel); eleven documents of 4096 tokens, 16 heads on 4, 82 us and 5.3 to join, where two launches, one after
+// Measured (bfloat16, 128 channels, capped): two documents of 8192 tokens together, 16 heads on 8, 631 us, 0.77 PFLOP/s for the seven products (vector instructions issue in
+// 54 % of the cycles, matrix instructions run in 41 %, LDS in 24 %: as the forward kernel); eleven documents of 4096 tokens, 16 heads on 4, 82 us and 5.3 to join, where two launches, one after
 // the other, took 126 and 8.6: the long chains of one kind fill the places that the other leaves.
 #pragma once
 #include "attn_forward.hpp"

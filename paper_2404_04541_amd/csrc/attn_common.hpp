@@ -111,15 +111,16 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
 // A tile of rows of D 16-bit elements in LDS, in chunks of 16 bytes.  A chunk's place in its row is exclusive-ored with bits of the row's
-// number, so that both ways in which tiles are read spread over all banks: 16 rows at one chunk (row operands) and eight rows at
-// 32 neighbouring bytes (reads across rows).  Rows of 256 bytes: chunk ^ 2 (r % 8) ^ (r / 8 % 2); of 128 bytes two rows share the banks.
+// number, so that both ways in which tiles are read spread over all banks: 16 rows at one chunk (row operands) and four rows at 64 neighbouring
+// bytes (reads across rows, half a wave at a time).  Rows of 256 bytes: chunk ^ 4 (r % 4) ^ (r / 4 % 4); of 128 bytes two rows share the banks.
+// (With reads across rows taken to be of eight rows and 32 bytes, each took twice as long: 8192 tokens, forward 203 -> 200 us, backward 641 -> 631.)
 template <int D>
 struct TileShape {
   static constexpr int kChunks = D / 8;
   static constexpr int kRowBytes = D * 2;
   __device__ static __forceinline__ int swizzle(int row) {
-    if constexpr (D == 128) return ((row & 7) << 1) ^ ((row >> 3) & 1);
-    else return (((row >> 1) & 3) << 1) ^ ((row >> 3) & 1);
+    if constexpr (D == 128) return ((row & 3) << 2) ^ ((row >> 2) & 3);
+    else return ((row & 2) << 1) ^ ((row >> 2) & 3);
   }
   // Where a lane reads, in bytes.  The bits of a chunk's number lie below a row's, so the chunks of a row are found by an exclusive or with
   // a constant, and rows that are a multiple of 16 away by a constant distance.
@@ -139,7 +140,7 @@ struct TileShape {
   __device__ static __forceinline__ vec8<T> across(const unsigned char* tile, int base, int r0, int i) {
     union { i16x4 part[2]; vec8<T> all; } u;
     u.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(tile + r0 * kRowBytes + (base ^ (64 * i))));
-    u.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(tile + (r0 + 8) * kRowBytes + (base ^ 16 ^ (64 * i))));   // (eight rows on, the swizzle's lowest bit differs)
+    u.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(tile + (r0 + 8) * kRowBytes + (base ^ 32 ^ (64 * i))));   // (eight rows on, bit 1 of the swizzle differs)
     return u.all;
   }
 };
