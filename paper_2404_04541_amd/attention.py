@@ -1,7 +1,7 @@
 """Thin Python binding of the C ABI in include/spattn.h (argument marshalling only), and one autograd function over it.
 
 Tensors of tokens are [tokens, heads, head_dim] with a contiguous last dimension; the other strides are the tensor's own.  Results come
-in fresh tensors.  Like everything in `binding`, nothing here computes: without the built library these calls raise.
+in fresh tensors, allocated on the handle's stream where it has one of its own; where another stream is current, ordering the two is the caller's.  Like everything in `binding`, nothing here computes: without the built library these calls raise.
 """
 from __future__ import annotations
 
@@ -93,6 +93,14 @@ def _like(t: torch.Tensor) -> torch.Tensor:
     return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
+def _results(handle: sg.Handle, make):
+    """make(), on the handle's stream, so that its memory goes to nobody else before the work is done."""
+    if handle.stream is None:
+        return make()
+    with torch.cuda.stream(handle.stream):
+        return make()
+
+
 def _result(t: torch.Tensor) -> TensorStruct:
     """A fresh contiguous tensor of this module's own."""
     strides = t.stride()
@@ -145,11 +153,8 @@ def symbolic(handle: sg.Handle, q_len: int, k_len: int, q_ptr: Optional[torch.Te
                             _array(colidx, "pattern colidx", torch.int32), None, 0)
         m.tiles = C.pointer(held)
     nbytes = lib.spattn_plan_bytes(C.byref(m))
-    if handle.stream is None and q_ptr is not None:
-        memory = q_ptr.new_empty(max(nbytes, 1), dtype=torch.uint8)
-    else:
-        with torch.cuda.stream(handle.stream) if handle.stream is not None else sg._nullctx():
-            memory = torch.empty(max(nbytes, 1), dtype=torch.uint8, device="cuda")
+    nbytes = max(nbytes, 1)
+    memory = _results(handle, lambda: torch.empty(nbytes, dtype=torch.uint8, device="cuda") if q_ptr is None else q_ptr.new_empty(nbytes, dtype=torch.uint8))
     checked = C.c_int32(0)
     handle._check(lib.spattn_symbolic(handle.ptr, C.byref(m), memory.data_ptr(), nbytes, C.byref(checked) if check else None))
     m.q_ptr = m.k_ptr = None          # (what follows needs the sizes only)
@@ -169,8 +174,7 @@ def forward(handle: sg.Handle, plan: Plan, q, k, v, scale: Optional[float] = Non
     """-> (o [q_len, heads, head_dim], lse float32 [heads, q_len]).  scale: 1 / sqrt(head_dim) unless given."""
     lib = _lib()
     a = _args(plan, q, k, v, scale, cap, slopes)
-    o = _like(q)
-    lse = q.new_empty((q.shape[1], plan.q_len), dtype=torch.float32)
+    o, lse = _results(handle, lambda: (_like(q), q.new_empty((q.shape[1], plan.q_len), dtype=torch.float32)))
     handle._check(lib.spattn_forward(handle.ptr, C.byref(a), _result(o), lse.data_ptr() or None))
     return o, lse
 
@@ -181,7 +185,7 @@ def backward(handle: sg.Handle, plan: Plan, q, k, v, o, lse, d_o, scale: Optiona
     a = _args(plan, q, k, v, scale, cap, slopes)
     if o.shape != q.shape or d_o.shape != q.shape:
         raise ValueError("o and d_o have q's shape")
-    dq, dk, dv = _like(q), _like(k), _like(v)
+    dq, dk, dv = _results(handle, lambda: (_like(q), _like(k), _like(v)))
     handle._check(lib.spattn_backward(handle.ptr, C.byref(a), _tensor(o, "o", plan.q_len, q), _array(lse, "lse", torch.float32, q.shape[1] * plan.q_len),
                                       _tensor(d_o, "d_o", plan.q_len, q), _result(dq), _result(dk), _result(dv)))
     return dq, dk, dv
@@ -267,7 +271,7 @@ def attend(handle: sg.Handle, cache: PagedCache, layer: int, table: PageTable, l
         raise ValueError("q: tokens of all sequences at one stride and a contiguous last dimension are wanted")
     if not q.is_cuda:
         raise ValueError("q: not on a GPU")
-    o = _like(q)
+    o = _results(handle, lambda: _like(q))
     rows = TensorStruct(q.data_ptr() or None, (per_sequence if q_len == 1 else per_token) if n * q_len > 1 else 0, per_head if heads > 1 else 0)
     handle._check(lib.spcache_attend(handle.ptr, C.byref(cache._struct), int(layer), C.byref(table.struct(cache)), _array(lens, "lens", torch.int32, n), q_len, heads,
                                      _dtype(q), 1.0 / math.sqrt(d) if scale is None else float(scale), float(cap), _slopes(slopes, heads), int(window),
@@ -285,9 +289,8 @@ def fork(handle: sg.Handle, cache: PagedCache, table: PageTable, lens: torch.Ten
     n = parent.numel()
     if entries is None:
         entries = int(((new_lens.clamp(min=0).to(torch.int64) + PAGE - 1) // PAGE).sum())
-    rowptr = parent.new_empty(n + 1, dtype=torch.int64)
-    pages = parent.new_empty(int(entries), dtype=torch.int32)
-    refs = parent.new_empty(cache.pages, dtype=torch.int32)
+    rowptr, pages, refs = _results(handle, lambda: (parent.new_empty(n + 1, dtype=torch.int64), parent.new_empty(int(entries), dtype=torch.int32),
+                                                    parent.new_empty(cache.pages, dtype=torch.int32)))
     nnz = C.c_int64(0)
     handle._check(lib.spcache_fork(handle.ptr, C.byref(cache._struct), C.byref(table.struct(cache)), _array(lens, "lens", torch.int32, table.rows), n,
                                    _array(parent, "parent", torch.int32), _array(new_lens, "new_lens", torch.int32, n), rowptr.data_ptr(),
@@ -298,7 +301,7 @@ def fork(handle: sg.Handle, cache: PagedCache, table: PageTable, lens: torch.Ten
 def compact(handle: sg.Handle, cache: PagedCache, table: PageTable, check: bool = True):
     """The pages in use to the front of the cache -> (PageTable, how many pages are in use; None without check)."""
     lib = _lib()
-    pages = torch.empty_like(table.pages)
+    pages = _results(handle, lambda: _like(table.pages))
     live = C.c_int64(0)
     handle._check(lib.spcache_compact(handle.ptr, C.byref(cache._struct), C.byref(table.struct(cache)), pages.data_ptr() if pages.numel() else None,
                                       C.byref(live) if check else None))

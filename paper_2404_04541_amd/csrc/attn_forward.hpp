@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
       for (int i = 0; i < D / 16; ++i) s[t] = mma(S::template row<T>(kt, row_base, 32 * t, i), q[i], s[t]);
     }
     // Where every key of a tile is at or before every row, a distance is a row's part less a key's: the key's goes into the product's scaling, the row's
-    // into the exponent, and an entry costs two operations less (5003 queries through a pattern: 174 -> 169.5 us then).
+    // into the exponent, and an entry costs two operations less (5003 queries through a pattern: 174 -> 169.5 us).
     float row_part[kKeyTile / 32] = {};
     if (BIAS && !CAP && whole && k0 + kKeyTile - 1 <= least_diag) {
 #pragma unroll

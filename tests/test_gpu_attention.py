@@ -258,6 +258,22 @@ def test_stream_of_its_own():
     stream.synchronize()
 
 
+def test_results_belong_to_the_stream():
+    """With another stream current, a result that is dropped at once is not the next tensor of that stream: the work may still be writing it."""
+    handle = sg.Handle(stream=torch.cuda.Stream())
+    q, k, v, d_o = tensors(14, BF, 300, 300, 4, 4, 64)
+    q_ptr = ints([0, 300])
+    torch.cuda.synchronize()
+    plan = at.symbolic(handle, 300, 300, q_ptr=q_ptr, k_ptr=q_ptr)
+    o, lse = at.forward(handle, plan, q, k, v)
+    grads = at.backward(handle, plan, q, k, v, o, lse, d_o)
+    handle.stream.synchronize()
+    mine = {t.data_ptr() for t in (plan.memory, o, lse, *grads)}
+    sizes = [t.numel() * t.element_size() for t in (plan.memory, o, lse, *grads)]
+    del plan, o, lse, grads
+    assert not mine & {t.data_ptr() for t in [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]}
+
+
 def test_graph(h):
     """Captured once, replayed on new inputs with the program's own work between: every replay is the eager result."""
     stream = torch.cuda.Stream()
