@@ -7,7 +7,7 @@
 // the queries, of all heads that share them, of 64 keys.  That computes S and dP twice, seven products where five would do with atomics on dQ in 32 bits.
 // P, dS are rounded to 16 bits once, as operands; all sums are held in 32 bits.
 //
-// Measured (bfloat16, 128 channels, capped): two documents of 8192 tokens together, 16 heads on 8, 631 us, 0.77 PFLOP/s for the seven products (vector instructions issue in
+// Measured (bfloat16, 128 channels, capped): two documents of 8192 tokens together, 16 heads on 8, 631 us, 0.77 PFLOP/s for the seven products (call after call without a trace 567 with the rows' sums; vector instructions issue in
 // 54 % of the cycles, matrix instructions run in 41 %, LDS in 24 %: as the forward kernel); eleven documents of 4096 tokens, 16 heads on 4, 82 us and 5.3 to join, where two launches, one after
 // the other, took 126 and 8.6: the long chains of one kind fill the places that the other leaves.
 #pragma once
@@ -147,9 +147,10 @@ __device__ __forceinline__ void dq_tile(unsigned char* lds, int n) {
     for (int t = 0; t < 2; ++t) {
       f32x16 s = {}, dp = {};
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) s = mma(S::template row<T>(kt, at_row, 32 * t, i), q[i], s);
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) dp = mma(S::template row<T>(vt, at_row, 32 * t, i), d_o[i], dp);
+      for (int i = 0; i < D / 16; ++i) {
+        s = mma(S::template row<T>(kt, at_row, 32 * t, i), q[i], s);
+        dp = mma(S::template row<T>(vt, at_row, 32 * t, i), d_o[i], dp);
+      }
       const float away = (float)(rb.diag - k0 - 4 * half - 32 * t);
       const unsigned span = rb.hi > rb.lo ? rb.hi - rb.lo : 0;
       const int off = k0 + 4 * half + 32 * t - rb.lo;

@@ -7,8 +7,8 @@
 // maximum m; sums and maxima in 32 bits, probabilities rounded to 16 bits once, as an operand.  The accumulators are brought to a
 // new maximum only where some row's grew by more than 2^8 since (the sum is in the same units, so nothing is approximated).
 //
-// Measured (bfloat16, 128 channels): two documents of 8192 tokens together, 16 heads on 8, capped, 200 us, 0.69 PFLOP/s; 5003 queries over 11 147 keys through a
-// pattern, 32 heads on 8, with distances, 166 us, 0.67.  Vector instructions issue in 57 % of the cycles (50 in the second), eight an entry with a cap,
+// Measured (bfloat16, 128 channels): two documents of 8192 tokens together, 16 heads on 8, capped, 200 us, 0.69 PFLOP/s (call after call without a trace 176, 0.78); 5003 queries over 11 147 keys through a
+// pattern, 32 heads on 8, with distances, 166 us, 0.67 (144, 0.78).  Vector instructions issue in 57 % of the cycles (50 in the second), eight an entry with a cap,
 // three of them powers and reciprocals; matrix instructions run in 38 % (39), LDS in 19 %: what vector and matrix instructions take
 // together bounds it, for two waves a SIMD, as many as the registers allow, hardly overlap.  Tiles of 32 keys for three waves, products of the next tile beside
 // the powers of this one (in the order of the code or by hints to the scheduler) and priorities were all slower.  Short rows (documents of a few
@@ -242,10 +242,11 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
     const bool whole = mine.all_lo <= k0 && mine.all_hi >= k0 + kKeyTile;
     f32x16 s[kKeyTile / 32];
 #pragma unroll
-    for (int t = 0; t < kKeyTile / 32; ++t) {
-      s[t] = f32x16{};
+    for (int t = 0; t < kKeyTile / 32; ++t) s[t] = f32x16{};
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) s[t] = mma(S::template row<T>(kt, row_base, 32 * t, i), q[i], s[t]);
+    for (int j = 0; j < kKeyTile / 32 * (D / 16); ++j) {   // (both halves in turn where a cap follows, 8192 tokens 176 us, one after the other 180; without one 146 | 144)
+      const int t = CAP ? j % 2 : j / (D / 16), i = CAP ? j / 2 : j % (D / 16);
+      s[t] = mma(S::template row<T>(kt, row_base, 32 * t, i), q[i], s[t]);
     }
     // Where every key of a tile is at or before every row, a distance is a row's part less a key's: the key's goes into the product's scaling, the row's
     // into the exponent, and an entry costs two operations less (5003 queries through a pattern: 174 -> 169.5 us).
