@@ -305,14 +305,14 @@ int spattn_symbolic(spgemm_handle h, const spattn_mask* mask, void* plan_mem, si
     m.window = (int)(mask->window < kMaxTokens ? mask->window : 0);   // (a window of 2^30 hides nothing)
     m.q_ptr = mask->q_ptr; m.k_ptr = mask->k_ptr; m.prefix = mask->prefix;
     if (mask->tiles) { m.pat_ptr = mask->tiles->rowptr; m.pat_col = mask->tiles->colidx; m.pat_nnz = mask->tiles->nnz; }
+    const int64_t flag_blocks = mask->tiles ? ceil_div(ceil_div(mask->q_len, kPatTile), 4) : 0;
     if (mask->q_len <= kSmallMask && mask->k_len <= kSmallMask) {
       k_plan_small<<<dim3(1), dim3(kSmallMask), 0, h->stream>>>(m, p);
+      if (flag_blocks) k_plan_pattern<<<dim3((unsigned)flag_blocks), dim3(256), 0, h->stream>>>(m, p);
     } else {
       k_plan_rows<<<dim3((unsigned)ceil_div(mask->q_len > 0 ? mask->q_len : 1, 256)), dim3(256), 0, h->stream>>>(m, p);
-      k_plan_cols<<<dim3((unsigned)(ceil_div(ceil_div(mask->k_len, kKeyTile), 4) + 1)), dim3(256), 0, h->stream>>>(m.q_len, m.k_len, p);
+      k_plan_cols<<<dim3((unsigned)(ceil_div(ceil_div(mask->k_len, kKeyTile), 4) + flag_blocks + 1)), dim3(256), 0, h->stream>>>(m, p);
     }
-    if (mask->tiles && mask->q_len > 0)
-      k_plan_pattern<<<dim3((unsigned)ceil_div(ceil_div(mask->q_len, kPatTile), 4)), dim3(256), 0, h->stream>>>(m, p);
     if ((rc = launched(h))) return rc;
     if (!checked) return SPGEMM_OK;
     int32_t error = 0;

@@ -1,6 +1,6 @@
 // The structure of a mask: bounds of its rows, of groups of rows and of columns, and a pattern's flags.  Bandwidth does not matter here (28 bytes a row);
-// what a plan costs is its launches: two, or one where the mask is small, and one more with a pattern.  us: 257 tokens 4.3; 4096 in eleven documents
-// 4.7 + 5; 8192 4.8 + 7; 5003 queries over 11 147 keys 4.9 + 6.4, and 4.8 for their pattern.
+// what a plan costs is its launches: two, or one where the mask is small (and then one more for a pattern).  us: 257 tokens 4.3; 4096 in eleven documents
+// 4.7 + 5; 8192 4.8 + 7; 5003 queries over 11 147 keys with a pattern 4.9 + 6.6 (its flags in a launch of their own: 4.8 more).
 #pragma once
 #include "attn_common.hpp"
 
@@ -166,12 +166,32 @@ __device__ __forceinline__ void order_by_work(int n, F reach, int4* order) {
   }
 }
 
+// The pattern's flags, a wave a row of tiles r.  Bits are only set, so neither the order of a row's columns nor repeated ones matter.
+__device__ __forceinline__ void set_flags(const MaskView& m, const PlanView& p, int r) {
+  const int rows = ceil_div_d(m.q_len, kPatTile), cols = ceil_div_d(m.k_len, kPatTile);
+  if (r >= rows) return;
+  const int64_t a = m.pat_ptr[r], b = m.pat_ptr[r + 1];
+  if (a < 0 || b < a || b > m.pat_nnz) {
+    if (lane_id() == 0) *p.error = 1;
+    return;
+  }
+  for (int64_t e = a + lane_id(); e < b; e += kWave) {
+    const int c = m.pat_col[e];
+    if (c < 0 || c >= cols) { *p.error = 1; continue; }
+    atomicOr(&p.seen[(int64_t)r * p.seen_words + c / 32], 1u << (c % 32));
+    atomicOr(&p.seen_by[(int64_t)c * p.seen_by_words + r / 32], 1u << (r % 32));
+  }
+}
+__global__ void __launch_bounds__(256) k_plan_pattern(MaskView m, PlanView p) { set_flags(m, p, blockIdx.x * 4 + threadIdx.x / kWave); }
+
 // What both kinds of tiles reach, a wave a tile of keys; those of queries by a workgroup of its own, which also brings them into order of work: the card
 // holds a few workgroups a compute unit, and long rows that begin late are waited for (two documents of 4000 tokens, tiles from the last row
 // backwards: 1.3 waves a SIMD on average where two fit).  Few tiles all run at once and need no order.  (Tiles of keys are ordered beside
 // k_attn_facts: here that would have to wait for all waves, and a forward pass does not need it; 4096 tokens 8.0 -> 6.7 us, by counting 5.2.)
+// Workgroups behind those of the keys set a pattern's flags.
 constexpr int kOrderQueries = 17;
-__global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanView p) {
+__global__ void __launch_bounds__(256) k_plan_cols(MaskView m, PlanView p) {
+  const int q_len = m.q_len, k_len = m.k_len;
   const int q_tiles = ceil_div_d(q_len, kPatTile), k_tiles = ceil_div_d(k_len, kKeyTile);
   if (blockIdx.x == gridDim.x - 1) {
     auto reach = [&](int i) { return query_tile_reach(p, q_len, i); };
@@ -185,7 +205,8 @@ __global__ void __launch_bounds__(256) k_plan_cols(int q_len, int k_len, PlanVie
     if (q_tiles >= kOrderQueries) order_by_work(q_tiles, reach, p.q_order);
     return;
   }
-  const int c = blockIdx.x * 4 + threadIdx.x / kWave;
+  const int c = blockIdx.x * 4 + threadIdx.x / kWave, behind = c - ceil_div_d(k_tiles, 4) * 4;
+  if (behind >= 0) set_flags(m, p, behind);
   if (c >= k_tiles) return;
   const int2 r = key_tile_reach(p, q_len, k_len, c);
   if (lane_id() == 0) {
@@ -221,24 +242,6 @@ __global__ void __launch_bounds__(kSmallMask) k_plan_small(MaskView m, PlanView 
   }
   __syncthreads();
   if (threadIdx.x < 2) p.totals[threadIdx.x] = totals[threadIdx.x];
-}
-
-// The pattern's flags, a wave a row of tiles.  Bits are only set, so neither the order of a row's columns nor repeated ones matter.
-__global__ void __launch_bounds__(256) k_plan_pattern(MaskView m, PlanView p) {
-  const int rows = ceil_div_d(m.q_len, kPatTile), cols = ceil_div_d(m.k_len, kPatTile);
-  const int r = blockIdx.x * 4 + threadIdx.x / kWave;
-  if (r >= rows) return;
-  const int64_t a = m.pat_ptr[r], b = m.pat_ptr[r + 1];
-  if (a < 0 || b < a || b > m.pat_nnz) {
-    if (lane_id() == 0) *p.error = 1;
-    return;
-  }
-  for (int64_t e = a + lane_id(); e < b; e += kWave) {
-    const int c = m.pat_col[e];
-    if (c < 0 || c >= cols) { *p.error = 1; continue; }
-    atomicOr(&p.seen[(int64_t)r * p.seen_words + c / 32], 1u << (c % 32));
-    atomicOr(&p.seen_by[(int64_t)c * p.seen_by_words + r / 32], 1u << (r % 32));
-  }
 }
 
 }  // namespace spg

@@ -315,6 +315,16 @@ def test_documents_are_checked(h):
         assert e.value.status == -8
 
 
+def test_a_large_pattern_is_checked(h):
+    """Beyond 1024 tokens, where a plan's launches are others: 9 x 9 tiles."""
+    rows = list(range(10))
+    at.symbolic(h, 1100, 1100, tiles=(ints(rows), ints([8, 0, 1, 2, 3, 4, 5, 6, 7], torch.int32)))
+    for ptr, cols in ((rows, [0, 1, 2, 3, 9, 5, 6, 7, 8]), (rows, [0, 1, 2, 3, 4, 5, 6, 7, -1]), (rows[:-1] + [10], list(range(9))), ([0, 2, 1] + rows[3:], list(range(9)))):
+        with pytest.raises(sg.SpgemmError) as e:
+            at.symbolic(h, 1100, 1100, tiles=(ints(ptr), ints(cols, torch.int32)))
+        assert e.value.status == -8
+
+
 def test_unchecked_documents_are_cut(h):
     """Pointers that leave the tensors, not looked at by the host: every access stays inside, rows see what exists."""
     q, k, v, _ = tensors(19, BF, 100, 100, 1, 1, 64)
