@@ -69,18 +69,11 @@ __device__ __forceinline__ float fast_rcp(float x) { return __builtin_amdgcn_rcp
 // tanh(x), given x * 2 log2(e): 1 - 2 / (exp(2x) + 1).  Off by at most about 2e-7 in absolute terms, which is what a capped score needs.
 __device__ __forceinline__ float tanh_of(float x2) { return 1.0f - 2.0f * fast_rcp(fast_exp2(x2) + 1.0f); }
 
-// The largest and the smallest of three, as one instruction each (fmaxf and fminf first bring what might be a signalling NaN into order); NaN is
-// passed over.
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
-__device__ __forceinline__ float min3(float a, float b, float c) {
-  float r;
-  asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
+// The largest and the smallest of three, as one instruction each; NaN comes through (a row with a score of NaN has no other result).  By builtins, for the
+// compiler places the waits behind a matrix instruction, whose results arrive cycles later, only in front of instructions that it knows: between
+// the last product and an instruction in inline assembly there was none.  (fmaxf and fminf would first bring what might be a signalling NaN into order.)
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
+__device__ __forceinline__ float min3(float a, float b, float c) { return __builtin_elementwise_minimum(__builtin_elementwise_minimum(a, b), c); }
 
 // A value that all lanes have, in a scalar register: descriptors and addresses that depend on it then need no loop over the lanes.
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }

@@ -206,6 +206,24 @@ def test_large_scores(h):
     assert torch.isfinite(o).all() and torch.allclose(lse.double(), torch.logsumexp(best, -1), rtol=1e-5)
 
 
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("peak", [63, 60, 31, 4])
+def test_maxima_that_rise_with_every_tile(h, dtype, d, peak):
+    """Of every whole tile of 64 keys one, at its end or elsewhere, has a score that is 32 above the one of the tile before: with that maximum a power would be 2^46."""
+    q, k, v, d_o = tensors(27, dtype, 160, 576, 2, 1, d)
+    q *= 0.5
+    k *= 0.5
+    q[:, :, 0], k[:, :, 0] = 8, 0
+    for tile in range(9):
+        k[64 * tile + peak, :, 0] = 4 * tile
+    x = (q, k, v, d_o)
+    first = run(h, *x, {"causal": False}, scale=1.0)
+    for _ in range(3):
+        again = run(h, *x, {"causal": False}, scale=1.0)
+        assert all(torch.equal(first[n], again[n]) for n in first)
+
+
 def test_gradients_against_differences(h):
     """Central differences of the definition in 64 bits, at entries all over the tensors."""
     mask, cap, scale = {"q_ptr": [0, 20, 50], "k_ptr": [0, 25, 60], "window": 30}, 8.0, 0.4
