@@ -127,7 +127,8 @@ int spcache_attend(spgemm_handle h, const spcache* c, int64_t layer, const spgem
  *   parent, new_lens: device, n_out.  out_rowptr: device, n_out + 1; out_pages: device, room entries; refs: device, pages: how often
  *   the new table has each page.  Outputs must not overlap inputs.
  *   nnz_out: host, or null.  Given, the call waits and SPGEMM_INVALID_INPUT (a parent or page out of range, a parent without its pages, room too
- *   small) and SPGEMM_ALLOC_FAILED (no page left) are reported; without it such a call leaves the cache as it is and the outputs unspecified. */
+ *   small) and SPGEMM_ALLOC_FAILED (no page left, or a row longer than the whole cache) are reported; without it such a call leaves the cache as it is and the
+ *   outputs unspecified. */
 int spcache_fork(spgemm_handle h, const spcache* c, const spgemm_csr* table, const int32_t* lens, int64_t n_out, const int32_t* parent,
                  const int32_t* new_lens, int64_t* out_rowptr, int32_t* out_pages, int64_t room, int32_t* refs, int64_t* nnz_out);
 

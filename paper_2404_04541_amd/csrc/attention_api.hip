@@ -13,11 +13,12 @@
 
 using namespace spg;
 
+static_assert(kPage == SPCACHE_PAGE, "the header's page");
+
 namespace {
 
 constexpr int64_t kMaxTokens = int64_t(1) << 30;
 constexpr int64_t kMaxStride = int64_t(1) << 23;    // elements: 128 rows stay within 31 bits of bytes
-constexpr int64_t kMaxPages = int64_t(1) << 24;     // 64 rows' pages are added up in 32 bits
 
 // Nothing leaves a C entry but a status: an exception (a string that finds no memory) becomes one.
 template <typename F>
@@ -519,7 +520,7 @@ int spcache_fork(spgemm_handle h, const spcache* c, const spgemm_csr* table, con
     if ((rc = copy_and_report(h, g, n_out, nnz_out ? &out : nullptr))) return rc;
     if (!nnz_out) return SPGEMM_OK;
     *nnz_out = out.nnz;
-    if (out.error == 2) return fail(h, SPGEMM_ALLOC_FAILED, "the cache has no page left");
+    if (out.error == kForkPages) return fail(h, SPGEMM_ALLOC_FAILED, "the cache has no page left");
     return out.error ? fail(h, SPGEMM_INVALID_INPUT, "a parent, length or page out of range, or too little room for the table") : SPGEMM_OK;
   });
 }

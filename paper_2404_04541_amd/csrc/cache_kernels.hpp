@@ -7,10 +7,10 @@
 // the 16 neighbouring keys whose 16 bytes of a value's channel are one load, and nothing moves between lanes.  Pages go from memory to registers.
 #pragma once
 #include "attn_forward.hpp"
+#include "page_need.hpp"
 
 namespace spg {
 
-constexpr int kPage = 64;
 constexpr int kRows = 16;             // query rows of a workgroup
 constexpr float kMost8 = 448.0f;      // the largest e4m3 value
 

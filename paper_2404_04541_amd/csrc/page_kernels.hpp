@@ -42,20 +42,23 @@ struct ForkArgs {
   PageMoves* out;
 };
 
-// What row r keeps of its parent: tokens, their pages, where those are in the last table.
-struct Kept { int64_t tokens, at; int pages, need; bool ok; };
+// What row r keeps of its parent: tokens, their pages, where those are in the last table; and how many pages it needs.  error: kForkInput, or
+// kForkPages for a row longer than the cache.
+constexpr int kForkInput = 1, kForkPages = 2;
+struct Kept { int64_t tokens, at; int pages, need, error; };
 __device__ __forceinline__ Kept kept_of(const ForkArgs& a, int r) {
   const int p = a.parent[r];
   const int64_t len = a.new_lens[r];
-  Kept k{0, 0, 0, 0, p >= -1 && p < a.t.seqs && len >= 0};
-  if (!k.ok) return k;
-  k.need = (int)((len + kPage - 1) / kPage);
+  Kept k{0, 0, 0, 0, p >= -1 && p < a.t.seqs && len >= 0 ? 0 : kForkInput};
+  if (k.error) return k;
+  k.need = page_need(len, a.pages);
+  if (k.need < 0) { k.need = 0; k.error = kForkPages; return k; }
   if (p >= 0) {
     const int64_t had = a.t.lens[p], b = a.t.ptr[p], e = a.t.ptr[p + 1];
     k.tokens = had < len ? had : len;
     k.at = b;
     k.pages = k.tokens > 0 ? (int)((k.tokens + kPage - 1) / kPage) : 0;
-    if (had < 0 || b < 0 || e < b || e > a.t.nnz || k.pages > e - b) { k.ok = false; k.pages = 0; k.tokens = 0; }
+    if (had < 0 || b < 0 || e < b || e > a.t.nnz || k.pages > e - b) { k.error = kForkInput; k.pages = 0; k.tokens = 0; }
   }
   return k;
 }
@@ -92,14 +95,14 @@ __device__ __forceinline__ void fork_rows(const ForkArgs& a) {
       a.rows,
       [&](int64_t r) {
         const Kept k = kept_of(a, (int)r);
-        if (!k.ok) bad = 1;
+        if (k.error) atomicOr(&bad, k.error);
         return k.need;
       },
       [&](int64_t r, int64_t sum) { a.ptr[r] = sum; });
   __syncthreads();
   if (threadIdx.x == 0) {
     a.ptr[a.rows] = nnz;
-    *a.out = PageMoves{bad || nnz > a.room ? 1 : 0, 0u, nnz, 0};
+    *a.out = PageMoves{bad & kForkInput || nnz > a.room ? kForkInput : bad, 0u, nnz, 0};
   }
 }
 
@@ -116,7 +119,7 @@ __device__ __forceinline__ void fork_gather(const ForkArgs& a, int r) {
   const int64_t to = a.ptr[r];
   for (int j = lane_id(); j < k.pages; j += kWave) {
     const int p = a.t.page[k.at + j];
-    if (p < 0 || p >= a.pages) { a.out->error = 1; continue; }
+    if (p < 0 || p >= a.pages) { a.out->error = kForkInput; continue; }
     a.page[to + j] = p;
     atomicAdd(&a.refs[p], 1);
     atomicMin(&a.owner[p], (int64_t)(j + 1) * kPage > k.tokens ? r : -1);
@@ -186,7 +189,7 @@ __device__ __forceinline__ void fork_assign(const ForkArgs& a, int r) {
   const int64_t to = a.ptr[r], rank = a.fresh[r];
   for (int j = lane_id(); j < k.need - k.pages + copy; j += kWave) {
     const int64_t p = free_page(a.used, rank + j);
-    if (p < 0) { a.out->error = 2; continue; }
+    if (p < 0) { a.out->error = kForkPages; continue; }
     const int at = k.pages - copy + j;
     if (copy && j == 0) {
       const int old = a.t.page[k.at + at];

@@ -1,4 +1,5 @@
 """The 8-bit paged cache: what an append leaves in it (bit for bit), attention over it against 64 bits, page tables and their copies."""
+import ctypes as C
 import math
 import random
 
@@ -333,6 +334,33 @@ def test_fork_refusals(h):
         assert torch.equal(a, b)
     out, refs = at.fork(h, cache, table, i32(lens), i32([]), i32([]))              # every row ends
     assert out.rows == 0 and not refs.any()
+
+
+def test_fork_of_lengths_beyond_the_cache(h):
+    """Lengths near 2^31 in enough rows that their pages would pass 32 bits: refused, and nothing written, whatever room the table has."""
+    cache = filled(32, 1, 6, 1, 64)
+    before = clone(cache)
+    table, lens = at.PageTable(*flat([[0, 1], [2]])), i32([100, 64])
+    most = 2 ** 31 - 1
+    for rows in (1, 63, 64, 65, 1100):
+        guard = torch.full((rows + 4096,), -7, dtype=torch.int32, device="cuda")
+        rowptr, refs = torch.empty(rows + 1, dtype=torch.int64, device="cuda"), torch.empty(6, dtype=torch.int32, device="cuda")
+        new_lens, out = i32([most] * rows), guard[4096:]
+        for parent in (-1, 0):
+            parents = i32([parent] * rows)
+            for room in (0, 3, 8):
+                nnz = C.c_int64(0)
+                status = at._lib().spcache_fork(h.ptr, C.byref(cache._struct), C.byref(table.struct(cache)), lens.data_ptr(), rows, parents.data_ptr(), new_lens.data_ptr(),
+                                                rowptr.data_ptr(), out.data_ptr(), min(room, rows), refs.data_ptr(), C.byref(nnz))
+                assert status == -5, (rows, parent, room)
+                assert (guard == -7).all()
+    with pytest.raises(sg.SpgemmError) as e:                                        # a length that the cache could hold, and one that it could not
+        at.fork(h, cache, table, lens, i32([0, -1]), i32([100, most]), entries=2)
+    assert e.value.status == -5
+    with pytest.raises(sg.SpgemmError) as e:                                        # ... and a parent that there is not
+        at.fork(h, cache, table, lens, i32([5, -1]), i32([100, most]), entries=2)
+    assert e.value.status == -8
+    assert torch.equal(cache.k, before.k) and torch.equal(cache.v, before.v)
 
 
 @pytest.mark.parametrize("seed", range(6))
