@@ -12,8 +12,11 @@
  *     head_stride (strides in elements).  Base and strides must be multiples of 16 bytes, a token stride below 2^23 elements.
  *   - head_dim is a multiple of 8 from 8 to 128.
  *   - A call only enqueues work on the handle's stream, unless it is given a host pointer for its result: then it waits for the stream.
- *   - Scratch memory comes from the handle's allocator, grows with the largest call and stays with the handle.  (A call that needs more than
- *     any before waits for the stream; a graph is captured after a call of its size.)
+ *   - Scratch memory comes from the handle's allocator, grows with the largest call and stays with the handle.  A call that needs more than
+ *     any before waits for the stream, so a graph is best captured after a call of its size.  What a captured call uses stays where it is until
+ *     spgemm_destroy, whatever calls follow: a graph may be replayed for as long as the handle that it was captured with lives.  All calls and graphs of a
+ *     handle share the scratch memory, so no two of them run at the same time: they go to the handle's stream, or are ordered by the caller.
+ *   - spgemm_destroy waits for the handle's stream where such calls were made: the stream has to exist still, and no capture be under way.
  *   - Sums, maxima and logarithms are held in 32 bits; probabilities and their gradients are rounded to the 16-bit type where they
  *     become an operand of a matrix instruction.  The same inputs give the same bits.
  */

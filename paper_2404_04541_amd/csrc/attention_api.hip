@@ -36,20 +36,32 @@ int launched(spgemm_context* h) {
   return SPGEMM_OK;
 }
 
-// The handle's scratch memory, at least so many bytes: grown where a call needs more than any before it.
+// The handle's scratch memory, at least so many bytes: grown where a call needs more than any before it.  A captured call leaves the block's address in the
+// graph, whose replays use it for as long as the handle lives; so a block that was captured, or is outgrown while a capture goes on (which cannot wait for the
+// stream), stays, and the next is at least twice as large, so that all that stay together are smaller than the last.  Any other is released.
 int scratch(spgemm_context* h, size_t bytes, void** out) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(h->stream, &status) != hipSuccess) (void)hipGetLastError();
+  const bool captures = status != hipStreamCaptureStatusNone;
   if (bytes > h->work_bytes) {
-    if (h->work) {
+    size_t want = bytes;
+    if (h->work && (h->work_captured || captures)) {
+      want = bytes > 2 * h->work_bytes ? bytes : 2 * h->work_bytes;
+      h->outgrown.push_back(h->work);
+    } else if (h->work) {
       HIP_TRY(h, hipStreamSynchronize(h->stream));
       dev_free(h, h->work);
-      h->work = nullptr;
-      h->work_bytes = 0;
     }
-    void* p = dev_alloc(h, bytes);
+    h->work = nullptr;
+    h->work_bytes = 0;
+    h->work_captured = false;
+    void* p = dev_alloc(h, want);
+    if (!p && want > bytes) p = dev_alloc(h, want = bytes);
     if (!p) return fail(h, SPGEMM_ALLOC_FAILED, "scratch memory");
     h->work = p;
-    h->work_bytes = bytes;
+    h->work_bytes = want;
   }
+  h->work_captured |= captures;
   *out = h->work;
   return SPGEMM_OK;
 }

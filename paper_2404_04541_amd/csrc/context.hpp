@@ -40,6 +40,8 @@ struct spgemm_context {
   int second_device = -1;
   void* work = nullptr;           // scratch memory of the attention and cache calls, of the largest one so far
   size_t work_bytes = 0;
+  bool work_captured = false;     // a graph has it in its nodes
+  std::vector<void*> outgrown;    // blocks that graphs still have, after a larger call: released with the handle
 };
 
 namespace spg {

@@ -922,9 +922,10 @@ int spgemm_destroy(spgemm_handle h) {
   for (auto e : h->event_pool) (void)hipEventDestroy(e);
   for (auto& t : h->timed) { (void)hipEventDestroy(t.start); (void)hipEventDestroy(t.stop); }
   if (h->second) (void)hipStreamDestroy(h->second);
-  if (h->work) {
+  if (h->work || !h->outgrown.empty()) {
     (void)hipStreamSynchronize(h->stream);   // (kernels that use it may be on their way)
     dev_free(h, h->work);
+    for (void* p : h->outgrown) dev_free(h, p);
   }
   delete h;
   return SPGEMM_OK;

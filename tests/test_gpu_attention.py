@@ -323,6 +323,63 @@ def test_graph(h):
         assert all(torch.equal(a, b) for a, b in zip(out, want)), seed
 
 
+def test_graph_after_a_larger_call():
+    """A graph keeps its scratch memory when a later call on the handle needs more: a replay gives the eager result, and writes nothing that belongs to others."""
+    stream = torch.cuda.Stream()
+    handle, other = sg.Handle(stream=stream), sg.Handle(stream=stream)
+    q_ptr, large_ptr = ints([0, 100, 260]), ints([0, 3000])
+    x = list(tensors(31, BF, 260, 260, 4, 2, 64))
+    large = tensors(32, BF, 3000, 3000, 4, 2, 64)
+
+    def step(which, x, ptr):
+        n = x[0].shape[0]
+        plan = at.symbolic(which, n, n, q_ptr=ptr, k_ptr=ptr, check=False)
+        o, lse = at.forward(which, plan, *x[:3])
+        return (o, lse) + at.backward(which, plan, *x[:3], o, lse, x[3])
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        step(handle, x, q_ptr)
+    stream.synchronize()
+    before = dict(handle._live)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        out = step(handle, x, q_ptr)
+    sizes = [t.numel() for t in handle._live.values()]
+    with torch.cuda.stream(stream):
+        first = step(handle, large, large_ptr)
+        assert all(p in handle._live for p in before)                          # kept, and a block of at least twice the size beside it
+        assert len(handle._live) == len(before) + 1 and max(t.numel() for t in handle._live.values()) >= 2 * max(sizes)
+        others = [torch.full((n,), 77, dtype=torch.uint8, device="cuda") for n in sizes * 8]
+    for seed in range(33, 36):
+        for t, new in zip(x, tensors(seed, BF, 260, 260, 4, 2, 64)):
+            t.copy_(new)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            graph.replay()
+            again = step(handle, large, large_ptr)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            want = step(other, x, q_ptr)
+        stream.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), seed
+        assert all(torch.equal(a, b) for a, b in zip(first, again)) and all((t == 77).all() for t in others)
+    live = handle._live
+    handle.close()
+    assert not live
+
+
+def test_scratch_without_graphs_is_replaced():
+    """Where no graph has it, a block that is too small goes when a larger one comes."""
+    handle = sg.Handle()
+    for n in (260, 3000):
+        x = tensors(34, BF, n, n, 4, 2, 64)
+        plan = plan_of(handle, n, n)
+        o, lse = at.forward(handle, plan, *x[:3])
+        at.backward(handle, plan, *x[:3], o, lse, x[3])
+        assert len(handle._live) == 1
+
+
 def test_documents_are_checked(h):
     good = dict(q_ptr=ints([0, 50, 100]), k_ptr=ints([0, 50, 100]))
     at.symbolic(h, 100, 100, **good)

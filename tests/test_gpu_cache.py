@@ -256,6 +256,37 @@ def test_decode_graph(h):
         assert torch.equal(out, want) and torch.equal(cache.k, eager.k) and torch.equal(cache.v, eager.v), i
 
 
+def test_decode_graph_after_a_larger_call(h):
+    """A captured step of serving, and then a batch on the same handle that needs more scratch memory."""
+    stream = torch.cuda.Stream()
+    handle = sg.Handle(stream=stream)
+    cache = filled(60, 1, 600, 2, 64)
+    table, lens = at.PageTable(*flat([list(range(40)), list(range(40, 43))])), i32([2500, 130])
+    many = at.PageTable(*flat([list(range(9 * i, 9 * i + 9)) for i in range(60)]))
+    many_lens = i32([570] * 60)
+    gen = torch.Generator(device="cuda").manual_seed(61)
+    q, large = randn(gen, (2, 1, 4, 64), BF), randn(gen, (60, 4, 4, 64), BF)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        at.attend(handle, cache, 0, table, lens, q)
+    stream.synchronize()
+    sizes = [t.numel() for t in handle._live.values()]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        out = at.attend(handle, cache, 0, table, lens, q)
+    with torch.cuda.stream(stream):
+        at.attend(handle, cache, 0, many, many_lens, large)
+        assert len(handle._live) == 2
+        others = [torch.full((n,), 77, dtype=torch.uint8, device="cuda") for n in sizes * 4]
+    for _ in range(3):
+        q.copy_(randn(gen, q.shape, BF))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, at.attend(h, cache, 0, table, lens, q)) and all((t == 77).all() for t in others)
+
+
 # ---- tables ---------------------------------------------------------------------------------------
 
 def made_table(rng, rows, pages, most, shared):
