@@ -11,6 +11,7 @@ from dataclasses import dataclass
 from typing import Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as sg
 
@@ -200,6 +201,7 @@ class _Attention(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_o):
         q, k, v, o, lse = ctx.saved_tensors
         handle, plan, scale, cap, slopes = ctx.rest
@@ -207,7 +209,7 @@ class _Attention(torch.autograd.Function):
 
 
 def attention(handle: sg.Handle, plan: Plan, q, k, v, scale: Optional[float] = None, cap: float = 0.0, slopes: Optional[torch.Tensor] = None):
-    """forward's o, differentiable in q, k and v (not in slopes).  The handle's stream has to be the current one, forward and backward."""
+    """forward's o, differentiable once in q, k and v (not in slopes); second derivatives raise.  The handle's stream has to be the current one, forward and backward."""
     return _Attention.apply(q, k, v, handle, plan, scale, cap, slopes)
 
 
