@@ -306,6 +306,14 @@ __global__ void __launch_bounds__(256, R == 128 ? 3 : 4) k_cache_attend(AttendAr
     const int64_t next_page = next < end ? page_of(next) : -1;
     if (page >= 0) {
       const float ks = load_uniform(a.c.k_scale + page * a.c.heads + kv), vs = load_uniform(a.c.v_scale + page * a.c.heads + kv);
+      if (a.c.bytes8 < R) {                        // channels behind the head's may hold anything, and 0 times NaN is NaN
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          const unsigned keep = (R / 4) * quarter + 8 * i < a.c.bytes8 ? ~0u : 0u;
+#pragma unroll
+          for (int t = 0; t < 4; ++t) { kw[t][i / 2][2 * (i % 2)] &= keep; kw[t][i / 2][2 * (i % 2) + 1] &= keep; }
+        }
+      }
       f32x4 x[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {

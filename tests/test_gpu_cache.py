@@ -168,6 +168,27 @@ def test_attend(h, name, dtype):
     check(name, o, want, bound)
 
 
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("d", [8, 40, 56, 72, 96, 120])
+def test_attend_channels_behind_the_head_anything(h, dtype, d):
+    """Channels from the head's last to the room's hold NaN in every page: no score and no result shows them, before and after tokens are added."""
+    cache = filled(53, 1, 12, 2, d)
+    cache.k[..., d:], cache.v[..., d:, :] = 0x7F, 0xFF
+    cache.k[..., d::2], cache.v[..., d::2, :] = 0xFF, 0x7F
+    lens, rows = [300, 64, 1], rows_for([300, 64, 1], 12, 2)
+    gen = torch.Generator(device="cuda").manual_seed(54)
+    q = randn(gen, (3, 2, 4, d), dtype, 1.5)
+    table = at.PageTable(*flat(rows))
+    host = HostCache(cache, 0)
+    check("imported", at.attend(h, cache, 0, table, i32(lens), q), *attend_reference(host, rows, lens, q, 1 / math.sqrt(d)))
+    k, v = randn(gen, (5, 2, d), dtype, 4.0), randn(gen, (5, 2, d), dtype, 4.0)
+    lens = [304, 64, 2]
+    host.append(rows, lens, [0, 4, 4, 5], k, v)
+    at.append(h, cache, 0, table, i32(lens), i64([0, 4, 4, 5]), k, v)
+    host.same(cache, 0, rows, lens)
+    check("appended", at.attend(h, cache, 0, table, i32(lens), q), *attend_reference(host, rows, lens, q, 1 / math.sqrt(d)))
+
+
 def test_attend_behind_a_window_anything(h):
     """Pages that no query's window reaches are not looked at, nor the tokens before it in its first page."""
     cache = filled(10, 1, 8, 1, 64)
