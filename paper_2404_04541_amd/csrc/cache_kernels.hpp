@@ -278,7 +278,8 @@ __global__ void __launch_bounds__(256, R == 128 ? 3 : 4) k_cache_attend(AttendAr
   f32x4 acc[kOut];
 #pragma unroll
   for (int i = 0; i < kOut; ++i) acc[i] = f32x4{0, 0, 0, 0};
-  float m = -INFINITY, l = 0.0f, unit = 1.0f;      // acc is in units of the last page's scale of values
+  float m = -INFINITY, l = 0.0f;
+  int unit = 127, most = 0;                        // acc is in units of 2^(unit - 127); the largest exponent of a scale of values so far
   u32x4 kw[4][kLoads], vw[kOut];
 
   auto page_of = [&](int n) {
@@ -358,9 +359,14 @@ __global__ void __launch_bounds__(256, R == 128 ? 3 : 4) k_cache_attend(AttendAr
       top = max_quarters(top);
       const float now = fmaxf(m, top), base = now == -INFINITY ? 0.0f : now;
       const float by = m == now ? 1.0f : fast_exp2(m - now);
-      const int shift = (int)(__float_as_uint(unit) >> 23) - (int)(__float_as_uint(vs) >> 23);
+      // acc goes to units of the page's scale, which costs nothing beside the new maximum; but not further down than 2^-64 of the largest scale so far: a page
+      // of zeros has the scale 2^-100, next to which sums of large values would overflow (448 * 2^31 tokens * 2^64 is finite).  A page below that has its
+      // probabilities scaled instead: what float16 has no room for there is less than 2^-63 of the largest value of the cache.
+      const int exponent = uniform((int)(__float_as_uint(vs) >> 23));
+      most = max(most, exponent);
+      const int new_unit = max(exponent, most - 64), shift = unit - new_unit;
       m = now;
-      unit = vs;
+      unit = new_unit;
       l *= by;
 #pragma unroll
       for (int i = 0; i < kOut; ++i)
@@ -371,10 +377,19 @@ __global__ void __launch_bounds__(256, R == 128 ? 3 : 4) k_cache_attend(AttendAr
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float e = fast_exp2(x[t][i] - base);
-          l += e;
-          p[t / 2][4 * (t % 2) + i] = (T)e;
+          x[t][i] = fast_exp2(x[t][i] - base);
+          l += x[t][i];
         }
+      if (exponent != unit) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[t][i] = __builtin_amdgcn_ldexpf(x[t][i], exponent - unit);
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[t / 2][4 * (t % 2) + i] = (T)x[t][i];
 #pragma unroll
       for (int i = 0; i < kOut; ++i) {
         acc[i] = mma(widen(u32x2{vw[i][0], vw[i][1]}, T()), p[0], acc[i]);
@@ -395,7 +410,7 @@ __global__ void __launch_bounds__(256, R == 128 ? 3 : 4) k_cache_attend(AttendAr
   __shared__ __align__(16) float sums[4][kRows][R + 4];
   if (quarter == 0) { ms[wave][col] = m; ls[wave][col] = l; }
 #pragma unroll
-  for (int i = 0; i < kOut; ++i) *reinterpret_cast<f32x4*>(&sums[wave][col][16 * i + 4 * quarter]) = acc[i] * unit;
+  for (int i = 0; i < kOut; ++i) *reinterpret_cast<f32x4*>(&sums[wave][col][16 * i + 4 * quarter]) = acc[i] * __uint_as_float((unsigned)unit << 23);
   __syncthreads();
   const int64_t cell = (slot * gridDim.y + kv) * gridDim.z + tile;
   for (int i = threadIdx.x; i < kRows * R / 4; i += 256) {

@@ -202,6 +202,24 @@ def test_attend_behind_a_window_anything(h):
     assert torch.equal(at.attend(h, cache, 0, table, i32(lens), q, window=100), want)
 
 
+@pytest.mark.parametrize("dtype, large, small", [(BF, 2.0 ** 30, 0.0), (BF, 2.0 ** 30, 2.0 ** -90), (BF, 2.0 ** 100, 2.0 ** -100), (F16, 3e4, 0.0), (F16, 3e4, 2.0 ** -20)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("first", [0, 4])
+def test_attend_pages_of_very_different_scales(h, dtype, large, small, d, first):
+    """Four pages of large values and four of zeros or tiny ones in turn, in workgroups that go over eight: what a wave has summed up of one page stays finite next to any other."""
+    gen = torch.Generator(device="cuda").manual_seed(55)
+    tokens, kv, heads = 6400, 8, 64
+    cache, rows = at.PagedCache.empty(1, 100, kv, d), rows_for([tokens], 100, 3)
+    k, v = randn(gen, (tokens, kv, d), dtype), torch.rand((tokens, kv, d), generator=gen, device="cuda") + 0.5
+    page = torch.arange(tokens, device="cuda") // PAGE
+    v = (v * torch.where((page + first) % 8 < 4, large, small)[:, None, None]).to(dtype)
+    table = at.PageTable(*flat(rows))
+    at.append(h, cache, 0, table, i32([tokens]), i64([0, tokens]), k, v)
+    q = randn(gen, (1, 16, heads, d), dtype)
+    o = at.attend(h, cache, 0, table, i32([tokens]), q)
+    check("o", o, *attend_reference(HostCache(cache, 0), rows, [tokens], q, 1 / math.sqrt(d)))
+
+
 def test_shared_and_missing_pages(h):
     """Sequences over the same pages; a table with fewer pages than its lengths, and ids that do not exist: what is there is attended to."""
     cache = filled(12, 1, 10, 2, 64)
