@@ -88,7 +88,8 @@ int spattn_forward(spgemm_handle h, const spattn_args* a, spattn_tensor o, float
 
 /* Gradients of sum(o * d_o) with respect to q, k and v, from forward's o and lse.  Key heads that several query heads share get the sum.
  * Probabilities and the scores' gradients are rounded to the type once, as operands, and so is o, which the row sums of o * d_o are made from: against 64 bits
- * the gradients are off by about 1.7 times what rounding the result alone costs.  In float16 a score's gradient beyond 65504 becomes infinite. */
+ * the gradients are off by about 1.7 times what rounding the result alone costs.  In float16 both operands are scaled by powers of two, a row's or key's
+ * own where its gradients are large, so that neither small nor large ones, nor long rows, lose digits before the result is rounded. */
 int spattn_backward(spgemm_handle h, const spattn_args* a, spattn_tensor o, const float* lse, spattn_tensor d_o, spattn_tensor dq,
                     spattn_tensor dk, spattn_tensor dv);
 

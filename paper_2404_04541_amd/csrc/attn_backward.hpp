@@ -5,7 +5,8 @@
 // k_attn_facts sums up what the rows' exponents begin with and -delta; after it workgroups of two kinds run in one launch, each with a fixed order of its
 // sums (no atomics: the same inputs give the same bits): for dQ they go over the keys of 128 queries as the forward kernel does, for dK and dV over
 // the queries, of all heads that share them, of 64 keys.  That computes S and dP twice, seven products where five would do with atomics on dQ in 32 bits.
-// P, dS are rounded to 16 bits once, as operands; all sums are held in 32 bits.
+// P, dS are rounded to 16 bits once, as operands; all sums are held in 32 bits.  In float16, whose smallest step is 2^-24, both are held 2^15 times as large, and
+// dS less where a row (for dQ) or a key (for dK) would pass 2^15: so neither the length of the rows nor the size of dO costs digits (Lift).
 //
 // Measured (bfloat16, 128 channels, capped): two documents of 8192 tokens together, 16 heads on 8, 631 us, 0.77 PFLOP/s for the seven products (call after call without a trace 567 with the rows' sums; vector instructions issue in
 // 54 % of the cycles, matrix instructions run in 41 %, LDS in 24 %: as the forward kernel); eleven documents of 4096 tokens, 16 heads on 4, 82 us and 5.3 to join, where two launches, one after
@@ -15,6 +16,32 @@
 #include "attn_plan_kernels.hpp"
 
 namespace spg {
+
+// What an operand made of P is multiplied by: P is at most 1, so 2^15 times P fits float16, and probabilities down to 2^-29 keep all digits.  bfloat16
+// has float's exponents.
+template <typename T> constexpr bool kLifted = std::is_same<T, f16_t>::value;
+template <typename T> constexpr float kLift = kLifted<T> ? 15.0f : 0.0f;   // in units of log 2
+constexpr float kLiftMost = 32768.0f;
+
+// dS of a lane's row (key) goes to sums that are in units of 2^-15 / lower, lower a power of two.  Where an entry would pass 2^15, entries, sums and `lower` go down
+// so far that the largest is below it; never up again, so that what the sums hold is exact.  Both halves of a wave have the same row (key).  us without | with: 2003 tokens,
+// 8 heads of 64 channels 23.6 | 26, 8192 tokens, 16 heads on 8 of 128, capped, 650 | 664.
+template <int N>
+__device__ __forceinline__ float lift_step(f32x16& ds, f32x16* sums, float& lower) {
+  float top = fabsf(ds[0]);
+#pragma unroll
+  for (int i = 1; i < 15; i += 2) top = max3(top, fabsf(ds[i]), fabsf(ds[i + 1]));
+  top = max_halves(fmaxf(top, fabsf(ds[15])));
+  float by = 1.0f;
+  if (__any(top >= kLiftMost)) {
+    by = top >= kLiftMost ? __uint_as_float((unsigned)(127 + 127 + 14 - (int)(__float_as_uint(top) >> 23)) << 23) : 1.0f;   // 2^(14 - exponent)
+    lower *= by;
+    ds *= by;
+#pragma unroll
+    for (int i = 0; i < N; ++i) sums[i] *= by;
+  }
+  return by;
+}
 
 // The work of n tiles as a list, most first, by one workgroup of 256 threads; tiles of up to 256 are cut into pieces where there are places for them (more
 // fill the card).  counts: the list's length, and how many of its entries belong to cut tiles: they come first.
@@ -88,7 +115,7 @@ __global__ void __launch_bounds__(256) k_attn_facts(AttnArgs a, AttnGrads g) {
   const RowBound rb = real ? a.plan.rows[row] : RowBound{0, 0, 0, 0};
   const float lse = real ? a.lse[(int64_t)head * a.q_len + row] : -INFINITY;
   RowFacts& facts = g.facts[(int64_t)head * a.q_tiles * (kPatTile / kQueryTile) + n];
-  facts.base[i] = lse == -INFINITY ? -INFINITY : (a.score.cap > 0.0f && !a.score.slopes ? a.score.cap * kLog2e : 0.0f) - lse * kLog2e;   // (a row that sees nothing: every power is 0)
+  facts.base[i] = lse == -INFINITY ? -INFINITY : (a.score.cap > 0.0f && !a.score.slopes ? a.score.cap * kLog2e : 0.0f) - lse * kLog2e + kLift<T>;   // (a row that sees nothing: every power is 0)
   facts.less[i] = -deltas[i];
   facts.lo[i] = rb.lo;
   facts.hi[i] = rb.hi;
@@ -125,7 +152,8 @@ __device__ __forceinline__ void dq_tile(unsigned char* lds, int n) {
   const bool real = row < a.q_len;
   const RowBound rb = real ? a.plan.rows[row] : RowBound{0, 0, 0, 0};
   const RowFacts& facts = g.facts[((int64_t)head * a.q_tiles + qt) * (kPatTile / kQueryTile) + wave / 2];
-  const float base = facts.base[row % kQueryTile], less = facts.less[row % kQueryTile];
+  float base = facts.base[row % kQueryTile], lower = 1.0f;
+  const float less = facts.less[row % kQueryTile];
   vec8<T> q[D / 16], d_o[D / 16];
   load_row<T, D>(a.q.of(head), row, real, a.bytes, half, q);
   load_row<T, D>(g.d_o.of(head), row, real, a.bytes, half, d_o);
@@ -165,6 +193,7 @@ __device__ __forceinline__ void dq_tile(unsigned char* lds, int n) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = (unsigned)(off + 8 * (i / 4) + i % 4) < span ? s[i] : 0.0f;
       }
+      if constexpr (kLifted<T>) base += __builtin_amdgcn_logf(lift_step<D / 32>(s, acc, lower));   // (a power of two: exact)
       vec8<T> p[2];
       to_operand<T>(s, p);
 #pragma unroll
@@ -193,6 +222,10 @@ __device__ __forceinline__ void dq_tile(unsigned char* lds, int n) {
     c = next;
   }
 
+  if constexpr (kLifted<T>) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) acc[i] *= 1.0f / (kLiftMost * lower);
+  }
   const BackArgs end_args = back_args();
   if (share.pieces > 1) leave_sums<D>(end_args.g.sums, load_uniform(&end_args.g.counts->cut_keys) * (end_args.a.heads / end_args.a.group) + n, acc);
   else if (row < end_args.a.q_len) store_rows<T, D>(end_args.g.dq, head, row, half, 0, end_args.a.bytes, acc, (CAP ? 4.0f : 1.0f) * end_args.a.score.scale);
@@ -250,6 +283,7 @@ __device__ __forceinline__ void dkv_tile(unsigned char* lds, int n) {
     return group < groups ? load_uniform(a.plan.groups + group) : GroupBound{0, 0, 0, 0};
   };
   ScoreFactors f = score_factors<CAP, BIAS>(a.score, kv * a.group);
+  float lower = 1.0f;
   auto compute = [&](const QueryTile<D>& t, const GroupBound& b) {
     if ((b.lo >= k0 + 32) | (b.hi <= k0)) return;
     const bool whole = (b.all_lo <= k0) & (b.all_hi >= k0 + 32);
@@ -300,6 +334,10 @@ __device__ __forceinline__ void dkv_tile(unsigned char* lds, int n) {
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) dv[i] = mma(S::template across<T>(to, at_across, 16 * u, i), p[u], dv[i]);
+    if constexpr (kLifted<T>) {
+      dp *= lower;                              // (a branch around it where lower is 1 costs 40 scalar registers)
+      lift_step<D / 32>(dp, dk, lower);
+    }
     to_operand<T>(dp, p);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -345,6 +383,10 @@ __device__ __forceinline__ void dkv_tile(unsigned char* lds, int n) {
   }
 
   // wave (keys, part 0) takes over the other's dK, wave (keys, part 1) its dV
+  if constexpr (kLifted<T>) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) { dk[i] *= 1.0f / (kLiftMost * lower); dv[i] *= 1.0f / kLiftMost; }
+  }
   __syncthreads();
   f32x4* room = reinterpret_cast<f32x4*>((wave & 1) ? odd.q : even.q) + part * (D / 8 * kWave) + lane;
   static_assert(2 * (D / 8) * kWave * 16 <= 2 * kQueryTile * D * 2, "both waves' sums fit a buffer's queries and dO");

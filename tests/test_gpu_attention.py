@@ -5,6 +5,7 @@ import math
 import pytest
 import torch
 
+import attn_helpers
 from attn_helpers import check, reference, visible
 from paper_2404_04541_amd import attention as at
 from paper_2404_04541_amd import binding as sg
@@ -255,6 +256,39 @@ def test_gradients_against_differences(h):
                 values.append(loss(moved))
             slope = (values[0] - values[1]) / (2 * step)
             assert abs(float(got[name][at_]) - slope) <= 1.01 * float(bounds[name][1][at_]) + 1e-6, (name, at_)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap, bias", [(0.0, False), (30.0, False), (0.0, True), (30.0, True)])
+@pytest.mark.parametrize("size", [2.0 ** -18, 2.0 ** -10, 1.0])
+def test_small_gradients_in_float16(h, monkeypatch, size, d, cap, bias):
+    """The digits of a score's gradient do not depend on how large d_o is: it is scaled, by a power of two for each row or key, before it becomes an operand.
+    The scale is 2^15, or what brings the largest of a row or key below 2^15: those here are below 2^7, so that half of float16's smallest
+    step, 2^-25, stands for at most 2^-33, and for 2^-40 where they are below 1.  (Scores lie within 8 of each other: no probability of the forward
+    pass is below float16's normal range.)  Queries and keys are small and the factor of the scores is large, so that the gradients are not."""
+    slopes = torch.tensor([0.002, 0.001, 0.0, 0.003], device="cuda") if bias else None
+    gen = torch.Generator(device="cuda").manual_seed(28)
+    part = lambda n, heads: torch.randn((n, heads, d), generator=gen, device="cuda").clamp(-2.5, 2.5)  # noqa: E731
+    scale = 2.0 ** 19 / d ** 0.5
+    monkeypatch.setitem(attn_helpers.TINY, F16, 2.0 ** -33 if size == 1.0 else 2.0 ** -40)
+    for tq, tk, mask in ((200, 1000, {"causal": False}), (700, 700, {"q_ptr": [0, 200, 700], "k_ptr": [0, 200, 700]})):
+        q, k, v, d_o = part(tq, 4) * 2.0 ** -10, part(tk, 2) * 2.0 ** -10, part(tk, 2), part(tq, 4) * size
+        run(h, *(t.to(F16) for t in (q, k, v, d_o)), mask, cap=cap, slopes=slopes, scale=scale)
+
+
+def test_probabilities_of_long_rows_in_float16(h, monkeypatch):
+    """Rows of 196 608 equal scores: each probability is 85.3 of float16's smallest steps, and keeps its digits as an operand of the values' gradient, where it is
+    2^15 times as large.  (In the forward pass they are 1 before the division.)"""
+    monkeypatch.setitem(attn_helpers.TINY, F16, 2.0 ** -40)
+    q, k, v, d_o = tensors(29, F16, 64, 3 << 16, 1, 1, 8)
+    run(h, torch.zeros_like(q), k, v, d_o.abs() * 1024, {"causal": False})
+
+
+@pytest.mark.parametrize("cap", [0.0, 3000.0])
+def test_large_gradients_in_float16(h, cap):
+    """Scores' gradients beyond float16's largest number, between inputs and gradients that it holds."""
+    q, k, v, d_o = tensors(30, F16, 300, 400, 4, 2, 64)
+    run(h, q * 16, k * 16, v * 256, d_o * 256, {"q_ptr": [0, 100, 300], "k_ptr": [0, 150, 400]}, scale=2.0 ** -12, cap=cap)
 
 
 def test_autograd(h):
