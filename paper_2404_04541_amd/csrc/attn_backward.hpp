@@ -8,8 +8,8 @@
 // P, dS are rounded to 16 bits once, as operands; all sums are held in 32 bits.  In float16, whose smallest step is 2^-24, both are held 2^15 times as large, and
 // dS less where a row (for dQ) or a key (for dK) would pass 2^15: so neither the length of the rows nor the size of dO costs digits (Lift).
 //
-// Measured (bfloat16, 128 channels, capped): two documents of 8192 tokens together, 16 heads on 8, 631 us, 0.77 PFLOP/s for the seven products (call after call without a trace 567 with the rows' sums; vector instructions issue in
-// 54 % of the cycles, matrix instructions run in 41 %, LDS in 24 %: as the forward kernel); eleven documents of 4096 tokens, 16 heads on 4, 82 us and 5.3 to join, where two launches, one after
+// Measured (bfloat16, 128 channels, capped): two documents of 8192 tokens together, 16 heads on 8, 639 us, 0.76 PFLOP/s for the seven products (call after call without a trace 567 with the rows' sums; vector instructions issue in
+// 55 % of the cycles, matrix instructions run in 42 %, LDS in 24 %: as the forward kernel); eleven documents of 4096 tokens, 16 heads on 4, 80 us and 5.2 to join, where two launches, one after
 // the other, took 126 and 8.6: the long chains of one kind fill the places that the other leaves.
 #pragma once
 #include "attn_forward.hpp"
@@ -43,8 +43,8 @@ __device__ __forceinline__ float lift_step(f32x16& ds, f32x16* sums, float& lowe
   return by;
 }
 
-// The work of n tiles as a list, most first, by one workgroup of 256 threads; tiles of up to 256 are cut into pieces where there are places for them (more
-// fill the card).  counts: the list's length, and how many of its entries belong to cut tiles: they come first.
+// The work of n tiles as a list, most first, by one workgroup of 256 threads; up to 256 tiles are cut into pieces where there are places for them.  More
+// are not, whatever the places: with one key head their chains are then the time.  counts: the list's length, and how many of its entries belong to cut tiles: they come first.
 template <typename F, typename W>
 __device__ __forceinline__ void list_work(int n, F reach, W tiles, unsigned long long total, const AttnGrads& g, int4* list, int* counts) {
   if (n > 256) {
@@ -72,7 +72,7 @@ __device__ __forceinline__ void list_work(int n, F reach, W tiles, unsigned long
 }
 
 // A workgroup has 64 rows of a head: D / 8 lanes a row, 16 bytes of O and dO each.  The first two make the lists of work meanwhile.
-// Memory bounds it: 8192 tokens, 16 heads of 128 channels 14.2 us, 4.7 TB/s; 4096 tokens 8.2 us, with lists of cut work 9.5.
+// Memory bounds it: 8192 tokens, 16 heads of 128 channels 14.8 us, 4.5 TB/s; 4096 tokens, with lists of cut work, 9.3.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_attn_facts(AttnArgs a, AttnGrads g) {
   constexpr int kLanes = D / 8, kStep = 256 / kLanes;

@@ -7,9 +7,9 @@
 // maximum m; sums and maxima in 32 bits, probabilities rounded to 16 bits once, as an operand.  The accumulators are brought to a
 // new maximum only where some row's grew by more than 2^8 since (the sum is in the same units, so nothing is approximated).
 //
-// Measured (bfloat16, 128 channels): two documents of 8192 tokens together, 16 heads on 8, capped, 200 us, 0.69 PFLOP/s (call after call without a trace 176, 0.78); 5003 queries over 11 147 keys through a
-// pattern, 32 heads on 8, with distances, 166 us, 0.67 (144, 0.78).  Vector instructions issue in 57 % of the cycles (50 in the second), eight an entry with a cap,
-// three of them powers and reciprocals; matrix instructions run in 38 % (39), LDS in 19 %: what vector and matrix instructions take
+// Measured (bfloat16, 128 channels): two documents of 8192 tokens together, 16 heads on 8, capped, 199 us, 0.69 PFLOP/s (call after call without a trace 176, 0.78); 5003 queries over 11 147 keys through a
+// pattern, 32 heads on 8, with distances, 165 us, 0.68 (144, 0.78).  Vector instructions issue in 59 % of the cycles (51 in the second), eight an entry with a cap,
+// three of them powers and reciprocals; matrix instructions run in 39 % (39), LDS in 19 %: what vector and matrix instructions take
 // together bounds it, for two waves a SIMD, as many as the registers allow, hardly overlap.  Tiles of 32 keys for three waves, products of the next tile beside
 // the powers of this one (in the order of the code or by hints to the scheduler) and priorities were all slower.  Short rows (documents of a few
 // hundred tokens) are bound by the chain of their tiles, 2 us each.
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(256, 2) k_attn_fwd(AttnArgs a) {
   finish_rows<T, D>(a, head, row, half, 0, acc, m, l);
 }
 
-// A workgroup has 32 channels of a tile's rows.  2003 tokens, 8 heads of 64 channels: 4.8 us.
+// A workgroup has 32 channels of a tile's rows.  2003 tokens, 8 heads of 64 channels: 5 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
   const Place at = place_of(blockIdx.x, a.heads, a.plan.q_order);

@@ -1,6 +1,6 @@
 // The structure of a mask: bounds of its rows, of groups of rows and of columns, and a pattern's flags.  Bandwidth does not matter here (28 bytes a row);
-// what a plan costs is its launches: two, or one where the mask is small (and then one more for a pattern).  us: 257 tokens 4.3; 4096 in eleven documents
-// 4.7 + 5; 8192 4.8 + 7; 5003 queries over 11 147 keys with a pattern 4.9 + 6.6 (its flags in a launch of their own: 4.8 more).
+// what a plan costs is its launches: two, or one where the mask is small (and then one more for a pattern).  us: 257 tokens 4.4; 4096 in eleven documents
+// 4.8 + 4.5; 8192 4.9 + 6.8; 5003 queries over 11 147 keys with a pattern 5.0 + 6.3 (its flags in a launch of their own: 4.8 more).
 #pragma once
 #include "attn_common.hpp"
 

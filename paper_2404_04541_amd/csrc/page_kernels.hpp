@@ -3,8 +3,8 @@
 // A table is a compressed structure (rows: sequences, columns: pages).  Everything here but the copies is a few bytes a row or page: what it
 // costs is launches and dependent loads, so that ranks (the k-th free page) are found by counting bits in a flag list, as the
 // product's kernels rank columns.  No result depends on the order of atomics: they count, take minima, or set bits.
-// us, without copies: a fork of 8 rows 2.4 + 2.7 + 2.6 + 3.9 (by one workgroup 17), 512 rows from 384 3.1 + 8 + 3.7 + 7.3 (gather: atomics on pages that many rows share);
-// compacting 2048 pages 1.5 + 4.6 + 2.3 + 4.0.
+// us, without copies: a fork of 8 rows 2.6 + 2.8 + 2.8 + 4.1 (by one workgroup 17), 512 rows from 384 3.2 + 8.4 + 3.3 + 7.0 (gather: atomics on pages that many rows share);
+// compacting 2048 pages 1.7 + 4.5 + 2.0 + 3.9.
 #pragma once
 #include "cache_kernels.hpp"
 
@@ -164,7 +164,8 @@ __device__ __forceinline__ void fork_flags(const ForkArgs& a, int64_t block) {
   __syncthreads();
 }
 
-// The k-th page (from 0) that is not in use, or -1.
+// The k-th page (from 0) that is not in use, or -1.  (Blocks are walked one after the other, then words: a cache of 60 000 pages that is nearly full takes up to 60
+// dependent loads and 32 more.)
 __device__ __forceinline__ int64_t free_page(const PageFlags& f, int64_t k) {
   const int64_t blocks = (f.pages + kPageBlock - 1) / kPageBlock;
   for (int64_t b = 0; b < blocks; ++b) {
@@ -314,7 +315,7 @@ struct CopyArgs {
 
 constexpr int kCopyPiece = 16384;    // bytes that a workgroup copies at a time: four loads of 16 bytes in flight a lane
 
-// Destinations are distinct and no source, so the copies need no order.  Memory bounds it: 237 MB read and written 40 us, 5.9 TB/s; 530 MB 116 us, 4.6.
+// Destinations are distinct and no source, so the copies need no order.  Memory bounds it: 237 MB read and written 40 us, 5.9 TB/s; 530 MB 117 us, 4.5.
 __global__ void __launch_bounds__(256) k_page_copy(CopyArgs a) {
   if (a.report && blockIdx.x == 0 && threadIdx.x == 0) *a.report = *a.in;
   if (a.in && a.in->error) return;
