@@ -25,22 +25,23 @@ constexpr float kLiftMost = 32768.0f;
 
 // dS of a lane's row (key) goes to sums that are in units of 2^-15 / lower, lower a power of two.  Where an entry would pass 2^15, entries, sums and `lower` go down
 // so far that the largest is below it; never up again, so that what the sums hold is exact.  Both halves of a wave have the same row (key).  us without | with: 2003 tokens,
-// 8 heads of 64 channels 23.6 | 26, 8192 tokens, 16 heads on 8 of 128, capped, 650 | 664.
+// 8 heads of 64 channels 23.6 | 25, 8192 tokens, 16 heads on 8 of 128, capped, 650 | 666.
+// What comes later is lowered through `base`, which is added to its exponents, where there is one.
 template <int N>
-__device__ __forceinline__ float lift_step(f32x16& ds, f32x16* sums, float& lower) {
+__device__ __forceinline__ void lift_step(f32x16& ds, f32x16* sums, float& lower, float* base) {
   float top = fabsf(ds[0]);
 #pragma unroll
   for (int i = 1; i < 15; i += 2) top = max3(top, fabsf(ds[i]), fabsf(ds[i + 1]));
   top = max_halves(fmaxf(top, fabsf(ds[15])));
-  float by = 1.0f;
   if (__any(top >= kLiftMost)) {
-    by = top >= kLiftMost ? __uint_as_float((unsigned)(127 + 127 + 14 - (int)(__float_as_uint(top) >> 23)) << 23) : 1.0f;   // 2^(14 - exponent)
+    const int down = top >= kLiftMost ? (int)(__float_as_uint(top) >> 23) - 127 - 14 : 0;
+    const float by = __uint_as_float((unsigned)(127 - down) << 23);
     lower *= by;
+    if (base) *base -= (float)down;
     ds *= by;
 #pragma unroll
     for (int i = 0; i < N; ++i) sums[i] *= by;
   }
-  return by;
 }
 
 // The work of n tiles as a list, most first, by one workgroup of 256 threads; up to 256 tiles are cut into pieces where there are places for them.  More
@@ -193,7 +194,7 @@ __device__ __forceinline__ void dq_tile(unsigned char* lds, int n) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = (unsigned)(off + 8 * (i / 4) + i % 4) < span ? s[i] : 0.0f;
       }
-      if constexpr (kLifted<T>) base += __builtin_amdgcn_logf(lift_step<D / 32>(s, acc, lower));   // (a power of two: exact)
+      if constexpr (kLifted<T>) lift_step<D / 32>(s, acc, lower, &base);
       vec8<T> p[2];
       to_operand<T>(s, p);
 #pragma unroll
@@ -336,7 +337,7 @@ __device__ __forceinline__ void dkv_tile(unsigned char* lds, int n) {
       for (int i = 0; i < D / 32; ++i) dv[i] = mma(S::template across<T>(to, at_across, 16 * u, i), p[u], dv[i]);
     if constexpr (kLifted<T>) {
       dp *= lower;                              // (a branch around it where lower is 1 costs 40 scalar registers)
-      lift_step<D / 32>(dp, dk, lower);
+      lift_step<D / 32>(dp, dk, lower, nullptr);
     }
     to_operand<T>(dp, p);
 #pragma unroll
