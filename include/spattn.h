@@ -119,6 +119,12 @@ typedef struct {
 int spcache_append(spgemm_handle h, const spcache* c, int64_t layer, const spgemm_csr* table, const int32_t* lens, const int64_t* new_ptr,
                    int64_t tokens, int32_t dtype, spattn_tensor k, spattn_tensor v);
 
+/* Tokens back out of a layer, as rows of 16 bits: rows ptr[s] .. ptr[s+1] - 1 (device, rows + 1, from 0 to tokens) of k and v become the last tokens of sequence s, each the
+ * value that its 8 bits and its page's scale stand for, rounded to nearest (bfloat16 holds it exactly; what the type cannot hold becomes infinite or loses digits).  Where s has fewer tokens,
+ * or its table lacks the page, the row becomes 0.  Such rows are what spattn_forward takes: a long part of a prompt over what is cached of it, k_ptr = ptr. */
+int spcache_read(spgemm_handle h, const spcache* c, int64_t layer, const spgemm_csr* table, const int32_t* lens, const int64_t* ptr, int64_t tokens, int32_t dtype,
+                 spattn_tensor k, spattn_tensor v);
+
 /* o = attention of the last q_len tokens of every sequence (q and o: token s * q_len + i) over its cache.  Token i sees the keys up to itself, with
  * window > 0 only the last `window` of those.  Scores as in spattn_args.  A token before the sequence's first has the output 0.
  * q_len * heads is at most 65535. */

@@ -19,8 +19,8 @@ F16, BF16 = 0, 1
 TILE = 128
 PAGE = 64
 
-EXPORTED = ("spattn_plan_bytes", "spattn_symbolic", "spattn_forward", "spattn_backward", "spcache_append", "spcache_attend", "spcache_fork",
-            "spcache_compact", "spcache_copy")
+EXPORTED = ("spattn_plan_bytes", "spattn_symbolic", "spattn_forward", "spattn_backward", "spcache_append", "spcache_read", "spcache_attend",
+            "spcache_fork", "spcache_compact", "spcache_copy")
 
 
 class TensorStruct(C.Structure):
@@ -57,6 +57,7 @@ def _lib():
     lib.spattn_forward.argtypes = [V, P(ArgsStruct), T, V]
     lib.spattn_backward.argtypes = [V, P(ArgsStruct), T, V, T, T, T, T]
     lib.spcache_append.argtypes = [V, P(CacheStruct), I, P(sg.CsrStruct), V, V, I, C.c_int32, T, T]
+    lib.spcache_read.argtypes = [V, P(CacheStruct), I, P(sg.CsrStruct), V, V, I, C.c_int32, T, T]
     lib.spcache_attend.argtypes = [V, P(CacheStruct), I, P(sg.CsrStruct), V, I, C.c_int32, C.c_int32, C.c_float, C.c_float, V, I, T, T]
     lib.spcache_fork.argtypes = [V, P(CacheStruct), P(sg.CsrStruct), V, I, V, V, V, V, I, V, P(C.c_int64)]
     lib.spcache_compact.argtypes = [V, P(CacheStruct), P(sg.CsrStruct), V, P(C.c_int64)]
@@ -259,6 +260,20 @@ def append(handle: sg.Handle, cache: PagedCache, layer: int, table: PageTable, l
         raise ValueError("k and v: [tokens, kv_heads, head_dim] of the cache is wanted")
     handle._check(lib.spcache_append(handle.ptr, C.byref(cache._struct), int(layer), C.byref(table.struct(cache)), _array(lens, "lens", torch.int32, table.rows),
                                      _array(new_ptr, "new_ptr", torch.int64, table.rows + 1), k.shape[0], _dtype(k), _tensor(k, "k"), _tensor(v, "v", None, k)))
+
+
+def read(handle: sg.Handle, cache: PagedCache, layer: int, table: PageTable, lens: torch.Tensor, ptr: torch.Tensor, tokens: int, dtype: torch.dtype = torch.bfloat16):
+    """-> (k, v) [tokens, kv_heads, head_dim]: rows ptr[s] .. ptr[s + 1] - 1 (int64) are the last tokens of sequence s, back from 8 bits: what `forward` takes, with k_ptr = ptr.
+
+    tokens: how many rows there are, ptr's last element.  Rows of tokens that a sequence does not have, or whose page its table lacks, are zero."""
+    lib = _lib()
+    if tokens < 0:
+        raise ValueError("tokens: a negative number")
+    rows = _array(ptr, "ptr", torch.int64, table.rows + 1)
+    k, v = _results(handle, lambda: tuple(torch.empty((int(tokens), cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.k.device) for _ in range(2)))
+    handle._check(lib.spcache_read(handle.ptr, C.byref(cache._struct), int(layer), C.byref(table.struct(cache)), _array(lens, "lens", torch.int32, table.rows), rows,
+                                   int(tokens), _dtype(k), _result(k), _result(v)))
+    return k, v
 
 
 def attend(handle: sg.Handle, cache: PagedCache, layer: int, table: PageTable, lens: torch.Tensor, q, scale: Optional[float] = None, cap: float = 0.0,

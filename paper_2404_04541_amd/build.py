@@ -9,6 +9,7 @@ from concurrent.futures import ThreadPoolExecutor
 _HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(_HERE, "csrc", "spgemm_api.hip")
 SRC_ATTENTION = os.path.join(_HERE, "csrc", "attention_api.hip")
+SRC_DRAFTS = os.path.join(_HERE, "csrc", "draft_api.hip")
 LIB = os.path.join(_HERE, "libspgemm_gfx950.so")
 LIB_CLOCKS = os.path.join(_HERE, "libspgemm_gfx950_clocks.so")   # the same sources with -DSPG_PHASE_CLOCKS (profiling only)
 
@@ -38,8 +39,8 @@ def build_library(verbose: bool = False, phase_clocks: bool = False) -> str:
     if phase_clocks:
         _hipcc(["-shared", "-DSPG_PHASE_CLOCKS=1", "-o", LIB_CLOCKS, SRC], verbose)
         return LIB_CLOCKS
-    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(2) as pool:
-        sources = (SRC, SRC_ATTENTION)
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(3) as pool:
+        sources = (SRC, SRC_ATTENTION, SRC_DRAFTS)
         objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in sources]
         list(pool.map(lambda so: _hipcc(["-c", "-o", so[1], so[0]], verbose), zip(sources, objects)))
         _hipcc(["-shared", "-o", LIB, *objects], verbose)
