@@ -41,37 +41,6 @@ __device__ __forceinline__ Loaded<T> load_some(const T* row, int64_t at, int voc
   return r;
 }
 
-// What the rows have become after some children were not taken: r = max(r - q, 0) * r_by (r itself where r_by is 0), q = q * q_by, 0 at the token.
-struct Refused {
-  int count;
-  int token[kMostNodes];
-  double r_by[kMostNodes], q_by[kMostNodes];
-};
-
-struct Weights { double r, q; };
-// r and q of token v after the first `count` refusals.  near: v may be one of their tokens.
-template <bool DRAFT>
-__device__ __forceinline__ Weights weights(const Refused& f, int count, int v, float r0, float q0, bool near) {
-  Weights w{(double)r0, DRAFT ? (double)q0 : 0.0};
-  for (int i = 0; i < count; ++i) {
-    const bool is = near && f.token[i] == v;
-    if constexpr (DRAFT) {
-      const double by = f.r_by[i];
-      w.r = by != 0.0 ? fmax(w.r - w.q, 0.0) * by : w.r;
-      w.q = is ? 0.0 : w.q * f.q_by[i];
-    } else {
-      const double by = f.r_by[i];
-      w.r = by != 0.0 ? (is ? 0.0 : w.r * by) : w.r;
-    }
-  }
-  return w;
-}
-// What r becomes when x is refused, not divided by its sum.
-template <bool DRAFT>
-__device__ __forceinline__ double left_of(const Weights& w, bool is_x) {
-  return DRAFT ? fmax(w.r - w.q, 0.0) : is_x ? 0.0 : w.r;
-}
-
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int d = 1; d < kWave; d *= 2) v += __shfl_xor(v, d);
@@ -88,111 +57,254 @@ __device__ __forceinline__ bool first_taken(const VerifyArgs& a, int64_t parent,
   return (double)a.u[i] * q < p;
 }
 
-// f(v, r0, q0, near) for tokens from .. to - 1 of the rows, by one wave.  near: one of the first `count` refused tokens, or x, may be among the lane's.
+// The sum of f(token, entry of p, entry of q) over a part of the rows, by one wave.  Tokens of children are left out: where a batch of tokens may hold one (a bit of `marks` for every
+// batch, of 64 in turn) each is compared.  Four batches' loads are on their way together.
+constexpr int kInFlight = 4;
 template <typename T, bool DRAFT, typename F>
-__device__ __forceinline__ void walk_tokens(const T* p, const T* q, int vocab, int from, int to, const Refused& f, int count, int x, F each) {
+__device__ __forceinline__ void walk_tokens(const T* p, const T* q, int vocab, int from, int to, unsigned long long marks, const int* children, int count, F each) {
   constexpr int kCount = Loaded<T>::kCount, kBatch = kWave * kCount;
-  for (int b = from; b < to; b += kBatch) {
+  auto batch = [&](int b, const Loaded<T>& r, const Loaded<T>& s) {
     const int v0 = b + lane_id() * kCount;
-    const Loaded<T> r = load_some(p, v0, vocab);
-    Loaded<T> s = {};
-    if constexpr (DRAFT) s = load_some(q, v0, vocab);
-    bool near = x >= b && x < b + kBatch;
-    for (int i = 0; i < count; ++i) near |= f.token[i] >= b && f.token[i] < b + kBatch;
+    if (marks >> (b / kBatch % 64) & 1) {
+      unsigned out = 0;
+      for (int j = 0; j < count; ++j) {
+        const int at = children[j] - v0;
+        out |= at >= 0 && at < kCount ? 1u << at : 0u;
+      }
 #pragma unroll
-    for (int i = 0; i < kCount; ++i)
-      if (v0 + i < to) each(v0 + i, proper(r.v[i]), DRAFT ? proper(s.v[i]) : 0.0f, near);
+      for (int i = 0; i < kCount; ++i) each(v0 + i, out >> i & 1 ? 0.0f : proper(r.v[i]), DRAFT && !(out >> i & 1) ? proper(s.v[i]) : 0.0f);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCount; ++i) each(v0 + i, proper(r.v[i]), DRAFT ? proper(s.v[i]) : 0.0f);
+    }
+  };
+  int b = from;
+  for (; b + kInFlight * kBatch <= to; b += kInFlight * kBatch) {
+    Loaded<T> r[kInFlight], s[kInFlight];
+#pragma unroll
+    for (int i = 0; i < kInFlight; ++i) {
+      __builtin_memcpy(&r[i], p + b + i * kBatch + lane_id() * kCount, 16);
+      if constexpr (DRAFT) __builtin_memcpy(&s[i], q + b + i * kBatch + lane_id() * kCount, 16);
+    }
+#pragma unroll
+    for (int i = 0; i < kInFlight; ++i) batch(b + i * kBatch, r[i], s[i]);
+  }
+  for (; b < to; b += kBatch) {
+    const Loaded<T> r = load_some(p, b + lane_id() * kCount, vocab);
+    Loaded<T> s = {};
+    if constexpr (DRAFT) s = load_some(q, b + lane_id() * kCount, vocab);
+    batch(b, r, s);
   }
 }
 
+// The children of a node, in order, and the entries of the rows at their tokens.
+struct Children {
+  int count, node[kMostNodes], token[kMostNodes];
+  float p[kMostNodes], q[kMostNodes], u[kMostNodes];
+};
+
+// Both rows after some children were refused, as far as they are not at children's tokens: r = max(a P - b Q, 0), for max(max(x, 0) - c, 0) is max(x - c, 0) where c is not
+// negative, and q = c Q.  So a pass takes the same few operations however many children were refused.  What r and q are at children's tokens every wave holds in registers.
 template <typename T, bool DRAFT>
 __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
-  __shared__ Refused refused;
-  __shared__ double parts[2][kVerifyWaves];
-  __shared__ int found;
+  constexpr int kGroups = kMostNodes / kWave, kBatch = kWave * Loaded<T>::kCount;
+  __shared__ Children kids;
+  __shared__ int found[kGroups];
+  __shared__ double parts[2][kVerifyWaves], weights[kMostNodes];
   const int64_t token = blockIdx.x;
   const int wave = uniform(threadIdx.x / kWave), lane = lane_id();
   const int s = uniform(find_seq(a.trees.rows, token, [&](int i) { return tree_begin(a.trees, i); }));
   const Tree tree = tree_of(a.trees, s);
   const int node = (int)(token - tree.first);
   if (node < 0 || node >= tree.n) return;
-  // Can the walk come here?  It begins at node 0; a first child on the way has to be taken, and before another one the first may not be.
-  {
-    bool barred = false;
-    const int i = threadIdx.x;
-    if (i < tree.n && i / 64 < a.trees.words && a.trees.up[token * a.trees.words + i / 64] >> (i % 64) & 1) {
-      const int parent = a.trees.node[tree.first + i].x;
-      if (parent < 0) barred = i != 0;
-      else {
-        const int first = a.trees.node[tree.first + parent].y;
-        barred = first_taken<T, DRAFT>(a, tree.first + parent, tree.first + first) != (first == i);
-      }
-    }
-    if (__syncthreads_or(barred)) return;
-  }
   const T* p = static_cast<const T*>(a.target) + token * a.target_stride;
   const T* q = DRAFT ? static_cast<const T*>(a.draft) + token * a.draft_stride : nullptr;
-  constexpr int kBatch = kWave * Loaded<T>::kCount;
+  {
+    // Can the walk come here?  It begins at node 0; a first child on the way has to be taken, and before another one the first may not be.
+    bool barred = false, mine = false;
+    int i = threadIdx.x, rank = 0, x = 0;
+    float px = 0.0f, qx = 0.0f, ux = 0.0f;
+    if (i < kMostNodes) {
+      if (i < tree.n && i / 64 < a.trees.words && a.trees.up[token * a.trees.words + i / 64] >> (i % 64) & 1) {
+        const int parent = a.trees.node[tree.first + i].x;
+        if (parent < 0) barred = i != 0;
+        else {
+          const int first = a.trees.node[tree.first + parent].y;
+          barred = first_taken<T, DRAFT>(a, tree.first + parent, tree.first + first) != (first == i);
+        }
+      }
+    } else if (i < 2 * kMostNodes) {
+      i -= kMostNodes;
+      if (i < tree.n && a.trees.node[tree.first + i].x == node) {
+        x = a.ids[tree.first + i];
+        mine = x >= 0 && x < a.vocab;
+        if (mine) {
+          ux = a.u[tree.first + i];
+          px = proper(p[x]);
+          if constexpr (DRAFT) qx = proper(q[x]);
+        }
+      }
+      const unsigned long long all = __ballot(mine);
+      rank = __popcll(all & ((1ull << lane) - 1));
+      if (lane == 0) found[i / kWave] = __popcll(all);
+    }
+    if (__syncthreads_or(barred)) return;
+    if (mine) {
+      for (int g = 0; g < i / kWave; ++g) rank += found[g];
+      kids.node[rank] = i; kids.token[rank] = x;
+      kids.p[rank] = px; kids.q[rank] = qx; kids.u[rank] = ux;
+    }
+    if (threadIdx.x == 0) {
+      int n = 0;
+      for (int g = 0; g < kGroups; ++g) n += found[g];
+      kids.count = n;
+    }
+    __syncthreads();
+  }
+  const int count = uniform(kids.count), groups = ceil_div_d(count, kWave);
+  // r and q at the children's tokens (0 for one whose token an earlier one has), as they are and as they were at first
+  double r[kGroups] = {}, q_now[kGroups] = {}, q_all[kGroups] = {};
+  int x[kGroups];
+  bool again[kGroups];
+  unsigned long long marks = 0;
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    const int j = g * kWave + lane;
+    x[g] = -1;
+    again[g] = false;
+    if (g < groups && j < count) {
+      x[g] = kids.token[j];
+      for (int i = 0; i < j; ++i) again[g] |= kids.token[i] == x[g];
+      r[g] = again[g] ? 0.0 : kids.p[j];
+      q_now[g] = q_all[g] = again[g] ? 0.0 : kids.q[j];
+      marks |= 1ull << (x[g] / kBatch % 64);
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) marks |= __shfl_xor(marks, d);
+  const unsigned marks_lo = uniform((int)marks), marks_hi = uniform((int)(marks >> 32));
+  marks = (unsigned long long)marks_hi << 32 | marks_lo;
+
   const int part = ceil_div_d(ceil_div_d(a.vocab, kVerifyWaves), kBatch) * kBatch;
   const int from = min(wave * part, a.vocab), to = min(from + part, a.vocab);
-  if (threadIdx.x == 0) refused.count = 0;
-  // sums over the row of what f gives for a token, part by part
-  auto sums = [&](int count, int x, auto f) {
-    double r = 0.0, other = 0.0;
-    walk_tokens<T, DRAFT>(p, q, a.vocab, from, to, refused, count, x, [&](int v, float r0, float q0, bool near) { f(v, r0, q0, near, r, other); });
-    r = wave_sum(r);
+  double ra = 1.0, rb = 0.0, qc = 1.0;
+  // parts: of every wave's part of the rows, without the children's tokens, the sums of max(pa P - pb Q, 0) and of Q
+  bool have = false;
+  double pa = 1.0, pb = 0.0;
+  auto pass = [&](double sa, double sb) {
+    double sum = 0.0, other = 0.0;
+    if (DRAFT && sb != 0.0)
+      walk_tokens<T, DRAFT>(p, q, a.vocab, from, to, marks, kids.token, count, [&](int, float r0, float q0) {
+        sum += fmax(sa * (double)r0 - sb * (double)q0, 0.0);
+        other += (double)q0;
+      });
+    else                                 // (the draft's row of a node without children may hold anything)
+      walk_tokens<T, false>(p, q, a.vocab, from, to, marks, kids.token, count, [&](int, float r0, float) { sum += (double)r0; });
+    sum = wave_sum(sum);
     other = wave_sum(other);
     __syncthreads();                     // (whoever read the parts before is done)
-    if (lane == 0) { parts[0][wave] = r; parts[1][wave] = other; }
+    if (lane == 0) { parts[0][wave] = sum; parts[1][wave] = other; }
     __syncthreads();
-    r = other = 0.0;
-    for (int w = 0; w < kVerifyWaves; ++w) { r += parts[0][w]; other += parts[1][w]; }
-    return Weights{r, other};
+    have = true;
+    pa = sa;
+    pb = sb;
   };
-  int last = -1, count = 0;              // the last refused token, where the sums of the parts are of what r is after it
-  double total = 0.0;
-  for (int child = a.trees.node[token].y; child >= 0; child = a.trees.node[tree.first + child].z) {
-    const int x = a.ids[tree.first + child];
-    if (x < 0 || x >= a.vocab) continue;
-    __syncthreads();
-    const Weights w = weights<DRAFT>(refused, count, x, proper(p[x]), DRAFT ? proper(q[x]) : 0.0f, true);
-    if ((double)a.u[tree.first + child] * (DRAFT ? w.q : 1.0) < w.r) {
-      if (threadIdx.x == 0) a.onward[token] = make_int2(child, -1);
+  auto total = [&](int which) {
+    double v = 0.0;
+    for (int w = 0; w < kVerifyWaves; ++w) v += parts[which][w];
+    return v;
+  };
+  // the sum over children of f(group, lane's child)
+  auto over = [&](auto f) {
+    double v = 0.0;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+      if (g < groups && x[g] >= 0) v += f(g);
+    return wave_sum(v);
+  };
+  double w[kGroups] = {};                // what r was at the children's tokens before it was divided by its sum
+  bool undivided = false;                // parts and w are of r before that
+  for (int k = 0; k < count; ++k) {
+    double rk = 0.0, qk = 0.0;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+      if (g == k / kWave) { rk = __shfl(r[g], k % kWave); qk = __shfl(q_now[g], k % kWave); }
+    const int xk = kids.token[k];
+    // (a token that an earlier child has: its r and q are at that child)
+    bool repeated = false;
+    for (int i = 0; i < k && !repeated; ++i)
+      if (kids.token[i] == xk) {
+        repeated = true;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+          if (g == i / kWave) { rk = __shfl(r[g], i % kWave); qk = __shfl(q_now[g], i % kWave); }
+      }
+    if ((double)kids.u[k] * (DRAFT ? qk : 1.0) < rk) {
+      if (threadIdx.x == 0) a.onward[token] = make_int2(kids.node[k], -1);
       return;
     }
-    const Weights sum = sums(count, x, [&](int v, float r0, float q0, bool near, double& r, double& other) {
-      const Weights w = weights<DRAFT>(refused, count, v, r0, q0, near);
-      const bool is = near && v == x;
-      r += left_of<DRAFT>(w, is);
-      if constexpr (DRAFT) other += is ? 0.0 : w.q;
-    });
-    if (threadIdx.x == 0) {
-      refused.token[count] = x;
-      refused.r_by[count] = sum.r > 0.0 ? 1.0 / sum.r : 0.0;
-      refused.q_by[count] = sum.q > 0.0 ? 1.0 / sum.q : 0.0;
+    if constexpr (DRAFT) {
+      const double sb = rb + qc;
+      pass(ra, sb);
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        w[g] = fmax(r[g] - q_now[g], 0.0);
+        if (x[g] == xk) q_all[g] = 0.0;
+      }
+      const double left = total(0) + over([&](int g) { return w[g]; });
+      const double rest = total(1) + over([&](int g) { return q_all[g]; });
+      undivided = left > 0.0;
+      if (undivided) {
+        ra /= left;
+        rb = sb / left;
+      }
+      qc = rest > 0.0 ? 1.0 / rest : 0.0;
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        if (undivided) r[g] = w[g] / left;
+        q_now[g] = q_all[g] * qc;
+      }
+    } else {
+      if (!have) pass(1.0, 0.0);
+      const double left = ra * total(0) + over([&](int g) { return x[g] == xk ? 0.0 : r[g]; });
+      if (left > 0.0) {
+        ra /= left;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) r[g] = x[g] == xk ? 0.0 : r[g] / left;
+      }
     }
-    last = sum.r > 0.0 ? x : -1;
-    total = sum.r;
-    ++count;
   }
-  __syncthreads();
-  // The token that follows: from r as it is.  Where the last refusal left something, its sums are at hand: r is what was left, not yet divided.
-  const int before = last >= 0 ? count - 1 : count;
-  auto weight = [&](int v, float r0, float q0, bool near) {
-    const Weights w = weights<DRAFT>(refused, before, v, r0, q0, near);
-    return last >= 0 ? left_of<DRAFT>(w, near && v == last) : w.r;
+  // The token that follows: from r, in the units of the parts where those are at hand.
+  if (DRAFT && !undivided) have = false;
+  if (!have) pass(ra, rb);
+  const double by = DRAFT && pb != 0.0 ? 1.0 : ra;    // of the parts
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    if (!(DRAFT && undivided)) w[g] = r[g];
+    if (wave == 0 && g < groups && x[g] >= 0) weights[g * kWave + lane] = w[g];
+  }
+  // ... with the children's tokens in the parts that they lie in
+  auto with_children = [&](int b, int e) { return over([&](int g) { return x[g] >= b && x[g] < e ? w[g] : 0.0; }); };
+  {
+    const double mine = parts[0][wave] * by + with_children(from, to);
+    __syncthreads();
+    if (lane == 0) parts[0][wave] = mine;
+    __syncthreads();
+  }
+  const double goal = (double)a.u[tree.first] * total(0);
+  auto weights_of = [&](int b, int e, auto f) {
+    if (DRAFT && pb != 0.0) walk_tokens<T, DRAFT>(p, q, a.vocab, b, e, marks, kids.token, count, [&](int v, float r0, float q0) { f(v, fmax(pa * (double)r0 - pb * (double)q0, 0.0)); });
+    else walk_tokens<T, false>(p, q, a.vocab, b, e, marks, kids.token, count, [&](int v, float r0, float) { f(v, ra * (double)r0); });
   };
-  if (last < 0) total = sums(before, -1, [&](int v, float r0, float q0, bool near, double& r, double&) { r += weight(v, r0, q0, near); }).r;
-  const double goal = (double)a.u[tree.first] * total;
   // The part in which the running sum passes the goal, the share of it, and the token: where rounding lets none pass, the last that is above 0.
   int begin = 0, size = part;
   double sum = 0.0;
   for (int level = 0; level < 2; ++level) {
     int pick = -1;
     double at = sum;
-    for (int w = 0; w < kVerifyWaves; ++w) {
-      const double mine = parts[0][w];
-      if (mine > 0.0 && (pick < 0 || at <= goal)) { pick = w; sum = at; }
+    for (int i = 0; i < kVerifyWaves; ++i) {
+      const double mine = parts[0][i];
+      if (mine > 0.0 && (pick < 0 || at <= goal)) { pick = i; sum = at; }
       at += mine;
       if (at > goal && pick >= 0) break;
     }
@@ -206,8 +318,8 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
     size = ceil_div_d(ceil_div_d(size, kVerifyWaves), kBatch) * kBatch;
     double mine = 0.0;
     const int b = min(begin + wave * size, limit), e = min(b + size, limit);
-    walk_tokens<T, DRAFT>(p, q, a.vocab, b, e, refused, before, last, [&](int v, float r0, float q0, bool near) { mine += weight(v, r0, q0, near); });
-    mine = wave_sum(mine);
+    weights_of(b, e, [&](int, double v) { mine += v; });
+    mine = wave_sum(mine) + with_children(b, e);
     __syncthreads();
     if (lane == 0) parts[0][wave] = mine;
     __syncthreads();
@@ -217,13 +329,18 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
   int best = -1;
   for (int b = begin; b < end; b += kBatch) {
     constexpr int kCount = Loaded<T>::kCount;
-    double w[kCount] = {}, mine = 0.0;
-    walk_tokens<T, DRAFT>(p, q, a.vocab, b, min(b + kBatch, end), refused, before, last, [&](int v, float r0, float q0, bool near) {
-      const double x = weight(v, r0, q0, near);
+    double each[kCount] = {}, mine = 0.0;
+    const int v0 = b + lane * kCount;
+    weights_of(b, min(b + kBatch, end), [&](int v, double x) {
 #pragma unroll
-      for (int i = 0; i < kCount; ++i) w[i] = v == b + lane * kCount + i ? x : w[i];
-      mine += x;
+      for (int i = 0; i < kCount; ++i) each[i] = v == v0 + i ? x : each[i];
     });
+    if (marks >> (b / kBatch % 64) & 1)
+      for (int j = 0; j < count; ++j)
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) each[i] += kids.token[j] == v0 + i ? weights[j] : 0.0;
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) mine += each[i];
     double upto = mine;                  // of the lanes up to this one
 #pragma unroll
     for (int d = 1; d < kWave; d *= 2) {
@@ -235,9 +352,9 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
     int first = a.vocab, above = -1;     // the lane's first token that passes the goal, its last above 0
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
-      at += w[i];
-      if (w[i] > 0.0) {
-        above = b + lane * kCount + i;
+      at += each[i];
+      if (each[i] > 0.0) {
+        above = v0 + i;
         if (at > goal && first == a.vocab) first = above;
       }
     }

@@ -397,6 +397,23 @@ def test_verify_by_hand(h):
     assert verified(h, [[-1, 0, 0, 0]], i32([0, 0, 0, 2]), u(.9, .9, .9, .7), rows_of([.5, .2, .3], [1, 0, 0], [1, 0, 0], [0, 0, 1]), rows_of([.9, .05, .05], [1, 0, 0], [1, 0, 0], [1, 0, 0]))
 
 
+def test_verify_rows_that_are_not_asked(h):
+    """The draft's rows of nodes without children may hold anything, as may both rows of nodes that no first child's way leads to."""
+    gen = torch.Generator(device="cuda").manual_seed(78)
+    trees = [grown(20, 79), grown(9, 80), [-1], list(range(-1, 7))]
+    for noise in (0.1, 2.0):
+        target, draft, ids, u = drawn(gen, trees, 3001, F32, noise=noise)
+        want = verified(h, trees, ids, u, target, draft)
+        base = 0
+        for parent in trees:
+            for i in range(len(parent)):
+                if i not in parent:
+                    draft[base + i] = (math.inf, math.nan)[i % 2]
+            base += len(parent)
+        got = dr.verify(h, planned(h, trees), ids, u, target, draft)
+        assert [t.tolist() for t in got] == list(want)
+
+
 def test_verify_last_number(h):
     """u just below 1 gives the last token above 0, u = 0 the first, in rows with zeros at both ends."""
     for vocab in (50, 5000, 70001):
