@@ -16,7 +16,8 @@ struct TreeView {
   int rows, most, words;          // words: of 64 bits, that a node's ancestors take
   int64_t tokens;
   unsigned long long* up;         // [tokens][words]: the node's ancestors and itself
-  int4* node;                     // [tokens]: parent, first child, next node of the same parent (each -1: none), depth
+  int4* node;                     // [tokens]: parent and first child (-1: none), the first child of the parent, depth
+  int4* place;                    // [tokens]: the first of the node's tree, how many it has (0: a node of none), its sequence
 };
 
 struct Tree { int64_t first; int n; };
@@ -31,9 +32,11 @@ __device__ __forceinline__ Tree tree_of(const TreeView& t, int s) {
 
 // ---- structure --------------------------------------------------------------------------------
 
-// A workgroup has a tree: a thread walks up from its node through the parents in LDS, and looks through all nodes for its first child and its next sibling.
+// A workgroup has a tree.  A node's ancestors are found by doubling: it takes over what the node that it points to has, and then points to where that one points; a tree of depth d is done
+// after log d rounds.  48 trees of up to 26 nodes XX us.
 __global__ void __launch_bounds__(kMostNodes) k_trees(TreeView t, const int32_t* parent) {
-  __shared__ int par[kMostNodes];
+  __shared__ int jump[kMostNodes], child[kMostNodes];
+  __shared__ unsigned long long ups[kNodeWords][kMostNodes];
   const Tree tree = tree_of(t, blockIdx.x);
   const int i = threadIdx.x;
   int p = -1;
@@ -41,26 +44,42 @@ __global__ void __launch_bounds__(kMostNodes) k_trees(TreeView t, const int32_t*
     p = parent[tree.first + i];
     p = p >= 0 && p < i ? p : -1;
   }
-  par[i] = p;
+  unsigned long long up[kNodeWords];
+#pragma unroll
+  for (int w = 0; w < kNodeWords; ++w) ups[w][i] = up[w] = i / 64 == w ? 1ull << (i % 64) : 0ull;
+  int to = p;
+  jump[i] = p;
+  child[i] = kMostNodes;
   __syncthreads();
+  if (p >= 0) atomicMin(&child[p], i);      // (a minimum is the same in any order)
+  while (__syncthreads_or(to >= 0)) {
+    int next = -1;
+    if (to >= 0) {
+#pragma unroll
+      for (int w = 0; w < kNodeWords; ++w)
+        if (w < t.words) up[w] |= ups[w][to];
+      next = jump[to];
+    }
+    __syncthreads();
+    to = next;
+    jump[i] = to;
+#pragma unroll
+    for (int w = 0; w < kNodeWords; ++w) ups[w][i] = up[w];
+  }
+  // nodes that no tree has: those behind a tree's `most` first, and what ptr leaves out in front and behind
+  const int64_t begin = blockIdx.x == 0 ? 0 : tree.first, end = (int)blockIdx.x == t.rows - 1 ? t.tokens : tree_begin(t, blockIdx.x + 1);
+  for (int64_t x = begin + i; x < end; x += kMostNodes)
+    if (x < tree.first || x >= tree.first + tree.n) t.place[x] = make_int4(0, 0, 0, 0);
   if (i >= tree.n) return;
-  unsigned long long up[kNodeWords] = {};
   int depth = -1;
-  for (int a = i; a >= 0; a = par[a]) {
-    ++depth;
 #pragma unroll
-    for (int w = 0; w < kNodeWords; ++w) up[w] |= a / 64 == w ? 1ull << (a % 64) : 0ull;
-  }
-  int child = -1, next = -1;
-  for (int j = tree.n - 1; j > 0; --j) {
-    const int pj = par[j];
-    child = pj == i ? j : child;
-    next = j > i && pj == p ? j : next;
-  }
-  t.node[tree.first + i] = make_int4(p, child, next, depth);
-#pragma unroll
-  for (int w = 0; w < kNodeWords; ++w)
+  for (int w = 0; w < kNodeWords; ++w) {
+    depth += __popcll(up[w]);
     if (w < t.words) t.up[(tree.first + i) * t.words + w] = up[w];
+  }
+  const int first = child[i];
+  t.node[tree.first + i] = make_int4(p, first < kMostNodes ? first : -1, p >= 0 ? child[p] : i, depth);
+  t.place[tree.first + i] = make_int4((int)tree.first, tree.n, (int)blockIdx.x, 0);
 }
 
 // Is anything wrong with the trees?  One workgroup looks at all of them.
@@ -141,60 +160,159 @@ __device__ __forceinline__ Seen seen_nodes(const unsigned long long* up, int wor
   return r;
 }
 
+// ... and of a page's first `upto` tokens, which lie before the tree, those from `from` on.  (Of keys before the sequence's first there is no page: where ctx is below 0, the first page's bits begin with a later node.)
+__device__ __forceinline__ unsigned long long seen_context(int upto, int from) {
+  from = min(max(from, 0), kPage);
+  return (upto >= kPage ? ~0ull : (1ull << upto) - 1) & (from == kPage ? 0ull : ~0ull << from);
+}
+
 constexpr float kTreeLazy = 3.0f;      // probabilities stay below 2^3 times those of the maximum that the sums are in units of ...
 constexpr int kTreeShift = 12;         // ... and are operands 2^12 times as large: at most 2^15, in full digits down to 2^-26
 constexpr int kUnitRoom = 6;           // a page's scale may be so much smaller than the sums' unit (powers of two) before that changes
 
-// A workgroup has `chunk` pages of a sequence, a key head and up to 128 rows.  With at most 32 rows its four waves take the pages in turn, with at most 64 two pairs of them, else each has its own rows; waves of
-// the same rows are joined in LDS.  The second product is in float16 whatever the type: e4m3 values are exact in it, and probabilities keep 11 digits instead of bfloat16's 8.
+// 32 rows of a wave: what a lane knows of its row (column lane % 32 of the products) and has summed up of it.
 template <typename T, int R, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, 2) k_tree_attend(TreeAttendArgs a) {
-  constexpr int kSteps = R / 16, kBlocks = R / 32;
-  const int lane = lane_id(), half = lane >> 5, col = lane & 31, wave = uniform(threadIdx.x / kWave);
-  // tiles of the same pages go to one die, one after the other: its L2 cache then has the pages for all of them
-  const unsigned die = blockIdx.x % 8, turn = blockIdx.x / 8;
-  const int tile = turn % a.tiles;
-  const int64_t unit_no = (int64_t)(turn / a.tiles) * 8 + die;
-  const int kv = (int)(unit_no % a.c.heads);
-  const int64_t slot = unit_no / a.c.heads;
-  if (slot >= a.slots) return;
-  const int s = uniform(find_seq(a.t.seqs, slot, [&](int i) { return first_page(a.t, i) / a.chunk + i; }));
-  const TreePages sp = tree_pages(a, s);
-  const int rows = uniform(min(sp.tree.n * a.group - tile * kTreeRows, kTreeRows));
-  const int64_t piece = slot - (sp.at / a.chunk + s);
-  if (rows <= 0 || piece < 0 || piece * a.chunk >= sp.last) return;
-  const int begin = uniform(max(sp.first, (int)piece * a.chunk)), end = uniform(min(sp.last, (int)(piece + 1) * a.chunk));
-  if (begin >= end) return;
-  const bool alone = sp.first / a.chunk == (sp.last - 1) / a.chunk;    // nothing to join with
-  const int blocks = rows <= 32 ? 1 : rows <= 64 ? 2 : 4, turns = 4 / blocks;      // blocks of rows; waves that take the pages of one in turn
-  const int block = wave % blocks;
+struct TreeRows {
+  static constexpr int kBlocks = R / 32;
+  f32x16 acc[kBlocks];             // channels 32 j + 8 (i / 4) + 4 half + i % 4, in units of 2^(unit - 127 - kTreeShift)
+  float m, l;                      // what the sums are in units of (log 2), the probabilities' sum
+  int unit, most;                  // the largest exponent of a scale of values so far
+  float scale2, cap2, slope2;
+  int diag, row_lo;                // where the node stands, the first of the context's tokens that it sees
+  int64_t token;                   // its row
 
-  const int r = block * 32 + col, rr = tile * kTreeRows + r, node = rr / a.group, head = kv * a.group + rr % a.group;
-  const bool real = r < rows;
-  const int64_t token = sp.tree.first + (real ? node : 0);
-  vec8<T> q[kSteps];
-  {
-    const RowSource src = a.q.of(real ? head : 0);
-    const unsigned char* p = src.base + token * src.stride;
+  __device__ __forceinline__ void begin(const TreeAttendArgs& a, const TreePages& sp, int64_t token_, int head, bool real) {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int d = 32 * (i / 2) + 16 * half + 8 * (i % 2);
-      u32x4 w = {0, 0, 0, 0};
-      if (real && d < a.c.bytes8) w = *reinterpret_cast<const u32x4*>(p + d * 2);
-      q[i] = __builtin_bit_cast(vec8<T>, w);
-    }
+    for (int j = 0; j < kBlocks; ++j) acc[j] = f32x16{};
+    m = -INFINITY;
+    l = 0.0f;
+    unit = most = 0;
+    token = token_;
+    scale2 = CAP ? a.score.scale / a.score.cap * (2.0f * kLog2e) : a.score.scale * kLog2e;
+    cap2 = a.score.cap * kLog2e;
+    slope2 = BIAS && real ? a.score.slopes[head] * kLog2e : 0.0f;
+    diag = sp.ctx + (real ? a.trees.node[token].w : 0);
+    row_lo = a.window ? diag - a.window + 1 : 0;
   }
-  const float scale2 = CAP ? a.score.scale / a.score.cap * (2.0f * kLog2e) : a.score.scale * kLog2e, cap2 = a.score.cap * kLog2e;
-  const float slope2 = BIAS && real ? a.score.slopes[head] * kLog2e : 0.0f;
-  const int diag = sp.ctx + (real ? a.trees.node[token].w : 0);                     // where the node stands
-  const int row_lo = a.window ? diag - a.window + 1 : 0;
-  const int last_lo = a.window ? sp.ctx + sp.tree.n - a.window : 0;                 // no node's window begins behind it
 
-  f32x16 acc[kBlocks];
+  // From the products q.k of a page's keys to its probabilities.  x[t][i] is key H half + 32 t + i (H 16) or 32 t + 16 (i / 8) + i % 8 (H 8) of the page; p[2 t + i / 8][i % 8] becomes its probability, as an
+  // operand.
+  template <int H>
+  static __device__ __forceinline__ constexpr int key(int t, int i) { return H == 16 ? 32 * t + i : 32 * t + 16 * (i / 8) + i % 8; }
+  template <int H>
+  __device__ __forceinline__ void weigh(const TreeAttendArgs& a, const TreePages& sp, f32x16 (&x)[2], int k0, bool whole, float ks, float vs, int half, vec8<f16_t> (&p)[4]) {
+    const float c = fmaxf(scale2 * ks, 1.17549435e-38f);      // (above 0: what is not seen is -inf times it)
+    float unit2 = c;                                            // of x, in units of log 2
+    if constexpr (CAP || BIAS) {
+      unit2 = BIAS ? 1.0f : cap2;
 #pragma unroll
-  for (int j = 0; j < kBlocks; ++j) acc[j] = f32x16{};
-  float m = -INFINITY, l = 0.0f;                   // what the sums are in units of (log 2), the probabilities' sum
-  int unit = 0, most = 0;                          // acc is in units of 2^(unit - 127 - kTreeShift); the largest exponent of a scale of values so far
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float y = x[t][i] * c;
+          if constexpr (CAP) y = tanh_of(y);
+          if constexpr (CAP && BIAS) y *= cap2;
+          x[t][i] = y;
+        }
+    }
+    if (whole) {
+      if constexpr (BIAS) {
+        const float away = (float)(diag - k0 - H * half);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[t][i] -= slope2 * (away - (float)key<H>(t, i));
+      }
+    } else {
+      const Seen nodes = seen_nodes(a.trees.up + token * a.trees.words, a.trees.words, k0 - sp.ctx, a.window);
+      const int upto = min(max(sp.ctx - k0, 0), kPage);
+      const unsigned long long mine = (seen_context(upto, row_lo - k0) | nodes.bits) >> (H * half), own = nodes.bits >> (H * half);
+      const unsigned lo = (unsigned)mine, hi = (unsigned)(mine >> 32), own_lo = (unsigned)own, own_hi = (unsigned)(own >> 32);
+      const int context = upto - H * half, away = diag - k0 - H * half;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int b = key<H>(t, i);
+          const bool sees = (b < 32 ? lo : hi) >> (b % 32) & 1;
+          if constexpr (BIAS) {
+            // nodes between: those of the ancestors that come behind the key
+            const unsigned above = b % 32 == 31 ? 0u : ~0u << (b % 32 + 1);
+            const int between = nodes.above + (b < 32 ? __popc(own_lo & above) + __popc(own_hi) : __popc(own_hi & above));
+            x[t][i] -= slope2 * (float)(b < context ? away - b : between);
+          }
+          x[t][i] = sees ? x[t][i] : -INFINITY;
+        }
+    }
+    float top = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(x[0][i], x[1][i]));
+    top = max_halves(top) * unit2;
+    // The sums go to a new unit only where some row's maximum has grown by more than 2^3, or the page's scale is larger than the unit or much smaller.  Not further down than 2^-64 of the
+    // largest scale so far: a page of zeros has the scale 2^-100, next to which sums of large values would overflow.
+    const int exponent = uniform((int)(__float_as_uint(vs) >> 23));
+    most = max(most, exponent);
+    const bool other = exponent > unit || exponent < unit - kUnitRoom;
+    if (other || __any(top > m + kTreeLazy)) {
+      const float now = top > m + kTreeLazy ? top : m;                            // (a row's own: what its neighbours hold changes none of its bits)
+      const float by = m == now ? 1.0f : fast_exp2(m - now);
+      const int new_unit = other ? max(exponent, most - 64) : unit, shift = unit - new_unit;
+      m = now;
+      unit = new_unit;
+      l *= by;
+#pragma unroll
+      for (int j = 0; j < kBlocks; ++j)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[j][i] = __builtin_amdgcn_ldexpf(acc[j][i] * by, shift);
+    }
+    const int below = max(exponent - unit, -40);                                  // 0 and less; what lies further down only the sum of probabilities shows
+    const float base = (m == -INFINITY ? 0.0f : m) - (float)(kTreeShift + below);
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = fast_exp2(__builtin_fmaf(x[t][i], unit2, -base));
+        sum += e;
+        p[2 * t + i / 8][i % 8] = (f16_t)e;
+      }
+    if (exponent - unit < below)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) p[u] = vec8<f16_t>{};
+    l += __builtin_amdgcn_ldexpf(sum, -kTreeShift - below);
+  }
+};
+
+// Which bytes of a word of four tokens from `off` on lie from lo to before len.
+__device__ __forceinline__ unsigned live_bytes(int off, int lo, int len) {
+  unsigned mask = 0;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) mask |= off + b >= lo && off + b < len ? 0xffu << (8 * b) : 0u;
+  return mask;
+}
+// The highest bit of every byte that is NaN (0x7f, 0xff).
+__device__ __forceinline__ unsigned nan_bytes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// Values of a page that some rows do not see as a whole: the product multiplies all of them, by 0 where a row does not see them, so what is NaN becomes 0; the rows that see it become NaN in the end.
+__device__ __forceinline__ unsigned proper_bytes(unsigned w, bool& strange) {
+  const unsigned nan = nan_bytes(w);
+  strange |= nan != 0;
+  return w & ~((nan >> 7) * 0xffu);
+}
+
+// Where a workgroup is: its sequence, its pages begin .. end - 1, its rows.
+struct TreePlace {
+  TreePages sp;
+  int64_t slot;
+  int kv, tile, begin, end, rows;
+};
+
+// At most 64 rows: the four waves take the pages in turn (with more than 32 rows two pairs of them do), each page from memory to registers, and are joined in LDS.
+template <typename T, int R, bool CAP, bool BIAS>
+__device__ __forceinline__ bool tree_few_rows(const TreeAttendArgs& a, const TreePlace& at, TreeRows<T, R, CAP, BIAS>& rows, int block, int blocks, const vec8<T>* q) {
+  constexpr int kSteps = R / 16, kBlocks = R / 32;
+  const TreePages& sp = at.sp;
+  const int lane = lane_id(), half = lane >> 5, col = lane & 31, wave = uniform(threadIdx.x / kWave), turns = 4 / blocks;
+  const int last_lo = a.window ? sp.ctx + sp.tree.n - a.window : 0;                 // no node's window begins behind it
   u32x4 kw[2][kBlocks], vw[kBlocks][2];
 
   auto page_of = [&](int n) {
@@ -203,28 +321,29 @@ __global__ void __launch_bounds__(256, 2) k_tree_attend(TreeAttendArgs a) {
   };
   const int key = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
   auto load_k = [&](int64_t page) {
-    const unsigned char* p = a.c.k + (page * a.c.heads + kv) * (kPage * R) + key * R + 16 * half;
+    const unsigned char* p = a.c.k + (page * a.c.heads + at.kv) * (kPage * R) + key * R + 16 * half;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < kBlocks; ++i) kw[t][i] = *reinterpret_cast<const u32x4*>(p + 32 * t * R + 32 * i);
   };
   auto load_v = [&](int64_t page) {
-    const unsigned char* p = a.c.v + (page * a.c.heads + kv) * (kPage * R) + col * kPage + 16 * half;
+    const unsigned char* p = a.c.v + (page * a.c.heads + at.kv) * (kPage * R) + col * kPage + 16 * half;
 #pragma unroll
     for (int j = 0; j < kBlocks; ++j)
 #pragma unroll
       for (int t = 0; t < 2; ++t) vw[j][t] = *reinterpret_cast<const u32x4*>(p + 32 * j * kPage + 32 * t);
   };
 
-  int n = block * 32 < rows ? begin + wave / blocks : end;
-  int64_t page = n < end ? page_of(n) : -1;
+  bool strange = false;
+  int n = block * 32 < at.rows ? at.begin + wave / blocks : at.end;
+  int64_t page = n < at.end ? page_of(n) : -1;
   if (page >= 0) { load_k(page); load_v(page); }
-  while (n < end) {
+  while (n < at.end) {
     const int next = n + turns;
-    const int64_t next_page = next < end ? page_of(next) : -1;
+    const int64_t next_page = next < at.end ? page_of(next) : -1;
     if (page >= 0) {
-      const float ks = load_uniform(a.c.k_scale + page * a.c.heads + kv), vs = load_uniform(a.c.v_scale + page * a.c.heads + kv);
+      const float ks = load_uniform(a.c.k_scale + page * a.c.heads + at.kv), vs = load_uniform(a.c.v_scale + page * a.c.heads + at.kv);
       if (a.c.bytes8 < R) {                        // channels behind the head's may hold anything, and 0 times NaN is NaN
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
@@ -242,143 +361,23 @@ __global__ void __launch_bounds__(256, 2) k_tree_attend(TreeAttendArgs a) {
       }
       if (next_page >= 0) load_k(next_page);
       const int k0 = n * kPage;
-      const float c = fmaxf(scale2 * ks, 1.17549435e-38f);      // (above 0: what is not seen is -inf times it)
-      float unit2 = c;                              // of x, in units of log 2
-      if constexpr (CAP || BIAS) {
-        unit2 = BIAS ? 1.0f : cap2;
+      const bool whole = k0 + kPage <= sp.ctx && k0 >= last_lo;
+      vec8<f16_t> p[4];
+      rows.template weigh<16>(a, sp, x, k0, whole, ks, vs, half, p);
+      if (!whole) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float y = x[t][i] * c;
-            if constexpr (CAP) y = tanh_of(y);
-            if constexpr (CAP && BIAS) y *= cap2;
-            x[t][i] = y;
-          }
-      }
-      const bool whole = k0 + kPage <= sp.ctx && k0 >= last_lo;
-      unsigned seen[2] = {0xffffu, 0xffffu};        // of the lane's keys 32 t + 16 half + i
-      if (whole) {
-        if constexpr (BIAS) {
-          const float away = (float)(diag - k0 - 16 * half);
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[t][i] -= slope2 * (away - (float)(32 * t + i));
-        }
-      } else {
-        const Seen nodes = seen_nodes(a.trees.up + token * a.trees.words, a.trees.words, k0 - sp.ctx, a.window);
-        const int upto = min(max(sp.ctx - k0, 0), kPage), from = min(max(row_lo - k0, 0), kPage);
-        const unsigned long long before = upto == kPage ? ~0ull : (1ull << upto) - 1, behind = from == kPage ? 0ull : ~0ull << from;
-        // (keys before the sequence's first are never asked for: a node's bits begin at ctx, which is below 0 only where k0 is 0)
-        const unsigned long long bits = (before & behind) | (upto == kPage ? 0ull : nodes.bits >> upto << upto);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          seen[t] = (unsigned)(bits >> (32 * t + 16 * half)) & 0xffffu;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            if constexpr (BIAS) {
-              const int b = 32 * t + 16 * half + i;
-              const int far = b < upto ? diag - k0 - b : nodes.above + __popcll(b == 63 ? 0ull : nodes.bits >> (b + 1));
-              x[t][i] -= slope2 * (float)far;
-            }
-            x[t][i] = seen[t] >> i & 1 ? x[t][i] : -INFINITY;
-          }
-        }
-        // what no row of the sequence sees may hold anything: as values it becomes zero
-        unsigned strange = 0;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const int off = k0 + 32 * t + 16 * half, dead = sp.lo - off, live = sp.len - off;       // keys below dead and from live on
-#pragma unroll
           for (int w = 0; w < 4; ++w) {
-            unsigned mask = 0;
+            const unsigned live = live_bytes(k0 + 32 * t + 16 * half + 4 * w, sp.lo, sp.len);
 #pragma unroll
-            for (int b = 0; b < 4; ++b) mask |= 4 * w + b >= dead && 4 * w + b < live ? 0xffu << (8 * b) : 0u;
-#pragma unroll
-            for (int j = 0; j < kBlocks; ++j) {
-              vw[j][t][w] &= mask;
-              strange |= ((vw[j][t][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-            }
+            for (int j = 0; j < kBlocks; ++j) vw[j][t][w] = proper_bytes(vw[j][t][w] & live, strange);
           }
-        }
-        // a NaN among the values (0x7f, 0xff) reaches the rows that see it and no others, though the product multiplies it by the zeros of all: it is taken
-        // out, and a product of what is seen with 1 in its place says whose results it makes NaN
-        if (__any(strange != 0)) {
-          vec8<f16_t> sees[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sees[u][i] = seen[u / 2] >> (8 * (u % 2) + i) & 1 ? (f16_t)1.0f : (f16_t)0.0f;
-#pragma unroll
-          for (int j = 0; j < kBlocks; ++j) {
-            f32x16 hit = {};
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              vec8<f16_t> is;
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const unsigned w = vw[j][u / 2][2 * (u % 2) + i / 4];
-                is[i] = (w >> (8 * (i % 4)) & 0x7fu) == 0x7fu ? (f16_t)1.0f : (f16_t)0.0f;
-              }
-              hit = mma(is, sees[u], hit);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[j][i] = hit[i] > 0.0f ? NAN : acc[j][i];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                const unsigned nan = ((vw[j][t][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;      // its byte's highest bit
-                vw[j][t][w] &= ~((nan >> 7) * 0xffu);
-              }
-          }
-        }
       }
-      float top = max3(x[0][0], x[0][1], x[0][2]);
-#pragma unroll
-      for (int i = 3; i < 15; i += 2) top = fmaxf(top, fmaxf(x[0][i], x[0][i + 1]));
-      top = fmaxf(top, x[0][15]);
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) top = fmaxf(top, fmaxf(x[1][i], x[1][i + 1]));
-      top = max_halves(top) * unit2;
-      // The sums go to a new unit only where some row's maximum has grown by more than 2^3, or the page's scale is larger than the unit or much smaller.  Not further down than 2^-64 of the
-      // largest scale so far: a page of zeros has the scale 2^-100, next to which sums of large values would overflow.
-      const int exponent = uniform((int)(__float_as_uint(vs) >> 23));
-      most = max(most, exponent);
-      const bool other = exponent > unit || exponent < unit - kUnitRoom;
-      if (other || __any(top > m + kTreeLazy)) {
-        const float now = top > m + kTreeLazy ? top : m;                            // (a row's own: what its neighbours hold changes none of its bits)
-        const float by = m == now ? 1.0f : fast_exp2(m - now);
-        const int new_unit = other ? max(exponent, most - 64) : unit, shift = unit - new_unit;
-        m = now;
-        unit = new_unit;
-        l *= by;
-#pragma unroll
-        for (int j = 0; j < kBlocks; ++j)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[j][i] = __builtin_amdgcn_ldexpf(acc[j][i] * by, shift);
-      }
-      const int below = max(exponent - unit, -40);                                  // 0 and less; what lies further down only the sum of probabilities shows
-      const float base = (m == -INFINITY ? 0.0f : m) - (float)(kTreeShift + below);
-      vec8<f16_t> p[4];
-      float sum = 0.0f;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float e = fast_exp2(__builtin_fmaf(x[t][i], unit2, -base));
-          sum += e;
-          p[2 * t + i / 8][i % 8] = (f16_t)e;
-        }
-      if (exponent - unit < below)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) p[u] = vec8<f16_t>{};
-      l += __builtin_amdgcn_ldexpf(sum, -kTreeShift - below);
 #pragma unroll
       for (int j = 0; j < kBlocks; ++j)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) acc[j] = mma(widen(u32x2{vw[j][u / 2][2 * (u % 2)], vw[j][u / 2][2 * (u % 2) + 1]}, f16_t()), p[u], acc[j]);
+        for (int u = 0; u < 4; ++u) rows.acc[j] = mma(widen(u32x2{vw[j][u / 2][2 * (u % 2)], vw[j][u / 2][2 * (u % 2) + 1]}, f16_t()), p[u], rows.acc[j]);
       if (next_page >= 0) load_v(next_page);
     } else if (next_page >= 0) {
       load_k(next_page);
@@ -387,40 +386,202 @@ __global__ void __launch_bounds__(256, 2) k_tree_attend(TreeAttendArgs a) {
     n = next;
     page = next_page;
   }
-  l = add_halves(l);
+  return strange;
+}
+
+// More than 64 rows: a wave has its own 32, and all go over the same pages.  A page is widened to 16 bits once, on its way to LDS, where the four waves read it; the next one's bytes come to registers
+// meanwhile.  Keys lie there in the order of the products' rows: row 16 c + 8 a + 4 h + b holds key 16 c + 8 h + 4 a + b, so that half h of the wave has 8 neighbouring keys of every 16, one read of a value's channel.
+template <typename T, int R>
+struct TreeTiles {
+  __align__(16) unsigned char k[2][kPage * R * 2], v[2][kPage * R * 2];
+};
+template <typename T, int R, bool CAP, bool BIAS>
+__device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const TreePlace& at, TreeRows<T, R, CAP, BIAS>& rows, const vec8<T>* q, TreeTiles<T, R>& tiles) {
+  using SK = TileShape<R>;
+  using SV = TileShape<64>;
+  constexpr int kSteps = R / 16, kBlocks = R / 32, kPieces = kPage * R / 16 / 256;        // 16 bytes of a page that a thread brings
+  const TreePages& sp = at.sp;
+  const int lane = lane_id(), half = lane >> 5, tid = threadIdx.x;
+  const int last_lo = a.window ? sp.ctx + sp.tree.n - a.window : 0;
+  u32x4 kw[kPieces], vw[kPieces];
+  auto page_of = [&](int n) {
+    const int64_t p = load_uniform(a.t.page + sp.at + n);
+    return p >= 0 && p < a.c.pages ? p : (int64_t)-1;
+  };
+  auto load = [&](int64_t page) {
+    const int64_t at0 = (page * a.c.heads + at.kv) * (kPage * R) + tid * 16;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      kw[i] = *reinterpret_cast<const u32x4*>(a.c.k + at0 + i * 4096);
+      vw[i] = *reinterpret_cast<const u32x4*>(a.c.v + at0 + i * 4096);
+    }
+  };
+  bool strange = false;
+  auto whole_page = [&](int n) { return n * kPage + kPage <= sp.ctx && n * kPage >= last_lo; };
+  auto store = [&](int n, int into) {
+    const bool whole = whole_page(n);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int piece = tid + 256 * i;
+      {
+        const int key = piece / (R / 16), chunk = piece % (R / 16) * 2, row = (key & 0x33) | (key & 4) << 1 | (key & 8) >> 1;
+        u32x4 w = kw[i];
+        if (a.c.bytes8 < R) {                        // channels behind the head's may hold anything, and 0 times NaN is NaN
+          if (chunk * 8 >= a.c.bytes8) w[0] = w[1] = 0;
+          if (chunk * 8 + 8 >= a.c.bytes8) w[2] = w[3] = 0;
+        }
+        unsigned char* to = tiles.k[into] + row * SK::kRowBytes;
+        *reinterpret_cast<vec8<T>*>(to + ((chunk ^ SK::swizzle(row)) << 4)) = widen(u32x2{w[0], w[1]}, T());
+        *reinterpret_cast<vec8<T>*>(to + (((chunk + 1) ^ SK::swizzle(row)) << 4)) = widen(u32x2{w[2], w[3]}, T());
+      }
+      {
+        const int channel = piece / 4, chunk = piece % 4 * 2;
+        u32x4 w = vw[i];
+        if (!whole) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w[j] = proper_bytes(w[j] & live_bytes(n * kPage + chunk * 8 + 4 * j, sp.lo, sp.len), strange);
+        }
+        unsigned char* to = tiles.v[into] + channel * SV::kRowBytes;
+        *reinterpret_cast<vec8<f16_t>*>(to + ((chunk ^ SV::swizzle(channel)) << 4)) = widen(u32x2{w[0], w[1]}, f16_t());
+        *reinterpret_cast<vec8<f16_t>*>(to + (((chunk + 1) ^ SV::swizzle(channel)) << 4)) = widen(u32x2{w[2], w[3]}, f16_t());
+      }
+    }
+  };
+  const int k_base = SK::row_base(lane), v_base = SV::row_base(lane);
+  int n = at.begin;
+  int64_t page = page_of(n);
+  if (page >= 0) { load(page); store(n, 0); }
+  for (int from = 0; n < at.end; ++n, from ^= 1) {
+    const int64_t next = n + 1 < at.end ? page_of(n + 1) : -1;
+    if (next >= 0) load(next);
+    __syncthreads();                                 // the page is there; the one before it is not read any more
+    if (page >= 0) {
+      const float ks = load_uniform(a.c.k_scale + page * a.c.heads + at.kv), vs = load_uniform(a.c.v_scale + page * a.c.heads + at.kv);
+      const unsigned char *kt = tiles.k[from], *vt = tiles.v[from];
+      f32x16 x[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        x[t] = f32x16{};
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) x[t] = mma(SK::template row<T>(kt, k_base, 32 * t, i), q[i], x[t]);
+      }
+      const bool whole = whole_page(n);
+      vec8<f16_t> p[4];
+      rows.template weigh<8>(a, sp, x, n * kPage, whole, ks, vs, half, p);
+#pragma unroll
+      for (int j = 0; j < kBlocks; ++j)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) rows.acc[j] = mma(SV::template row<f16_t>(vt, v_base, 32 * j, u), p[u], rows.acc[j]);
+    }
+    if (next >= 0) store(n + 1, from ^ 1);
+    page = next;
+  }
+  return strange;
+}
+
+// A workgroup has `chunk` pages of a sequence, a key head and up to 128 rows.  The second product is in float16 whatever the type: e4m3 values are exact in it, and probabilities keep 11 digits instead of bfloat16's 8.
+template <typename T, int R, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(256, 2) k_tree_attend(TreeAttendArgs a) {
+  constexpr int kSteps = R / 16, kBlocks = R / 32;
+  const int lane = lane_id(), half = lane >> 5, col = lane & 31, wave = uniform(threadIdx.x / kWave);
+  TreePlace at;
+  // tiles of the same pages go to one die, one after the other: its L2 cache then has the pages for all of them
+  const unsigned die = blockIdx.x % 8, turn = blockIdx.x / 8;
+  at.tile = turn % a.tiles;
+  const int64_t unit_no = (int64_t)(turn / a.tiles) * 8 + die;
+  at.kv = (int)(unit_no % a.c.heads);
+  at.slot = unit_no / a.c.heads;
+  if (at.slot >= a.slots) return;
+  const int s = uniform(find_seq(a.t.seqs, at.slot, [&](int i) { return first_page(a.t, i) / a.chunk + i; }));
+  at.sp = tree_pages(a, s);
+  const TreePages& sp = at.sp;
+  at.rows = uniform(min(sp.tree.n * a.group - at.tile * kTreeRows, kTreeRows));
+  const int64_t piece = at.slot - (sp.at / a.chunk + s);
+  if (at.rows <= 0 || piece < 0 || piece * a.chunk >= sp.last) return;
+  at.begin = uniform(max(sp.first, (int)piece * a.chunk));
+  at.end = uniform(min(sp.last, (int)(piece + 1) * a.chunk));
+  if (at.begin >= at.end) return;
+  const bool alone = sp.first / a.chunk == (sp.last - 1) / a.chunk;    // nothing to join with
+  const int blocks = at.rows <= 32 ? 1 : at.rows <= 64 ? 2 : 4;        // blocks of rows
+  const int block = wave % blocks;
+
+  const int r = block * 32 + col, rr = at.tile * kTreeRows + r, head = at.kv * a.group + rr % a.group;
+  const bool real = r < at.rows;
+  const int64_t token = sp.tree.first + (real ? rr / a.group : 0);
+  TreeRows<T, R, CAP, BIAS> rows;
+  rows.begin(a, sp, token, head, real);
+  vec8<T> q[kSteps];
+  {
+    const RowSource src = a.q.of(real ? head : 0);
+    const unsigned char* p = src.base + token * src.stride;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int d = blocks == 4 ? 16 * i + 8 * half : 32 * (i / 2) + 16 * half + 8 * (i % 2);
+      u32x4 w = {0, 0, 0, 0};
+      if (real && d < a.c.bytes8) w = *reinterpret_cast<const u32x4*>(p + d * 2);
+      q[i] = __builtin_bit_cast(vec8<T>, w);
+    }
+  }
+  struct Joined { float ms[4][32], ls[4][32]; __align__(16) float sums[4][32][R + 4]; };
+  __shared__ __align__(16) union { TreeTiles<T, R> tiles; Joined joined; } lds;
+  bool strange;
+  if (blocks == 4) strange = tree_many_rows<T, R, CAP, BIAS>(a, at, rows, q, lds.tiles);
+  else strange = tree_few_rows<T, R, CAP, BIAS>(a, at, rows, block, blocks, q);
+  strange = __syncthreads_or(strange);             // (and the tiles are not read any more)
+  const float m = rows.m, l = add_halves(rows.l);
 
   // join the waves of the same rows by their maxima
-  __shared__ float ms[4][32], ls[4][32];
-  __shared__ __align__(16) float sums[4][32][R + 4];
-  if (half == 0) { ms[wave][col] = m; ls[wave][col] = l; }
+  Joined& j = lds.joined;
+  if (half == 0) { j.ms[wave][col] = m; j.ls[wave][col] = l; }
 #pragma unroll
-  for (int j = 0; j < kBlocks; ++j)
+  for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       f32x4 v;
 #pragma unroll
-      for (int b = 0; b < 4; ++b) v[b] = __builtin_amdgcn_ldexpf(acc[j][4 * i + b], unit - 127 - kTreeShift);
-      *reinterpret_cast<f32x4*>(&sums[wave][col][32 * j + 8 * i + 4 * half]) = v;
+      for (int b = 0; b < 4; ++b) v[b] = __builtin_amdgcn_ldexpf(rows.acc[c][4 * i + b], rows.unit - 127 - kTreeShift);
+      *reinterpret_cast<f32x4*>(&j.sums[wave][col][32 * c + 8 * i + 4 * half]) = v;
     }
   __syncthreads();
-  const int64_t cell = (slot * a.c.heads + kv) * a.tiles + tile;
-  for (int i = threadIdx.x; i < rows * (R / 4); i += 256) {
-    const int row = i / (R / 4), d = i % (R / 4) * 4, at = row % 32;
+  if (strange) {
+    // rows that see a value that is NaN: looked up element by element
+    for (int i = threadIdx.x; i < at.rows * R; i += 256) {
+      const int row = i / R, d = i % R, rt = at.tile * kTreeRows + row;
+      const int64_t its = sp.tree.first + rt / a.group;
+      const int stands = sp.ctx + a.trees.node[its].w;
+      for (int n = at.begin; n < at.end; ++n) {
+        const int64_t page = a.t.page[sp.at + n];
+        if (page < 0 || page >= a.c.pages) continue;
+        const int k0 = n * kPage;
+        const unsigned long long sees = seen_context(min(max(sp.ctx - k0, 0), kPage), a.window ? stands - a.window + 1 - k0 : 0) |
+                                        seen_nodes(a.trees.up + its * a.trees.words, a.trees.words, k0 - sp.ctx, a.window).bits;
+        const unsigned* v = reinterpret_cast<const unsigned*>(a.c.v + (page * a.c.heads + at.kv) * (kPage * R) + d * kPage);
+        for (int w = 0; w < kPage / 4; ++w) {
+          const unsigned bits = (unsigned)(sees >> (4 * w)) & 15u, nan = nan_bytes(v[w]) >> 7;
+          if (bits & ((nan & 1) | (nan >> 7 & 2) | (nan >> 14 & 4) | (nan >> 21 & 8))) j.sums[row / 32][row % 32][d] = NAN;
+        }
+      }
+    }
+    __syncthreads();
+  }
+  const int64_t cell = (at.slot * a.c.heads + at.kv) * a.tiles + at.tile;
+  for (int i = threadIdx.x; i < at.rows * (R / 4); i += 256) {
+    const int row = i / (R / 4), d = i % (R / 4) * 4, mine = row % 32;
     float top = -INFINITY;
-    for (int w = row / 32; w < 4; w += blocks) top = fmaxf(top, ms[w][at]);
+    for (int w = row / 32; w < 4; w += blocks) top = fmaxf(top, j.ms[w][mine]);
     const float base = top == -INFINITY ? 0.0f : top;
     f32x4 v = {0, 0, 0, 0};
     float sum = 0.0f;
     for (int w = row / 32; w < 4; w += blocks) {
-      const float f = fast_exp2(ms[w][at] - base);
-      v += *reinterpret_cast<const f32x4*>(&sums[w][at][d]) * f;
-      sum += ls[w][at] * f;
+      const float f = fast_exp2(j.ms[w][mine] - base);
+      v += *reinterpret_cast<const f32x4*>(&j.sums[w][mine][d]) * f;
+      sum += j.ls[w][mine] * f;
     }
     if (alone) {
       if (d < a.c.bytes8) {
         const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-        const int rt = tile * kTreeRows + row;
-        const RowSource dst = a.o.of(kv * a.group + rt % a.group);
+        const int rt = at.tile * kTreeRows + row;
+        const RowSource dst = a.o.of(at.kv * a.group + rt % a.group);
         T out[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) out[b] = (T)(v[b] * by);
@@ -440,15 +601,16 @@ __global__ void __launch_bounds__(256) k_tree_join(TreeAttendArgs a) {
   constexpr int kThreads = R / 4, kLanes = 256 / kThreads;
   const int64_t token = blockIdx.x;
   const int head = blockIdx.y, kv = head / a.group;
-  const int s = uniform(find_seq(a.trees.rows, token, [&](int i) { return tree_begin(a.trees, i); }));
-  const TreePages sp = tree_pages(a, s);
+  const int4 place = load_uniform(a.trees.place + token);
+  if (place.y == 0) return;
+  const TreePages sp = tree_pages(a, place.z);
   const int64_t node = token - sp.tree.first;
   if (node < 0 || node >= sp.tree.n) return;
   const bool none = sp.first >= sp.last;
   const int c0 = none ? 0 : sp.first / a.chunk, c1 = none ? 0 : (sp.last - 1) / a.chunk + 1;
   if (c1 - c0 == 1) return;
   const int rr = (int)node * a.group + head % a.group, d = threadIdx.x % kThreads * 4, mine = threadIdx.x / kThreads;
-  const int64_t slot = sp.at / a.chunk + s;
+  const int64_t slot = sp.at / a.chunk + place.z;
   float top = -INFINITY, sum = 0.0f;
   f32x4 v = {0, 0, 0, 0};
 #pragma unroll 4

@@ -21,8 +21,8 @@ struct VerifyArgs {
   int32_t *path, *kept, *next;
 };
 
-// A row of probabilities.  What is negative or NaN counts as 0.
-template <typename T> __device__ __forceinline__ float proper(T v) { return fmaxf((float)v, 0.0f); }
+// An entry of a row: what is negative or NaN counts as 0 (of three numbers one of which is NaN the instruction gives the smallest).
+template <typename T> __device__ __forceinline__ float proper(T v) { return __builtin_amdgcn_fmed3f((float)v, 0.0f, INFINITY); }
 
 template <typename T>
 struct Loaded {            // 16 bytes of a row, which may begin at any element
@@ -58,7 +58,7 @@ __device__ __forceinline__ bool first_taken(const VerifyArgs& a, int64_t parent,
 }
 
 // The sum of f(token, entry of p, entry of q) over a part of the rows, by one wave.  Tokens of children are left out: where a batch of tokens may hold one (a bit of `marks` for every
-// batch, of 64 in turn) each is compared.  Four batches' loads are on their way together.
+// batch, of 64 in turn) each is compared.  The loads of four batches are on their way while four others are used.
 constexpr int kInFlight = 4;
 template <typename T, bool DRAFT, typename F>
 __device__ __forceinline__ void walk_tokens(const T* p, const T* q, int vocab, int from, int to, unsigned long long marks, const int* children, int count, F each) {
@@ -78,16 +78,37 @@ __device__ __forceinline__ void walk_tokens(const T* p, const T* q, int vocab, i
       for (int i = 0; i < kCount; ++i) each(v0 + i, proper(r.v[i]), DRAFT ? proper(s.v[i]) : 0.0f);
     }
   };
-  int b = from;
-  for (; b + kInFlight * kBatch <= to; b += kInFlight * kBatch) {
-    Loaded<T> r[kInFlight], s[kInFlight];
+  Loaded<T> r[2][kInFlight], s[2][kInFlight];
+  auto fetch = [&](int n, int b) {
 #pragma unroll
     for (int i = 0; i < kInFlight; ++i) {
-      __builtin_memcpy(&r[i], p + b + i * kBatch + lane_id() * kCount, 16);
-      if constexpr (DRAFT) __builtin_memcpy(&s[i], q + b + i * kBatch + lane_id() * kCount, 16);
+      __builtin_memcpy(&r[n][i], p + b + i * kBatch + lane_id() * kCount, 16);
+      if constexpr (DRAFT) __builtin_memcpy(&s[n][i], q + b + i * kBatch + lane_id() * kCount, 16);
     }
+  };
+  auto use = [&](int n, int b) {
 #pragma unroll
-    for (int i = 0; i < kInFlight; ++i) batch(b + i * kBatch, r[i], s[i]);
+    for (int i = 0; i < kInFlight; ++i) batch(b + i * kBatch, r[n][i], s[n][i]);
+  };
+  constexpr int kStep = kInFlight * kBatch;
+  int b = from;
+  if (b + kStep <= to) {
+    fetch(0, b);
+    for (; b + 3 * kStep <= to; b += 2 * kStep) {
+      fetch(1, b + kStep);
+      use(0, b);
+      fetch(0, b + 2 * kStep);
+      use(1, b + kStep);
+    }
+    if (b + 2 * kStep <= to) {
+      fetch(1, b + kStep);
+      use(0, b);
+      use(1, b + kStep);
+      b += 2 * kStep;
+    } else {
+      use(0, b);
+      b += kStep;
+    }
   }
   for (; b < to; b += kBatch) {
     const Loaded<T> r = load_some(p, b + lane_id() * kCount, vocab);
@@ -103,7 +124,7 @@ struct Children {
   float p[kMostNodes], q[kMostNodes], u[kMostNodes];
 };
 
-// Both rows after some children were refused, as far as they are not at children's tokens: r = max(a P - b Q, 0), for max(max(x, 0) - c, 0) is max(x - c, 0) where c is not
+// Both rows after some children were refused, as far as they are not at children's tokens: r = a max(P - b Q, 0), for max(max(x, 0) - c, 0) is max(x - c, 0) where c is not
 // negative, and q = c Q.  So a pass takes the same few operations however many children were refused.  What r and q are at children's tokens every wave holds in registers.
 template <typename T, bool DRAFT>
 __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
@@ -113,8 +134,8 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
   __shared__ double parts[2][kVerifyWaves], weights[kMostNodes];
   const int64_t token = blockIdx.x;
   const int wave = uniform(threadIdx.x / kWave), lane = lane_id();
-  const int s = uniform(find_seq(a.trees.rows, token, [&](int i) { return tree_begin(a.trees, i); }));
-  const Tree tree = tree_of(a.trees, s);
+  const int4 place = load_uniform(a.trees.place + token);
+  const Tree tree{place.x, place.y};
   const int node = (int)(token - tree.first);
   if (node < 0 || node >= tree.n) return;
   const T* p = static_cast<const T*>(a.target) + token * a.target_stride;
@@ -126,12 +147,9 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
     float px = 0.0f, qx = 0.0f, ux = 0.0f;
     if (i < kMostNodes) {
       if (i < tree.n && i / 64 < a.trees.words && a.trees.up[token * a.trees.words + i / 64] >> (i % 64) & 1) {
-        const int parent = a.trees.node[tree.first + i].x;
-        if (parent < 0) barred = i != 0;
-        else {
-          const int first = a.trees.node[tree.first + parent].y;
-          barred = first_taken<T, DRAFT>(a, tree.first + parent, tree.first + first) != (first == i);
-        }
+        const int4 at = a.trees.node[tree.first + i];
+        if (at.x < 0 || at.x >= tree.n || at.z >= tree.n) barred = i != 0;
+        else barred = first_taken<T, DRAFT>(a, tree.first + at.x, tree.first + at.z) != (at.z == i);
       }
     } else if (i < 2 * kMostNodes) {
       i -= kMostNodes;
@@ -188,26 +206,31 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
   const int part = ceil_div_d(ceil_div_d(a.vocab, kVerifyWaves), kBatch) * kBatch;
   const int from = min(wave * part, a.vocab), to = min(from + part, a.vocab);
   double ra = 1.0, rb = 0.0, qc = 1.0;
-  // parts: of every wave's part of the rows, without the children's tokens, the sums of max(pa P - pb Q, 0) and of Q
+  // parts: of every wave's part of the rows, without the children's tokens, the sums of max(P - by Q, 0), and of Q from the first pass over it
   bool have = false;
-  double pa = 1.0, pb = 0.0;
-  auto pass = [&](double sa, double sb) {
+  double by = 0.0, all_q = 0.0;
+  auto pass = [&](double times, bool first) {
     double sum = 0.0, other = 0.0;
-    if (DRAFT && sb != 0.0)
+    by = times;
+    if (DRAFT && first)
       walk_tokens<T, DRAFT>(p, q, a.vocab, from, to, marks, kids.token, count, [&](int, float r0, float q0) {
-        sum += fmax(sa * (double)r0 - sb * (double)q0, 0.0);
+        sum += fmax(__builtin_fma(-by, (double)q0, (double)r0), 0.0);
         other += (double)q0;
       });
+    else if (DRAFT && by != 0.0)
+      walk_tokens<T, DRAFT>(p, q, a.vocab, from, to, marks, kids.token, count,
+                            [&](int, float r0, float q0) { sum += fmax(__builtin_fma(-by, (double)q0, (double)r0), 0.0); });
     else                                 // (the draft's row of a node without children may hold anything)
       walk_tokens<T, false>(p, q, a.vocab, from, to, marks, kids.token, count, [&](int, float r0, float) { sum += (double)r0; });
     sum = wave_sum(sum);
-    other = wave_sum(other);
+    if (first) other = wave_sum(other);
     __syncthreads();                     // (whoever read the parts before is done)
-    if (lane == 0) { parts[0][wave] = sum; parts[1][wave] = other; }
+    if (lane == 0) {
+      parts[0][wave] = sum;
+      if (first) parts[1][wave] = other;
+    }
     __syncthreads();
     have = true;
-    pa = sa;
-    pb = sb;
   };
   auto total = [&](int which) {
     double v = 0.0;
@@ -223,7 +246,8 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
     return wave_sum(v);
   };
   double w[kGroups] = {};                // what r was at the children's tokens before it was divided by its sum
-  bool undivided = false;                // parts and w are of r before that
+  double unit = 1.0;                     // ... and a then
+  bool undivided = false;                // parts, w and unit are of r before that
   for (int k = 0; k < count; ++k) {
     double rk = 0.0, qk = 0.0;
 #pragma unroll
@@ -244,19 +268,20 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
       return;
     }
     if constexpr (DRAFT) {
-      const double sb = rb + qc;
-      pass(ra, sb);
+      const double times = rb + qc / ra;
+      pass(times, !have);
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
         w[g] = fmax(r[g] - q_now[g], 0.0);
         if (x[g] == xk) q_all[g] = 0.0;
       }
-      const double left = total(0) + over([&](int g) { return w[g]; });
+      const double left = ra * total(0) + over([&](int g) { return w[g]; });
       const double rest = total(1) + over([&](int g) { return q_all[g]; });
       undivided = left > 0.0;
+      unit = ra;
       if (undivided) {
         ra /= left;
-        rb = sb / left;
+        rb = times;
       }
       qc = rest > 0.0 ? 1.0 / rest : 0.0;
 #pragma unroll
@@ -265,7 +290,7 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
         q_now[g] = q_all[g] * qc;
       }
     } else {
-      if (!have) pass(1.0, 0.0);
+      if (!have) pass(0.0, false);
       const double left = ra * total(0) + over([&](int g) { return x[g] == xk ? 0.0 : r[g]; });
       if (left > 0.0) {
         ra /= left;
@@ -275,9 +300,8 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
     }
   }
   // The token that follows: from r, in the units of the parts where those are at hand.
-  if (DRAFT && !undivided) have = false;
-  if (!have) pass(ra, rb);
-  const double by = DRAFT && pb != 0.0 ? 1.0 : ra;    // of the parts
+  if (!DRAFT || !undivided) unit = ra;
+  if (!have || (DRAFT && !undivided)) pass(rb, false);
 #pragma unroll
   for (int g = 0; g < kGroups; ++g) {
     if (!(DRAFT && undivided)) w[g] = r[g];
@@ -286,15 +310,16 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
   // ... with the children's tokens in the parts that they lie in
   auto with_children = [&](int b, int e) { return over([&](int g) { return x[g] >= b && x[g] < e ? w[g] : 0.0; }); };
   {
-    const double mine = parts[0][wave] * by + with_children(from, to);
+    const double mine = parts[0][wave] * unit + with_children(from, to);
     __syncthreads();
     if (lane == 0) parts[0][wave] = mine;
     __syncthreads();
   }
   const double goal = (double)a.u[tree.first] * total(0);
   auto weights_of = [&](int b, int e, auto f) {
-    if (DRAFT && pb != 0.0) walk_tokens<T, DRAFT>(p, q, a.vocab, b, e, marks, kids.token, count, [&](int v, float r0, float q0) { f(v, fmax(pa * (double)r0 - pb * (double)q0, 0.0)); });
-    else walk_tokens<T, false>(p, q, a.vocab, b, e, marks, kids.token, count, [&](int v, float r0, float) { f(v, ra * (double)r0); });
+    if (DRAFT && by != 0.0)
+      walk_tokens<T, DRAFT>(p, q, a.vocab, b, e, marks, kids.token, count, [&](int v, float r0, float q0) { f(v, unit * fmax(__builtin_fma(-by, (double)q0, (double)r0), 0.0)); });
+    else walk_tokens<T, false>(p, q, a.vocab, b, e, marks, kids.token, count, [&](int v, float r0, float) { f(v, unit * (double)r0); });
   };
   // The part in which the running sum passes the goal, the share of it, and the token: where rounding lets none pass, the last that is above 0.
   int begin = 0, size = part;
