@@ -306,6 +306,36 @@ struct TreePlace {
   int kv, tile, begin, end, rows;
 };
 
+// The pages of a piece, one after another: the table's entries come 64 at a time, one a lane.
+struct PageList {
+  const int32_t* entries;
+  int64_t pages;
+  int first, end, mine;           // mine: of the lane's page, first + lane
+  __device__ __forceinline__ PageList(const TreeAttendArgs& a, const TreePlace& at) : entries(a.t.page + at.sp.at), pages(a.c.pages), end(at.end) { fetch(at.begin); }
+  __device__ __forceinline__ void fetch(int n) {
+    first = n;
+    mine = n + lane_id() < end ? entries[n + lane_id()] : -1;
+  }
+  // -1 where the cache has no such page.  n does not fall.
+  __device__ __forceinline__ int64_t operator()(int n) {
+    if (n >= end) return -1;
+    if (n >= first + kWave) fetch(n);
+    const int p = __builtin_amdgcn_readlane(mine, n - first);
+    return p >= 0 && p < pages ? p : (int64_t)-1;
+  }
+};
+
+// The scales of a page, asked for with its bytes: as vector loads, for waits on scalar ones (which come out of order) would be waits on everything in LDS.
+struct Scales {
+  float k, v;
+  __device__ __forceinline__ void load(const TreeAttendArgs& a, int64_t page, int kv) {
+    const int64_t at = page * a.c.heads + kv + in_loop(0);
+    k = a.c.k_scale[at];
+    v = a.c.v_scale[at];
+  }
+};
+__device__ __forceinline__ float uniform_of(float v) { return __uint_as_float((unsigned)uniform((int)__float_as_uint(v))); }
+
 // At most 64 rows: the four waves take the pages in turn (with more than 32 rows two pairs of them do), each page from memory to registers, and are joined in LDS.
 template <typename T, int R, bool CAP, bool BIAS>
 __device__ __forceinline__ bool tree_few_rows(const TreeAttendArgs& a, const TreePlace& at, TreeRows<T, R, CAP, BIAS>& rows, int block, int blocks, const vec8<T>* q) {
@@ -315,10 +345,8 @@ __device__ __forceinline__ bool tree_few_rows(const TreeAttendArgs& a, const Tre
   const int last_lo = a.window ? sp.ctx + sp.tree.n - a.window : 0;                 // no node's window begins behind it
   u32x4 kw[2][kBlocks], vw[kBlocks][2];
 
-  auto page_of = [&](int n) {
-    const int64_t p = load_uniform(a.t.page + sp.at + n);
-    return p >= 0 && p < a.c.pages ? p : (int64_t)-1;
-  };
+  PageList page_of(a, at);
+  Scales scales;
   const int key = 16 * ((col >> 2) & 1) + 4 * (col >> 3) + (col & 3);
   auto load_k = [&](int64_t page) {
     const unsigned char* p = a.c.k + (page * a.c.heads + at.kv) * (kPage * R) + key * R + 16 * half;
@@ -337,13 +365,13 @@ __device__ __forceinline__ bool tree_few_rows(const TreeAttendArgs& a, const Tre
 
   bool strange = false;
   int n = block * 32 < at.rows ? at.begin + wave / blocks : at.end;
-  int64_t page = n < at.end ? page_of(n) : -1;
-  if (page >= 0) { load_k(page); load_v(page); }
+  int64_t page = page_of(n);
+  if (page >= 0) { scales.load(a, page, at.kv); load_k(page); load_v(page); }
   while (n < at.end) {
     const int next = n + turns;
-    const int64_t next_page = next < at.end ? page_of(next) : -1;
+    const int64_t next_page = page_of(next);
     if (page >= 0) {
-      const float ks = load_uniform(a.c.k_scale + page * a.c.heads + at.kv), vs = load_uniform(a.c.v_scale + page * a.c.heads + at.kv);
+      const float ks = uniform_of(scales.k), vs = uniform_of(scales.v);
       if (a.c.bytes8 < R) {                        // channels behind the head's may hold anything, and 0 times NaN is NaN
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
@@ -359,7 +387,7 @@ __device__ __forceinline__ bool tree_few_rows(const TreeAttendArgs& a, const Tre
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) x[t] = mma(widen(u32x2{kw[t][i / 2][2 * (i % 2)], kw[t][i / 2][2 * (i % 2) + 1]}, T()), q[i], x[t]);
       }
-      if (next_page >= 0) load_k(next_page);
+      if (next_page >= 0) { scales.load(a, next_page, at.kv); load_k(next_page); }
       const int k0 = n * kPage;
       const bool whole = k0 + kPage <= sp.ctx && k0 >= last_lo;
       vec8<f16_t> p[4];
@@ -380,6 +408,7 @@ __device__ __forceinline__ bool tree_few_rows(const TreeAttendArgs& a, const Tre
         for (int u = 0; u < 4; ++u) rows.acc[j] = mma(widen(u32x2{vw[j][u / 2][2 * (u % 2)], vw[j][u / 2][2 * (u % 2) + 1]}, f16_t()), p[u], rows.acc[j]);
       if (next_page >= 0) load_v(next_page);
     } else if (next_page >= 0) {
+      scales.load(a, next_page, at.kv);
       load_k(next_page);
       load_v(next_page);
     }
@@ -404,12 +433,11 @@ __device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const Tr
   const int lane = lane_id(), half = lane >> 5, tid = threadIdx.x;
   const int last_lo = a.window ? sp.ctx + sp.tree.n - a.window : 0;
   u32x4 kw[kPieces], vw[kPieces];
-  auto page_of = [&](int n) {
-    const int64_t p = load_uniform(a.t.page + sp.at + n);
-    return p >= 0 && p < a.c.pages ? p : (int64_t)-1;
-  };
+  PageList page_of(a, at);
+  Scales scales;
   auto load = [&](int64_t page) {
     const int64_t at0 = (page * a.c.heads + at.kv) * (kPage * R) + tid * 16;
+    scales.load(a, page, at.kv);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       kw[i] = *reinterpret_cast<const u32x4*>(a.c.k + at0 + i * 4096);
@@ -450,13 +478,18 @@ __device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const Tr
   const int k_base = SK::row_base(lane), v_base = SV::row_base(lane);
   int n = at.begin;
   int64_t page = page_of(n);
-  if (page >= 0) { load(page); store(n, 0); }
+  float ks = 0.0f, vs = 0.0f;
+  if (page >= 0) {
+    load(page);
+    store(n, 0);
+    ks = uniform_of(scales.k);
+    vs = uniform_of(scales.v);
+  }
   for (int from = 0; n < at.end; ++n, from ^= 1) {
-    const int64_t next = n + 1 < at.end ? page_of(n + 1) : -1;
+    const int64_t next = page_of(n + 1);
     if (next >= 0) load(next);
     __syncthreads();                                 // the page is there; the one before it is not read any more
     if (page >= 0) {
-      const float ks = load_uniform(a.c.k_scale + page * a.c.heads + at.kv), vs = load_uniform(a.c.v_scale + page * a.c.heads + at.kv);
       const unsigned char *kt = tiles.k[from], *vt = tiles.v[from];
       f32x16 x[2];
 #pragma unroll
@@ -473,7 +506,11 @@ __device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const Tr
 #pragma unroll
         for (int u = 0; u < 4; ++u) rows.acc[j] = mma(SV::template row<f16_t>(vt, v_base, 32 * j, u), p[u], rows.acc[j]);
     }
-    if (next >= 0) store(n + 1, from ^ 1);
+    if (next >= 0) {
+      store(n + 1, from ^ 1);
+      ks = uniform_of(scales.k);
+      vs = uniform_of(scales.v);
+    }
     page = next;
   }
   return strange;
