@@ -1,6 +1,8 @@
 // C ABI of drafted tokens over the paged cache (see include/spdraft.h): argument checks, scratch memory, launches.  All device work is in the draft_ headers beside this file.
 #include "../../include/spdraft.h"
 
+#include <algorithm>
+
 #include "attn_host.hpp"
 #include "draft_attend.hpp"
 #include "draft_keep.hpp"
@@ -112,20 +114,29 @@ int spdraft_attend(spgemm_handle h, const spcache* c, int64_t layer, const spgem
     a.window = (int)(window < kMaxTokens ? window : 0);
     a.score = {scale, cap, slopes};
     const int room = room_of(c);
-    // Pages of a workgroup: so many that the workgroups fill the card twice, at least one for every wave.
-    const int64_t want = (int64_t)h->num_cus * 4;
-    int64_t chunk = ceil_div(table->nnz * c->kv_heads * a.tiles, want);
-    chunk = chunk < 4 ? 4 : ceil_div(chunk, 4) * 4;
-    a.chunk = (int)chunk;
-    a.slots = table->nnz / chunk + n;
-    const int64_t units = a.slots * c->kv_heads, cells = units * a.tiles;
-    if (cells > 0xffffff - 8 * a.tiles) return fail(h, SPGEMM_UNSUPPORTED, "too many pages");
+    a.places = h->num_cus * kTreeResident;
+    // Up to kMostEven sequences every workgroup finds its piece by itself.  Pieces: never more than kMostTurns times the places, or the units and as many pieces more as the places (pages_of_piece);
+    // nor more than the units and one for every kLeastPages pages.  Cells are for pieces of cut units alone, at most two for every kLeastPages pages.  Beyond, places of chunks are found by the table's row pointers.
+    const int64_t units = n * c->kv_heads * a.tiles, work = table->nnz * c->kv_heads * a.tiles;
+    int64_t pieces, cells;
+    if (n <= kMostEven) {
+      a.chunk = 0;
+      const int64_t most = std::max<int64_t>((int64_t)kMostTurns * a.places, units + a.places);
+      pieces = std::min(most, units + work / kLeastPages);
+      cells = std::min((int64_t)kMostTurns * a.places, 2 * (work / kLeastPages));
+    } else {
+      const int64_t chunk = ceil_div(work, 2 * a.places);
+      a.chunk = (int)(chunk < 8 ? 8 : ceil_div(chunk, 4) * 4);
+      pieces = cells = (table->nnz / a.chunk + n) * c->kv_heads * a.tiles;
+    }
+    if (pieces > 0xffffff - 128) return fail(h, SPGEMM_UNSUPPORTED, "too many pages");      // (2^32 threads are a launch's limit)
     const size_t part = align_up((size_t)cells * a.part_rows * room * sizeof(float)), ml = align_up((size_t)cells * a.part_rows * sizeof(float2));
     void* mem = nullptr;
     if ((rc = scratch(h, part + ml, &mem))) return rc;
+    a.cells = cells;
     a.part = static_cast<float*>(mem);
     a.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(mem) + part);
-    const dim3 grid((unsigned)(ceil_div(units, 8) * 8 * a.tiles)), join((unsigned)t->tokens, (unsigned)heads);
+    const dim3 grid((unsigned)(ceil_div(pieces, 128) * 128)), join((unsigned)t->tokens, (unsigned)c->kv_heads);
     dispatch(dtype, c->head_dim, cap > 0, slopes != nullptr, [&](auto type, auto dim, auto capped, auto bias) {
       k_tree_attend<decltype(type), dim(), capped(), bias()><<<grid, dim3(256), 0, h->stream>>>(a);
     });

@@ -99,19 +99,22 @@ __global__ void __launch_bounds__(1024) k_trees_check(TreeView t, const int32_t*
 // ---- attention --------------------------------------------------------------------------------
 
 constexpr int kTreeRows = 128;    // rows of a workgroup, at most: 32 a wave
+constexpr int kTreeResident = 2;  // workgroups of a compute unit (registers)
 
 struct TreeAttendArgs {
   CacheView c;
   TableView t;
   TreeView trees;
   HeadTensor q, o;          // row ptr[s] + i: node i of sequence s
-  int heads, group, tiles, window;
-  int chunk;                // pages of a workgroup
-  int64_t slots;            // places of chunks
-  int part_rows;            // rows that a workgroup's part has places for
+  int heads, group, window;
+  int tiles;                // of 128 rows, that a tree can have
+  int places;               // workgroups that the card holds at once
+  int chunk;                // pages of a workgroup where sequences are many; 0: Schedule says
+  int part_rows;            // rows that a cell has places for
+  int64_t cells;            // (row pointers that do not ascend could ask for more: such pieces are left out)
   ScoreShape score;
-  float* part;              // [slots][key heads][tiles][part_rows][R]: sums of what the workgroups saw, not divided
-  float2* part_ml;          // [slots][key heads][tiles][part_rows]: maximum (units of log 2) and sum
+  float* part;              // [cells][part_rows][R]: sums of what the workgroups saw, not divided
+  float2* part_ml;          // [cells][part_rows]: maximum (units of log 2) and sum
 };
 
 // Sequence s: its tree, its tokens and the pages first .. last - 1 that its nodes see.
@@ -135,6 +138,78 @@ __device__ __forceinline__ TreePages tree_pages(const TreeAttendArgs& a, int s) 
   r.first = r.lo / kPage;
   r.last = r.tree.n > 0 ? ceil_div_d(r.len, kPage) : r.first;
   return r;
+}
+
+// What has to be done is units: a sequence's pages (those that its nodes see), a tile of its rows, a key head.  Long units are cut into pieces of about `per` pages, for which there are cells where the
+// pieces' sums wait to be joined.  Every workgroup finds `per` and its piece by itself, from the lengths of all sequences, a lane each; that is one chain of loads more or less as long as a search for its sequence would be.
+//
+// per: the card has `places` workgroups at once.  If they are to be done in k turns, pieces have at least work / (k places - units) pages (cutting makes at most work / per pieces more than there are
+// units), and cost k (per + kPieceCost) pages' time, kPieceCost for what a workgroup does beside its pages; the best k up to 4 is taken.  Where units are more than that, only what is longer than twice the average
+// is cut.  (All pieces of the same length in no whole number of turns were worst: four sequences, 60 nodes, 65 011 tokens, 337 us with about 1.6 turns of 60 pages.)
+constexpr int kMostEven = 512;     // sequences that a workgroup looks through
+constexpr int kLeastPages = 4, kPieceCost = 3, kMostTurns = 4;
+struct Piece {
+  int s, kv, tile, piece, pieces;  // s: -1 where there is nothing to do
+  int64_t cell, stride;            // of the unit's first piece, to the next one
+};
+struct Units { int pages, tiles; };
+__device__ __forceinline__ Units units_of(const TreeAttendArgs& a, int s) {
+  if (s >= a.t.seqs) return {0, 0};
+  const TreePages sp = tree_pages(a, s);
+  const int pages = max(sp.last - sp.first, 0);
+  return {pages, pages ? ceil_div_d(sp.tree.n * a.group, kTreeRows) : 0};
+}
+__device__ __forceinline__ int pages_of_piece(double work, double units, int places) {
+  double best = 1e300;
+  int per = 0;
+#pragma unroll
+  for (int k = 1; k <= kMostTurns; ++k) {
+    const double room = (double)k * places - units;
+    if (room <= 0.0) continue;
+    const double pages = fmax(ceil(work / room), (double)kLeastPages), cost = k * (pages + kPieceCost);
+    if (cost < best) { best = cost; per = (int)fmin(pages, 1e9); }
+  }
+  return per ? per : (int)fmin(fmax(ceil(2.0 * work / places), (double)kLeastPages), 1e9);
+}
+// Piece number `at` of the list (sequence by sequence; of one its pieces, of those the key heads, of those the tiles); with one_s at least 0 the first piece of that sequence's unit (kv, tile).
+__device__ __forceinline__ Piece schedule(const TreeAttendArgs& a, int64_t at, int one_s, int kv, int tile) {
+  double work = 0.0, units = 0.0;
+  Units u{0, 0};
+  for (int b = 0; b < a.t.seqs; b += kWave) {
+    u = units_of(a, b + lane_id());
+    work += (double)u.pages * u.tiles;
+    units += u.tiles;
+  }
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) { work += __shfl_xor(work, d); units += __shfl_xor(units, d); }
+  const int per = uniform(pages_of_piece(work * a.c.heads, units * a.c.heads, a.places));
+  int64_t first = 0, cells = 0;    // of the sequences before these 64
+  for (int b = 0; b < a.t.seqs; b += kWave) {
+    if (a.t.seqs > kWave) u = units_of(a, b + lane_id());
+    const int pieces = ceil_div_d(u.pages, per), each = u.tiles * a.c.heads, count = pieces * each, cut = pieces > 1 ? count : 0;
+    int upto = count, cells_upto = cut;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const int x = __shfl_up(upto, d), y = __shfl_up(cells_upto, d);
+      upto += lane_id() >= d ? x : 0;
+      cells_upto += lane_id() >= d ? y : 0;
+    }
+    const unsigned long long hit = __ballot(one_s >= 0 ? b + lane_id() == one_s : count > 0 && at >= first + upto - count && at < first + upto);
+    if (hit) {
+      const int lane = __builtin_ctzll(hit), its_pieces = __shfl(pieces, lane), its_each = __shfl(each, lane), tiles = __shfl(u.tiles, lane);
+      const int64_t cell = cells + __shfl(cells_upto - cut, lane);
+      int i = 0;
+      if (one_s < 0) {
+        i = (int)(at - first) - __shfl(upto - count, lane);
+        tile = i % tiles;
+        kv = i / tiles % a.c.heads;
+      }
+      return {uniform(b + lane), uniform(kv), uniform(tile), its_each ? uniform(i / its_each) : 0, uniform(its_pieces), cell + kv * tiles + tile, its_each};
+    }
+    first += __shfl(upto, kWave - 1);
+    cells += __shfl(cells_upto, kWave - 1);
+  }
+  return {-1, 0, 0, 0, 0, 0, 0};
 }
 
 // Of the tree's nodes first .. first + 63 (first may be negative) those that node i, whose ancestors are at `up`, sees: bits; above: how many of its ancestors and itself come behind them.
@@ -299,10 +374,10 @@ __device__ __forceinline__ unsigned proper_bytes(unsigned w, bool& strange) {
   return w & ~((nan >> 7) * 0xffu);
 }
 
-// Where a workgroup is: its sequence, its pages begin .. end - 1, its rows.
+// Where a workgroup is: its sequence, its pages begin .. end - 1, its rows, and the cell that its sums go to (-1: nothing to join with).
 struct TreePlace {
   TreePages sp;
-  int64_t slot;
+  int64_t cell;
   int kv, tile, begin, end, rows;
 };
 
@@ -518,27 +593,39 @@ __device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const Tr
 
 // A workgroup has `chunk` pages of a sequence, a key head and up to 128 rows.  The second product is in float16 whatever the type: e4m3 values are exact in it, and probabilities keep 11 digits instead of bfloat16's 8.
 template <typename T, int R, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, 2) k_tree_attend(TreeAttendArgs a) {
+__global__ void __launch_bounds__(256, kTreeResident) k_tree_attend(TreeAttendArgs a) {
   constexpr int kSteps = R / 16, kBlocks = R / 32;
   const int lane = lane_id(), half = lane >> 5, col = lane & 31, wave = uniform(threadIdx.x / kWave);
   TreePlace at;
-  // tiles of the same pages go to one die, one after the other: its L2 cache then has the pages for all of them
+  // workgroups go to the eight dies in turn: 16 neighbours of the list stay on one, whose L2 cache then has the pages for all tiles of a unit
   const unsigned die = blockIdx.x % 8, turn = blockIdx.x / 8;
-  at.tile = turn % a.tiles;
-  const int64_t unit_no = (int64_t)(turn / a.tiles) * 8 + die;
-  at.kv = (int)(unit_no % a.c.heads);
-  at.slot = unit_no / a.c.heads;
-  if (at.slot >= a.slots) return;
-  const int s = uniform(find_seq(a.t.seqs, at.slot, [&](int i) { return first_page(a.t, i) / a.chunk + i; }));
-  at.sp = tree_pages(a, s);
+  const int64_t number = (int64_t)(turn / 16 * 8 + die) * 16 + turn % 16;
+  if (a.chunk == 0) {
+    const Piece mine = schedule(a, number, -1, 0, 0);
+    if (mine.s < 0) return;
+    at.sp = tree_pages(a, mine.s);
+    at.kv = mine.kv;
+    at.tile = mine.tile;
+    const int pages = ceil_div_d(at.sp.last - at.sp.first, mine.pieces);
+    at.begin = uniform(at.sp.first + mine.piece * pages);
+    at.end = uniform(min(at.begin + pages, at.sp.last));
+    at.cell = mine.pieces > 1 ? mine.cell + mine.piece * mine.stride : -1;
+  } else {
+    // many sequences: places of chunks, found without knowing the lengths.  s has ptr[s] / chunk + s and on
+    at.tile = (int)(number % a.tiles);
+    at.kv = (int)(number / a.tiles % a.c.heads);
+    const int64_t slot = number / a.tiles / a.c.heads;
+    const int s = uniform(find_seq(a.t.seqs, slot, [&](int i) { return first_page(a.t, i) / a.chunk + i; }));
+    at.sp = tree_pages(a, s);
+    const int64_t piece = slot - (at.sp.at / a.chunk + s);
+    if (piece < 0 || piece * a.chunk >= at.sp.last) return;
+    at.begin = uniform(max(at.sp.first, (int)piece * a.chunk));
+    at.end = uniform(min(at.sp.last, (int)(piece + 1) * a.chunk));
+    at.cell = at.sp.first / a.chunk == (at.sp.last - 1) / a.chunk ? -1 : number;
+  }
   const TreePages& sp = at.sp;
   at.rows = uniform(min(sp.tree.n * a.group - at.tile * kTreeRows, kTreeRows));
-  const int64_t piece = at.slot - (sp.at / a.chunk + s);
-  if (at.rows <= 0 || piece < 0 || piece * a.chunk >= sp.last) return;
-  at.begin = uniform(max(sp.first, (int)piece * a.chunk));
-  at.end = uniform(min(sp.last, (int)(piece + 1) * a.chunk));
-  if (at.begin >= at.end) return;
-  const bool alone = sp.first / a.chunk == (sp.last - 1) / a.chunk;    // nothing to join with
+  if (at.rows <= 0 || at.begin >= at.end || at.cell >= a.cells) return;
   const int blocks = at.rows <= 32 ? 1 : at.rows <= 64 ? 2 : 4;        // blocks of rows
   const int block = wave % blocks;
 
@@ -601,7 +688,6 @@ __global__ void __launch_bounds__(256, 2) k_tree_attend(TreeAttendArgs a) {
     }
     __syncthreads();
   }
-  const int64_t cell = (at.slot * a.c.heads + at.kv) * a.tiles + at.tile;
   for (int i = threadIdx.x; i < at.rows * (R / 4); i += 256) {
     const int row = i / (R / 4), d = i % (R / 4) * 4, mine = row % 32;
     float top = -INFINITY;
@@ -614,7 +700,7 @@ __global__ void __launch_bounds__(256, 2) k_tree_attend(TreeAttendArgs a) {
       v += *reinterpret_cast<const f32x4*>(&j.sums[w][mine][d]) * f;
       sum += j.ls[w][mine] * f;
     }
-    if (alone) {
+    if (at.cell < 0) {
       if (d < a.c.bytes8) {
         const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
         const int rt = at.tile * kTreeRows + row;
@@ -625,65 +711,75 @@ __global__ void __launch_bounds__(256, 2) k_tree_attend(TreeAttendArgs a) {
         *reinterpret_cast<u32x2*>(const_cast<unsigned char*>(dst.base) + (sp.tree.first + rt / a.group) * dst.stride + d * 2) = __builtin_bit_cast(u32x2, out);
       }
     } else {
-      *reinterpret_cast<f32x4*>(a.part + (cell * a.part_rows + row) * R + d) = v;
-      if (d == 0) a.part_ml[cell * a.part_rows + row] = make_float2(top, sum);
+      *reinterpret_cast<f32x4*>(a.part + (at.cell * a.part_rows + row) * R + d) = v;
+      if (d == 0) a.part_ml[at.cell * a.part_rows + row] = make_float2(top, sum);
     }
   }
 }
 
-// Joins a row's chunks; rows that no chunk has (no tokens) become zero.  A workgroup has a node and a head: R / 4 threads go over every (1024 / R)-th
-// chunk, four channels each, and their sums are joined in order.
+// Joins the pieces of a unit; rows that no piece has (no tokens) become zero.  A workgroup has a node and a key head: R / 4 lanes go over every (256 / R)-th piece of a row, four channels each, and what they
+// have is joined in order; the four waves take the rows of the heads that share the key head in turn.
 template <typename T, int R>
 __global__ void __launch_bounds__(256) k_tree_join(TreeAttendArgs a) {
-  constexpr int kThreads = R / 4, kLanes = 256 / kThreads;
+  constexpr int kThreads = R / 4, kLanes = kWave / kThreads;
   const int64_t token = blockIdx.x;
-  const int head = blockIdx.y, kv = head / a.group;
+  const int kv = blockIdx.y;
   const int4 place = load_uniform(a.trees.place + token);
   if (place.y == 0) return;
   const TreePages sp = tree_pages(a, place.z);
   const int64_t node = token - sp.tree.first;
   if (node < 0 || node >= sp.tree.n) return;
   const bool none = sp.first >= sp.last;
-  const int c0 = none ? 0 : sp.first / a.chunk, c1 = none ? 0 : (sp.last - 1) / a.chunk + 1;
-  if (c1 - c0 == 1) return;
-  const int rr = (int)node * a.group + head % a.group, d = threadIdx.x % kThreads * 4, mine = threadIdx.x / kThreads;
-  const int64_t slot = sp.at / a.chunk + place.z;
-  float top = -INFINITY, sum = 0.0f;
-  f32x4 v = {0, 0, 0, 0};
+  const int first = (int)node * a.group;
+  for (int g = threadIdx.x / kWave; g < a.group; g += 4) {
+    const int rr = first + g, tile = rr / kTreeRows, d = lane_id() % kThreads * 4, mine = lane_id() / kThreads;
+    int64_t cell = 0, stride = 0;
+    int pieces = 0;
+    if (!none) {
+      if (a.chunk == 0) {
+        const Piece p = schedule(a, 0, place.z, kv, tile);
+        cell = p.cell;
+        stride = p.stride;
+        pieces = p.pieces;
+      } else {
+        const int c0 = sp.first / a.chunk;
+        pieces = (sp.last - 1) / a.chunk + 1 - c0;
+        cell = ((sp.at / a.chunk + place.z + c0) * a.c.heads + kv) * a.tiles + tile;
+        stride = (int64_t)a.c.heads * a.tiles;
+      }
+      if (pieces == 1) return;
+    }
+    float top = -INFINITY, sum = 0.0f;
+    f32x4 v = {0, 0, 0, 0};
 #pragma unroll 4
-  for (int c = c0 + mine; c < c1; c += kLanes) {
-    const int64_t row = (((slot + c) * a.c.heads + kv) * a.tiles + rr / kTreeRows) * a.part_rows + rr % kTreeRows;
-    const float2 ml = a.part_ml[row];
-    const f32x4 w = *reinterpret_cast<const f32x4*>(a.part + row * R + d);
-    const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.0f : now;
-    const float f = fast_exp2(top - base), g = fast_exp2(ml.x - base);
-    v = v * f + w * g;
-    sum = sum * f + ml.y * g;
-    top = now;
+    for (int c = mine; c < pieces; c += kLanes) {
+      if (cell + c * stride >= a.cells) break;
+      const int64_t row = (cell + c * stride) * a.part_rows + rr % kTreeRows;
+      const float2 ml = a.part_ml[row];
+      const f32x4 w = *reinterpret_cast<const f32x4*>(a.part + row * R + d);
+      const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.0f : now;
+      const float f = fast_exp2(top - base), g2 = fast_exp2(ml.x - base);
+      v = v * f + w * g2;
+      sum = sum * f + ml.y * g2;
+      top = now;
+    }
+#pragma unroll
+    for (int step = kThreads; step < kWave; step *= 2) {
+      const float other = __shfl_xor(top, step), all = fmaxf(top, other), base = all == -INFINITY ? 0.0f : all;
+      const float f = fast_exp2(top - base), g2 = fast_exp2(other - base);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = v[j] * f + __shfl_xor(v[j], step) * g2;
+      sum = sum * f + __shfl_xor(sum, step) * g2;
+      top = all;
+    }
+    if (mine || d >= a.c.bytes8) continue;
+    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const RowSource dst = a.o.of(kv * a.group + g);
+    T out[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) out[j] = (T)(v[j] * by);
+    *reinterpret_cast<u32x2*>(const_cast<unsigned char*>(dst.base) + token * dst.stride + d * 2) = __builtin_bit_cast(u32x2, out);
   }
-  __shared__ __align__(16) f32x4 vs[256];
-  __shared__ float2 mls[kLanes];
-  vs[threadIdx.x] = v;
-  if (d == 0) mls[mine] = make_float2(top, sum);
-  __syncthreads();
-  if (mine || d >= a.c.bytes8) return;
-  float all = -INFINITY, total = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kLanes; ++i) all = fmaxf(all, mls[i].x);
-  all = all == -INFINITY ? 0.0f : all;
-  v = f32x4{0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < kLanes; ++i) {
-    const float f = fast_exp2(mls[i].x - all);
-    v += vs[i * kThreads + threadIdx.x] * f;
-    total += mls[i].y * f;
-  }
-  const float by = total == 0.0f ? 0.0f : 1.0f / total;
-  const RowSource dst = a.o.of(head);
-  T out[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) out[j] = (T)(v[j] * by);
-  *reinterpret_cast<u32x2*>(const_cast<unsigned char*>(dst.base) + token * dst.stride + d * 2) = __builtin_bit_cast(u32x2, out);
 }
 
 }  // namespace spg
