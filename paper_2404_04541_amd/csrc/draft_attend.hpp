@@ -237,6 +237,7 @@ __device__ __forceinline__ Seen seen_nodes(const unsigned long long* up, int wor
 
 // ... and of a page's first `upto` tokens, which lie before the tree, those from `from` on.  (Of keys before the sequence's first there is no page: where ctx is below 0, the first page's bits begin with a later node.)
 __device__ __forceinline__ unsigned long long seen_context(int upto, int from) {
+  upto = max(upto, 0);
   from = min(max(from, 0), kPage);
   return (upto >= kPage ? ~0ull : (1ull << upto) - 1) & (from == kPage ? 0ull : ~0ull << from);
 }
@@ -271,11 +272,11 @@ struct TreeRows {
   }
 
   // From the products q.k of a page's keys to its probabilities.  x[t][i] is key H half + 32 t + i (H 16) or 32 t + 16 (i / 8) + i % 8 (H 8) of the page; p[2 t + i / 8][i % 8] becomes its probability, as an
-  // operand.
+  // operand; false where the page's values are too small for them to show.
   template <int H>
   static __device__ __forceinline__ constexpr int key(int t, int i) { return H == 16 ? 32 * t + i : 32 * t + 16 * (i / 8) + i % 8; }
   template <int H>
-  __device__ __forceinline__ void weigh(const TreeAttendArgs& a, const TreePages& sp, f32x16 (&x)[2], int k0, bool whole, float ks, float vs, int half, vec8<f16_t> (&p)[4]) {
+  __device__ __forceinline__ bool weigh(const TreeAttendArgs& a, const TreePages& sp, f32x16 (&x)[2], int k0, bool whole, float ks, float vs, int half, vec8<f16_t> (&p)[4]) {
     const float c = fmaxf(scale2 * ks, 1.17549435e-38f);      // (above 0: what is not seen is -inf times it)
     float unit2 = c;                                            // of x, in units of log 2
     if constexpr (CAP || BIAS) {
@@ -319,9 +320,9 @@ struct TreeRows {
           x[t][i] = sees ? x[t][i] : -INFINITY;
         }
     }
-    float top = fmaxf(x[0][0], x[1][0]);
+    float top = __builtin_elementwise_maximum(x[0][0], x[1][0]);                  // (NaN where a score is: then nothing else matters of the row)
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(x[0][i], x[1][i]));
+    for (int i = 1; i < 16; ++i) top = max3(top, x[0][i], x[1][i]);
     top = max_halves(top) * unit2;
     // The sums go to a new unit only where some row's maximum has grown by more than 2^3, or the page's scale is larger than the unit or much smaller.  Not further down than 2^-64 of the
     // largest scale so far: a page of zeros has the scale 2^-100, next to which sums of large values would overflow.
@@ -351,20 +352,13 @@ struct TreeRows {
         sum += e;
         p[2 * t + i / 8][i % 8] = (f16_t)e;
       }
-    if (exponent - unit < below)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) p[u] = vec8<f16_t>{};
     l += __builtin_amdgcn_ldexpf(sum, -kTreeShift - below);
+    return exponent - unit == below;
   }
 };
 
-// Which bytes of a word of four tokens from `off` on lie from lo to before len.
-__device__ __forceinline__ unsigned live_bytes(int off, int lo, int len) {
-  unsigned mask = 0;
-#pragma unroll
-  for (int b = 0; b < 4; ++b) mask |= off + b >= lo && off + b < len ? 0xffu << (8 * b) : 0u;
-  return mask;
-}
+// The bytes of a word of four tokens whose bits are set.
+__device__ __forceinline__ unsigned bytes_of(unsigned bits) { return ((bits & 15u) * 0x00204081u & 0x01010101u) * 0xffu; }
 // The highest bit of every byte that is NaN (0x7f, 0xff).
 __device__ __forceinline__ unsigned nan_bytes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 // Values of a page that some rows do not see as a whole: the product multiplies all of them, by 0 where a row does not see them, so what is NaN becomes 0; the rows that see it become NaN in the end.
@@ -466,21 +460,23 @@ __device__ __forceinline__ bool tree_few_rows(const TreeAttendArgs& a, const Tre
       const int k0 = n * kPage;
       const bool whole = k0 + kPage <= sp.ctx && k0 >= last_lo;
       vec8<f16_t> p[4];
-      rows.template weigh<16>(a, sp, x, k0, whole, ks, vs, half, p);
+      const bool shows = rows.template weigh<16>(a, sp, x, k0, whole, ks, vs, half, p);
       if (!whole) {
+        const unsigned long long live = seen_context(sp.len - k0, sp.lo - k0) >> in_loop(16 * half);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
-            const unsigned live = live_bytes(k0 + 32 * t + 16 * half + 4 * w, sp.lo, sp.len);
+            const unsigned bytes = bytes_of((unsigned)(live >> (32 * t + 4 * w)));
 #pragma unroll
-            for (int j = 0; j < kBlocks; ++j) vw[j][t][w] = proper_bytes(vw[j][t][w] & live, strange);
+            for (int j = 0; j < kBlocks; ++j) vw[j][t][w] = proper_bytes(vw[j][t][w] & bytes, strange);
           }
       }
+      if (shows)
 #pragma unroll
-      for (int j = 0; j < kBlocks; ++j)
+        for (int j = 0; j < kBlocks; ++j)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) rows.acc[j] = mma(widen(u32x2{vw[j][u / 2][2 * (u % 2)], vw[j][u / 2][2 * (u % 2) + 1]}, f16_t()), p[u], rows.acc[j]);
+          for (int u = 0; u < 4; ++u) rows.acc[j] = mma(widen(u32x2{vw[j][u / 2][2 * (u % 2)], vw[j][u / 2][2 * (u % 2) + 1]}, f16_t()), p[u], rows.acc[j]);
       if (next_page >= 0) load_v(next_page);
     } else if (next_page >= 0) {
       scales.load(a, next_page, at.kv);
@@ -541,8 +537,9 @@ __device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const Tr
         const int channel = piece / 4, chunk = piece % 4 * 2;
         u32x4 w = vw[i];
         if (!whole) {
+          const unsigned live = (unsigned)(seen_context(sp.len - n * kPage, sp.lo - n * kPage) >> in_loop(chunk * 8));      // (in_loop: not computed where it is not wanted)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) w[j] = proper_bytes(w[j] & live_bytes(n * kPage + chunk * 8 + 4 * j, sp.lo, sp.len), strange);
+          for (int j = 0; j < 4; ++j) w[j] = proper_bytes(w[j] & bytes_of(live >> (4 * j)), strange);
         }
         unsigned char* to = tiles.v[into] + channel * SV::kRowBytes;
         *reinterpret_cast<vec8<f16_t>*>(to + ((chunk ^ SV::swizzle(channel)) << 4)) = widen(u32x2{w[0], w[1]}, f16_t());
@@ -575,11 +572,11 @@ __device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const Tr
       }
       const bool whole = whole_page(n);
       vec8<f16_t> p[4];
-      rows.template weigh<8>(a, sp, x, n * kPage, whole, ks, vs, half, p);
+      if (rows.template weigh<8>(a, sp, x, n * kPage, whole, ks, vs, half, p))
 #pragma unroll
-      for (int j = 0; j < kBlocks; ++j)
+        for (int j = 0; j < kBlocks; ++j)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) rows.acc[j] = mma(SV::template row<f16_t>(vt, v_base, 32 * j, u), p[u], rows.acc[j]);
+          for (int u = 0; u < 4; ++u) rows.acc[j] = mma(SV::template row<f16_t>(vt, v_base, 32 * j, u), p[u], rows.acc[j]);
     }
     if (next >= 0) {
       store(n + 1, from ^ 1);
