@@ -130,12 +130,13 @@ int spdraft_attend(spgemm_handle h, const spcache* c, int64_t layer, const spgem
       pieces = cells = (table->nnz / a.chunk + n) * c->kv_heads * a.tiles;
     }
     if (pieces > 0xffffff - 128) return fail(h, SPGEMM_UNSUPPORTED, "too many pages");      // (2^32 threads are a launch's limit)
-    const size_t part = align_up((size_t)cells * a.part_rows * room * sizeof(float)), ml = align_up((size_t)cells * a.part_rows * sizeof(float2));
+    const size_t part = align_up((size_t)cells * a.part_rows * room * sizeof(float)), ml = align_up((size_t)cells * a.part_rows * sizeof(float2)), cuts = n <= kMostEven ? (size_t)n * sizeof(int4) : 0;
     void* mem = nullptr;
-    if ((rc = scratch(h, part + ml, &mem))) return rc;
+    if ((rc = scratch(h, part + ml + cuts, &mem))) return rc;
     a.cells = cells;
     a.part = static_cast<float*>(mem);
     a.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(mem) + part);
+    a.cuts = reinterpret_cast<int4*>(static_cast<unsigned char*>(mem) + part + ml);
     const dim3 grid((unsigned)(ceil_div(pieces, 128) * 128)), join((unsigned)t->tokens, (unsigned)c->kv_heads);
     dispatch(dtype, c->head_dim, cap > 0, slopes != nullptr, [&](auto type, auto dim, auto capped, auto bias) {
       k_tree_attend<decltype(type), dim(), capped(), bias()><<<grid, dim3(256), 0, h->stream>>>(a);

@@ -115,6 +115,7 @@ struct TreeAttendArgs {
   ScoreShape score;
   float* part;              // [cells][part_rows][R]: sums of what the workgroups saw, not divided
   float2* part_ml;          // [cells][part_rows]: maximum (units of log 2) and sum
+  int4* cuts;               // of every sequence with something to do: Cut
 };
 
 // Sequence s: its tree, its tokens and the pages first .. last - 1 that its nodes see.
@@ -149,67 +150,84 @@ __device__ __forceinline__ TreePages tree_pages(const TreeAttendArgs& a, int s) 
 constexpr int kMostEven = 512;     // sequences that a workgroup looks through
 constexpr int kLeastPages = 4, kPieceCost = 3, kMostTurns = 4;
 struct Piece {
-  int s, kv, tile, piece, pieces;  // s: -1 where there is nothing to do
+  TreePages sp;                    // of its sequence
+  int kv, tile, piece, pieces;     // pieces: of the unit; 0 where there is nothing to do
   int64_t cell, stride;            // of the unit's first piece, to the next one
 };
-struct Units { int pages, tiles; };
-__device__ __forceinline__ Units units_of(const TreeAttendArgs& a, int s) {
-  if (s >= a.t.seqs) return {0, 0};
-  const TreePages sp = tree_pages(a, s);
-  const int pages = max(sp.last - sp.first, 0);
-  return {pages, pages ? ceil_div_d(sp.tree.n * a.group, kTreeRows) : 0};
+// What the join has to know of a sequence: cell of the first piece of its first unit, how far the next piece's is, how many pieces.
+typedef int4 Cut;
+
+__device__ __forceinline__ float wave_total(float v) {
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x111, 0xf, 0xf, true));    // row_shr:1, 2, 4, 8; the last lanes of rows to the next, of two rows to the next two
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x112, 0xf, 0xf, true));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x114, 0xf, 0xf, true));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x118, 0xf, 0xf, true));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), kWave - 1));
 }
-__device__ __forceinline__ int pages_of_piece(double work, double units, int places) {
-  double best = 1e300;
+__device__ __forceinline__ int64_t of_lane(int64_t v, int lane) {
+  return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, lane));
+}
+
+__device__ __forceinline__ int pages_of_piece(float work, float units, int places) {
+  float best = INFINITY;
   int per = 0;
 #pragma unroll
   for (int k = 1; k <= kMostTurns; ++k) {
-    const double room = (double)k * places - units;
-    if (room <= 0.0) continue;
-    const double pages = fmax(ceil(work / room), (double)kLeastPages), cost = k * (pages + kPieceCost);
-    if (cost < best) { best = cost; per = (int)fmin(pages, 1e9); }
+    const float room = (float)(k * places) - units;
+    // (in 24 digits the sums and the quotient are off by less than 2^-12 of them: what is added keeps the number of pieces within k places)
+    const float pages = fmaxf(ceilf(work * (1.0f + 0x1p-11f) * fast_rcp(room)), (float)kLeastPages), cost = (float)k * (pages + kPieceCost);
+    if (room > 0.0f && cost < best) { best = cost; per = (int)fminf(pages, 1e9f); }
   }
-  return per ? per : (int)fmin(fmax(ceil(2.0 * work / places), (double)kLeastPages), 1e9);
+  return per ? per : (int)fminf(fmaxf(ceilf(2.0f * work * fast_rcp((float)places)), (float)kLeastPages), 1e9f);
 }
-// Piece number `at` of the list (sequence by sequence; of one its pieces, of those the key heads, of those the tiles); with one_s at least 0 the first piece of that sequence's unit (kv, tile).
-__device__ __forceinline__ Piece schedule(const TreeAttendArgs& a, int64_t at, int one_s, int kv, int tile) {
-  double work = 0.0, units = 0.0;
-  Units u{0, 0};
+// Piece number `at` of the list: sequence by sequence; of one its pieces, of those the key heads, of those the tiles.  By the whole wave.
+__device__ __forceinline__ Piece schedule(const TreeAttendArgs& a, int64_t at) {
+  float work = 0.0f, units = 0.0f;
+  TreePages sp;
+  int pages = 0, tiles = 0;
+  auto look = [&](int b) {
+    const int s = b + lane_id();
+    pages = tiles = 0;
+    if (s < a.t.seqs) {
+      sp = tree_pages(a, s);
+      pages = max(sp.last - sp.first, 0);
+      tiles = pages ? ceil_div_d(sp.tree.n * a.group, kTreeRows) : 0;
+    }
+  };
   for (int b = 0; b < a.t.seqs; b += kWave) {
-    u = units_of(a, b + lane_id());
-    work += (double)u.pages * u.tiles;
-    units += u.tiles;
+    look(b);
+    work += (float)pages * (float)tiles;
+    units += (float)tiles;
   }
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) { work += __shfl_xor(work, d); units += __shfl_xor(units, d); }
-  const int per = uniform(pages_of_piece(work * a.c.heads, units * a.c.heads, a.places));
+  const int per = uniform(pages_of_piece(wave_total(work) * (float)a.c.heads, wave_total(units) * (float)a.c.heads, a.places));
   int64_t first = 0, cells = 0;    // of the sequences before these 64
   for (int b = 0; b < a.t.seqs; b += kWave) {
-    if (a.t.seqs > kWave) u = units_of(a, b + lane_id());
-    const int pieces = ceil_div_d(u.pages, per), each = u.tiles * a.c.heads, count = pieces * each, cut = pieces > 1 ? count : 0;
-    int upto = count, cells_upto = cut;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int x = __shfl_up(upto, d), y = __shfl_up(cells_upto, d);
-      upto += lane_id() >= d ? x : 0;
-      cells_upto += lane_id() >= d ? y : 0;
-    }
-    const unsigned long long hit = __ballot(one_s >= 0 ? b + lane_id() == one_s : count > 0 && at >= first + upto - count && at < first + upto);
+    if (a.t.seqs > kWave) look(b);
+    const int pieces = ceil_div_d(pages, per), each = tiles * a.c.heads, count = pieces * each, cut = pieces > 1 ? count : 0;
+    const int upto = wave_incl_scan(count), cells_upto = wave_incl_scan(cut);
+    const unsigned long long hit = __ballot(count > 0 && at >= first + upto - count && at < first + upto);
     if (hit) {
-      const int lane = __builtin_ctzll(hit), its_pieces = __shfl(pieces, lane), its_each = __shfl(each, lane), tiles = __shfl(u.tiles, lane);
-      const int64_t cell = cells + __shfl(cells_upto - cut, lane);
-      int i = 0;
-      if (one_s < 0) {
-        i = (int)(at - first) - __shfl(upto - count, lane);
-        tile = i % tiles;
-        kv = i / tiles % a.c.heads;
-      }
-      return {uniform(b + lane), uniform(kv), uniform(tile), its_each ? uniform(i / its_each) : 0, uniform(its_pieces), cell + kv * tiles + tile, its_each};
+      const int lane = uniform(__builtin_ctzll(hit));
+      auto its = [&](int v) { return __builtin_amdgcn_readlane(v, lane); };
+      Piece p;
+      p.sp = TreePages{Tree{of_lane(sp.tree.first, lane), its(sp.tree.n)}, of_lane(sp.at, lane), its(sp.len), its(sp.ctx), its(sp.lo), its(sp.first), its(sp.last)};
+      p.pieces = its(pieces);
+      p.stride = its(each);
+      const int i = (int)(at - first) - its(upto - count), n = its(tiles);
+      p.tile = i % n;
+      p.kv = i / n % a.c.heads;
+      p.piece = i / (int)p.stride;
+      p.cell = cells + its(cells_upto - cut) + p.kv * n + p.tile;
+      if (i == 0 && threadIdx.x == 0) a.cuts[b + lane] = make_int4((int)p.cell, (int)p.stride, p.pieces, n);
+      return p;
     }
-    first += __shfl(upto, kWave - 1);
-    cells += __shfl(cells_upto, kWave - 1);
+    first += __builtin_amdgcn_readlane(upto, kWave - 1);
+    cells += __builtin_amdgcn_readlane(cells_upto, kWave - 1);
   }
-  return {-1, 0, 0, 0, 0, 0, 0};
+  Piece none{};
+  return none;
 }
 
 // Of the tree's nodes first .. first + 63 (first may be negative) those that node i, whose ancestors are at `up`, sees: bits; above: how many of its ancestors and itself come behind them.
@@ -598,9 +616,9 @@ __global__ void __launch_bounds__(256, kTreeResident) k_tree_attend(TreeAttendAr
   const unsigned die = blockIdx.x % 8, turn = blockIdx.x / 8;
   const int64_t number = (int64_t)(turn / 16 * 8 + die) * 16 + turn % 16;
   if (a.chunk == 0) {
-    const Piece mine = schedule(a, number, -1, 0, 0);
-    if (mine.s < 0) return;
-    at.sp = tree_pages(a, mine.s);
+    const Piece mine = schedule(a, number);
+    if (mine.pieces == 0) return;
+    at.sp = mine.sp;
     at.kv = mine.kv;
     at.tile = mine.tile;
     const int pages = ceil_div_d(at.sp.last - at.sp.first, mine.pieces);
@@ -726,31 +744,33 @@ __global__ void __launch_bounds__(256) k_tree_join(TreeAttendArgs a) {
   const TreePages sp = tree_pages(a, place.z);
   const int64_t node = token - sp.tree.first;
   if (node < 0 || node >= sp.tree.n) return;
-  const bool none = sp.first >= sp.last;
+  int pieces = 0;
+  int64_t cell0 = 0, stride = 0;         // cell0: of key head kv, the first tile, the first piece
+  int tiles = a.tiles;
+  if (sp.first < sp.last) {
+    if (a.chunk == 0) {
+      const Cut cut = load_uniform(a.cuts + place.z);
+      pieces = cut.z;
+      tiles = cut.w;
+      cell0 = cut.x;
+      stride = cut.y;
+    } else {
+      const int c0 = sp.first / a.chunk;
+      pieces = (sp.last - 1) / a.chunk + 1 - c0;
+      cell0 = (sp.at / a.chunk + place.z + c0) * a.c.heads * a.tiles;
+      stride = (int64_t)a.c.heads * a.tiles;
+    }
+    if (pieces == 1) return;
+  }
   const int first = (int)node * a.group;
   for (int g = threadIdx.x / kWave; g < a.group; g += 4) {
-    const int rr = first + g, tile = rr / kTreeRows, d = lane_id() % kThreads * 4, mine = lane_id() / kThreads;
-    int64_t cell = 0, stride = 0;
-    int pieces = 0;
-    if (!none) {
-      if (a.chunk == 0) {
-        const Piece p = schedule(a, 0, place.z, kv, tile);
-        cell = p.cell;
-        stride = p.stride;
-        pieces = p.pieces;
-      } else {
-        const int c0 = sp.first / a.chunk;
-        pieces = (sp.last - 1) / a.chunk + 1 - c0;
-        cell = ((sp.at / a.chunk + place.z + c0) * a.c.heads + kv) * a.tiles + tile;
-        stride = (int64_t)a.c.heads * a.tiles;
-      }
-      if (pieces == 1) return;
-    }
+    const int rr = first + g, d = lane_id() % kThreads * 4, mine = lane_id() / kThreads;
+    const int64_t cell = cell0 + (int64_t)kv * tiles + rr / kTreeRows;
     float top = -INFINITY, sum = 0.0f;
     f32x4 v = {0, 0, 0, 0};
 #pragma unroll 4
     for (int c = mine; c < pieces; c += kLanes) {
-      if (cell + c * stride >= a.cells) break;
+      if ((uint64_t)(cell + c * stride) >= (uint64_t)a.cells) break;
       const int64_t row = (cell + c * stride) * a.part_rows + rr % kTreeRows;
       const float2 ml = a.part_ml[row];
       const f32x4 w = *reinterpret_cast<const f32x4*>(a.part + row * R + d);
