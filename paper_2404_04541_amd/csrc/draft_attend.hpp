@@ -148,7 +148,7 @@ __device__ __forceinline__ TreePages tree_pages(const TreeAttendArgs& a, int s) 
 // units), and cost k (per + kPieceCost) pages' time, kPieceCost for what a workgroup does beside its pages; the best k up to 4 is taken.  Where units are more than that, only what is longer than twice the average
 // is cut.  (All pieces of the same length in no whole number of turns were worst: four sequences, 60 nodes, 65 011 tokens, 337 us with about 1.6 turns of 60 pages.)
 constexpr int kMostEven = 512;     // sequences that a workgroup looks through
-constexpr int kLeastPages = 4, kPieceCost = 3, kMostTurns = 4;
+constexpr int kLeastPages = 4, kPieceCost = 8, kMostTurns = 4;
 struct Piece {
   TreePages sp;                    // of its sequence
   int kv, tile, piece, pieces;     // pieces: of the unit; 0 where there is nothing to do
@@ -514,7 +514,7 @@ struct TreeTiles {
   __align__(16) unsigned char k[2][kPage * R * 2], v[2][kPage * R * 2];
 };
 template <typename T, int R, bool CAP, bool BIAS>
-__device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const TreePlace& at, TreeRows<T, R, CAP, BIAS>& rows, const vec8<T>* q, TreeTiles<T, R>& tiles) {
+__device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const TreePlace& at, TreeRows<T, R, CAP, BIAS>& rows, const vec8<T>* q, bool busy, TreeTiles<T, R>& tiles) {
   using SK = TileShape<R>;
   using SV = TileShape<64>;
   constexpr int kSteps = R / 16, kBlocks = R / 32, kPieces = kPage * R / 16 / 256;        // 16 bytes of a page that a thread brings
@@ -579,7 +579,7 @@ __device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const Tr
     const int64_t next = page_of(n + 1);
     if (next >= 0) load(next);
     __syncthreads();                                 // the page is there; the one before it is not read any more
-    if (page >= 0) {
+    if (page >= 0 && busy) {
       const unsigned char *kt = tiles.k[from], *vt = tiles.v[from];
       f32x16 x[2];
 #pragma unroll
@@ -661,10 +661,14 @@ __global__ void __launch_bounds__(256, kTreeResident) k_tree_attend(TreeAttendAr
       q[i] = __builtin_bit_cast(vec8<T>, w);
     }
   }
-  struct Joined { float ms[4][32], ls[4][32]; __align__(16) float sums[4][32][R + 4]; };
+  struct Joined {
+    float ms[4][32], ls[4][32], by[4][32];             // by: what a wave's sums of a row are multiplied by
+    int64_t to[kTreeRows];                             // bytes from the results' first element, of a row that is written there
+    __align__(16) float sums[4][32][R + 4];
+  };
   __shared__ __align__(16) union { TreeTiles<T, R> tiles; Joined joined; } lds;
   bool strange;
-  if (blocks == 4) strange = tree_many_rows<T, R, CAP, BIAS>(a, at, rows, q, lds.tiles);
+  if (blocks == 4) strange = tree_many_rows<T, R, CAP, BIAS>(a, at, rows, q, block * 32 < at.rows, lds.tiles);
   else strange = tree_few_rows<T, R, CAP, BIAS>(a, at, rows, block, blocks, q);
   strange = __syncthreads_or(strange);             // (and the tiles are not read any more)
   const float m = rows.m, l = add_halves(rows.l);
@@ -703,31 +707,39 @@ __global__ void __launch_bounds__(256, kTreeResident) k_tree_attend(TreeAttendAr
     }
     __syncthreads();
   }
-  for (int i = threadIdx.x; i < at.rows * (R / 4); i += 256) {
-    const int row = i / (R / 4), d = i % (R / 4) * 4, mine = row % 32;
-    float top = -INFINITY;
-    for (int w = row / 32; w < 4; w += blocks) top = fmaxf(top, j.ms[w][mine]);
+  const int row = threadIdx.x;
+  if (row < at.rows) {
+    const int first = row / 32, mine = row % 32;
+    float top = -INFINITY, sum = 0.0f;
+    for (int w = first; w < 4; w += blocks) top = fmaxf(top, j.ms[w][mine]);
     const float base = top == -INFINITY ? 0.0f : top;
-    f32x4 v = {0, 0, 0, 0};
-    float sum = 0.0f;
-    for (int w = row / 32; w < 4; w += blocks) {
+    for (int w = first; w < 4; w += blocks) {
       const float f = fast_exp2(j.ms[w][mine] - base);
-      v += *reinterpret_cast<const f32x4*>(&j.sums[w][mine][d]) * f;
       sum += j.ls[w][mine] * f;
+      j.by[w][mine] = f;
     }
     if (at.cell < 0) {
-      if (d < a.c.bytes8) {
-        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-        const int rt = at.tile * kTreeRows + row;
-        const RowSource dst = a.o.of(at.kv * a.group + rt % a.group);
-        T out[4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) out[b] = (T)(v[b] * by);
-        *reinterpret_cast<u32x2*>(const_cast<unsigned char*>(dst.base) + (sp.tree.first + rt / a.group) * dst.stride + d * 2) = __builtin_bit_cast(u32x2, out);
-      }
+      const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+      for (int w = first; w < 4; w += blocks) j.by[w][mine] *= by;
+      const int rt = at.tile * kTreeRows + row;
+      j.to[row] = (sp.tree.first + rt / a.group) * a.o.stride + (int64_t)(at.kv * a.group + rt % a.group) * a.o.head;
     } else {
-      *reinterpret_cast<f32x4*>(a.part + (at.cell * a.part_rows + row) * R + d) = v;
-      if (d == 0) a.part_ml[at.cell * a.part_rows + row] = make_float2(top, sum);
+      a.part_ml[at.cell * a.part_rows + row] = make_float2(top, sum);
+    }
+  }
+  __syncthreads();
+  // a thread has four channels of every (1024 / R)-th row
+  constexpr int kThreads = R / 4, kStep = 256 / kThreads;
+  const int d = threadIdx.x % kThreads * 4;
+  for (int i = threadIdx.x / kThreads; i < at.rows; i += kStep) {
+    f32x4 v = *reinterpret_cast<const f32x4*>(&j.sums[i / 32][i % 32][d]) * j.by[i / 32][i % 32];
+    for (int w = i / 32 + blocks; w < 4; w += blocks) v += *reinterpret_cast<const f32x4*>(&j.sums[w][i % 32][d]) * j.by[w][i % 32];
+    if (at.cell >= 0) *reinterpret_cast<f32x4*>(a.part + (at.cell * a.part_rows + i) * R + d) = v;
+    else if (d < a.c.bytes8) {
+      T out[4];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) out[b] = (T)v[b];
+      *reinterpret_cast<u32x2*>(a.o.base + j.to[i] + d * 2) = __builtin_bit_cast(u32x2, out);
     }
   }
 }
