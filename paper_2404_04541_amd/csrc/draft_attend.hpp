@@ -152,7 +152,7 @@ constexpr int kLeastPages = 4, kPieceCost = 8, kMostTurns = 4;
 struct Piece {
   TreePages sp;                    // of its sequence
   int kv, tile, piece, pieces;     // pieces: of the unit; 0 where there is nothing to do
-  int64_t cell, stride;            // of the unit's first piece, to the next one
+  int64_t cell;                    // -1 where the unit is not cut
 };
 // What the join has to know of a sequence: cell of the first piece of its first unit, how far the next piece's is, how many pieces.
 typedef int4 Cut;
@@ -182,7 +182,7 @@ __device__ __forceinline__ int pages_of_piece(float work, float units, int place
   }
   return per ? per : (int)fminf(fmaxf(ceilf(2.0f * work * fast_rcp((float)places)), (float)kLeastPages), 1e9f);
 }
-// Piece number `at` of the list: sequence by sequence; of one its pieces, of those the key heads, of those the tiles.  By the whole wave.
+// Piece number `at` of the list: those of cut units first, which take longest; sequence by sequence; of one its pieces, of those the key heads, of those the tiles.  By the whole wave.
 __device__ __forceinline__ Piece schedule(const TreeAttendArgs& a, int64_t at) {
   float work = 0.0f, units = 0.0f;
   TreePages sp;
@@ -202,32 +202,30 @@ __device__ __forceinline__ Piece schedule(const TreeAttendArgs& a, int64_t at) {
     units += (float)tiles;
   }
   const int per = uniform(pages_of_piece(wave_total(work) * (float)a.c.heads, wave_total(units) * (float)a.c.heads, a.places));
-  int64_t first = 0, cells = 0;    // of the sequences before these 64
-  for (int b = 0; b < a.t.seqs; b += kWave) {
-    if (a.t.seqs > kWave) look(b);
-    const int pieces = ceil_div_d(pages, per), each = tiles * a.c.heads, count = pieces * each, cut = pieces > 1 ? count : 0;
-    const int upto = wave_incl_scan(count), cells_upto = wave_incl_scan(cut);
-    const unsigned long long hit = __ballot(count > 0 && at >= first + upto - count && at < first + upto);
-    if (hit) {
-      const int lane = uniform(__builtin_ctzll(hit));
-      auto its = [&](int v) { return __builtin_amdgcn_readlane(v, lane); };
-      Piece p;
-      p.sp = TreePages{Tree{of_lane(sp.tree.first, lane), its(sp.tree.n)}, of_lane(sp.at, lane), its(sp.len), its(sp.ctx), its(sp.lo), its(sp.first), its(sp.last)};
-      p.pieces = its(pieces);
-      p.stride = its(each);
-      const int i = (int)(at - first) - its(upto - count), n = its(tiles);
-      p.tile = i % n;
-      p.kv = i / n % a.c.heads;
-      p.piece = i / (int)p.stride;
-      p.cell = cells + its(cells_upto - cut) + p.kv * n + p.tile;
-      if (i == 0 && threadIdx.x == 0) a.cuts[b + lane] = make_int4((int)p.cell, (int)p.stride, p.pieces, n);
-      return p;
+  Piece p{};
+  int64_t before = 0;              // pieces of cut units, then of all, of the sequences before these 64
+  for (int cut = 1; cut >= 0 && p.pieces == 0; --cut)
+    for (int b = 0; b < a.t.seqs; b += kWave) {
+      if (a.t.seqs > kWave) look(b);
+      const int pieces = ceil_div_d(pages, per), each = tiles * a.c.heads, count = (pieces > 1) == (cut == 1) ? pieces * each : 0;
+      const int upto = wave_incl_scan(count);
+      const unsigned long long hit = __ballot(count > 0 && at >= before + upto - count && at < before + upto);
+      if (hit) {
+        const int lane = uniform(__builtin_ctzll(hit));
+        auto its = [&](int v) { return __builtin_amdgcn_readlane(v, lane); };
+        p.sp = TreePages{Tree{of_lane(sp.tree.first, lane), its(sp.tree.n)}, of_lane(sp.at, lane), its(sp.len), its(sp.ctx), its(sp.lo), its(sp.first), its(sp.last)};
+        p.pieces = its(pieces);
+        p.cell = cut ? at : -1;
+        const int first = its(upto - count), i = (int)(at - before) - first, n = its(tiles), stride = its(each);
+        p.tile = i % n;
+        p.kv = i / n % a.c.heads;
+        p.piece = i / stride;
+        if (i == 0 && threadIdx.x == 0) a.cuts[b + lane] = make_int4((int)at, stride, p.pieces, n);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(upto, kWave - 1);
     }
-    first += __builtin_amdgcn_readlane(upto, kWave - 1);
-    cells += __builtin_amdgcn_readlane(cells_upto, kWave - 1);
-  }
-  Piece none{};
-  return none;
+  return p;
 }
 
 // Of the tree's nodes first .. first + 63 (first may be negative) those that node i, whose ancestors are at `up`, sees: bits; above: how many of its ancestors and itself come behind them.
@@ -624,7 +622,7 @@ __global__ void __launch_bounds__(256, kTreeResident) k_tree_attend(TreeAttendAr
     const int pages = ceil_div_d(at.sp.last - at.sp.first, mine.pieces);
     at.begin = uniform(at.sp.first + mine.piece * pages);
     at.end = uniform(min(at.begin + pages, at.sp.last));
-    at.cell = mine.pieces > 1 ? mine.cell + mine.piece * mine.stride : -1;
+    at.cell = mine.cell;
   } else {
     // many sequences: places of chunks, found without knowing the lengths.  s has ptr[s] / chunk + s and on
     at.tile = (int)(number % a.tiles);
