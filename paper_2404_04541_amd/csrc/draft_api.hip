@@ -207,7 +207,7 @@ int spdraft_keep(spgemm_handle h, const spcache* c, const spgemm_csr* table, con
     a.t = view(table, lens);
     a.trees = view(t, nullptr);
     a.path = path; a.kept = kept; a.new_lens = new_lens;
-    const dim3 grid((unsigned)t->rows, (unsigned)c->kv_heads, (unsigned)(2 * c->layers));
+    const dim3 grid((unsigned)t->rows, (unsigned)c->kv_heads, (unsigned)ceil_div(2 * c->layers, 4));
     if (room_of(c) == 64) k_draft_keep<64><<<grid, dim3(256), 0, h->stream>>>(a);
     else k_draft_keep<128><<<grid, dim3(256), 0, h->stream>>>(a);
     return launched(h);

@@ -1,7 +1,8 @@
 // The nodes that stay move together: token start + way[i] of a sequence becomes token start + i, in all layers, keys and values.
 //
-// A workgroup has a sequence, a key head, a layer, and keys or values.  It goes over the pages that tokens come to, in order: way[i] >= i, so what a page's tokens are taken from lies in the page or
-// behind it, and nothing that is still to be read has been written.  A page's tokens are gathered in LDS first, with the largest magnitude that comes from other pages; then the scale is known.
+// A wave has a sequence, a key head, a layer, and keys or values; the four of a workgroup share what they have to know of the sequence.  It goes over the pages that tokens come to, in order: way[i] >= i, so what
+// a page's tokens are taken from lies in the page or behind it, and nothing that is still to be read has been written.  Only where tokens come from another page are they read twice, first for the scale.
+// A step moves few bytes, and what it costs is the chain of loads that leads to them: a whole workgroup for what a wave has now made six turns of the card of it, 47 us for 48 sequences in 16 layers of 8 heads.
 #pragma once
 #include "draft_attend.hpp"
 
@@ -27,15 +28,20 @@ struct Way {
   int64_t page[kKeepPlaces];      // of places start / 64 and on; -1: none
 };
 
+// What the wave's lanes have put into LDS is there for the others.
+__device__ __forceinline__ void in_wave_order() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
+}
+
 template <int R>
 __global__ void __launch_bounds__(256) k_draft_keep(KeepArgs a) {
   __shared__ Way way;
-  __shared__ __align__(16) unsigned char codes[R * (kPage + 4)];      // keys: [token][R], values: [channel][64 + 4]
-  __shared__ float tops[4];
-  const int s = blockIdx.x, head = blockIdx.y, layer = blockIdx.z / 2, values = blockIdx.z % 2, tid = threadIdx.x;
+  __shared__ unsigned tiles[2][R][kPage / 4 + 1];           // of the two waves that have values
+  const int s = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, lane = lane_id(), wave = uniform(tid / kWave), unit = blockIdx.z * 4 + wave;
+  const int layer = unit / 2, values = unit % 2;
   const Tree tree = tree_of(a.trees, s);
   const int64_t len = a.t.lens[s], start = len - tree.n;
-  const bool first = head == 0 && blockIdx.z == 0 && tid == 0;
   const int asked = min(max(a.kept[s], 0), tree.n);
   if (tid == 0) way.count = asked;
   __syncthreads();
@@ -53,86 +59,126 @@ __global__ void __launch_bounds__(256) k_draft_keep(KeepArgs a) {
     way.page[tid] = page;
   }
   lacks = __syncthreads_or(lacks);
-  const int count = way.count;
-  if (first) a.new_lens[s] = (int)(lacks ? len : start + count);
-  if (lacks || count == 0 || way.i[count - 1] == count - 1) return;      // nothing moves
+  const int count = uniform(way.count);
+  if (head == 0 && blockIdx.z == 0 && tid == 0) a.new_lens[s] = (int)(lacks ? len : start + count);
+  if (lacks || count == 0 || layer >= a.layers || uniform(way.i[count - 1]) == count - 1) return;      // nothing moves
 
   const int64_t layer0 = (int64_t)layer * a.pages;
   unsigned char* const data = a.data[values];
   float* const scale = a.scale[values];
   auto cell = [&](int place) { return (layer0 + way.page[place]) * a.heads + head; };
-  for (int place = 0; place * kPage + (int64_t)place0 * kPage < start + count; ++place) {
-    const int64_t t0 = (int64_t)(place0 + place) * kPage;                              // the page's first token
-    const int begin = (int)(start > t0 ? start - t0 : 0), until = (int)(start + count - t0 < kPage ? start + count - t0 : kPage);
-    const int i0 = (int)(t0 + begin - start), moves = until - begin;
-    if (way.i[i0 + moves - 1] == i0 + moves - 1) continue;
+  const int start0 = (int)(start - (int64_t)place0 * kPage);                         // the tree's first token, counted from the first page's first one, as all tokens are from here on
+  for (int place = 0; place * kPage < start0 + count; ++place) {
+    const int t0 = place * kPage, begin = max(start0 - t0, 0), until = min(start0 + count - t0, kPage);
+    const int i0 = t0 + begin - start0, last = i0 + until - begin - 1;
+    if (uniform(way.i[last]) == last) continue;
+    auto source = [&](int o) { return start0 + way.i[t0 + o - start0]; };            // of the page's token o
     const int64_t mine = cell(place);
     const float old = scale[mine];
-    auto source = [&](int i) { return start + way.i[i0 + i] - (int64_t)place0 * kPage; };   // counted from the first page's first token
-    float top = 0.0f;
-    auto measure = [&](float code, float by) { const float v = fabsf(code) * by; top = v < INFINITY ? fmaxf(top, v) : top; };
-    if (!values) {
-      for (int n = tid; n < moves * (R / 4); n += 256) {
-        const int i = n / (R / 4), w = n % (R / 4), from = (int)source(i);
+    float now = old;
+    if (source(until - 1) / kPage != place) {
+      // what comes from other pages: its largest magnitude
+      float top = 0.0f;
+      auto measure = [&](float code, float by) { const float v = fabsf(code) * by; top = v < INFINITY ? fmaxf(top, v) : top; };
+      for (int o = begin; o < until; ++o) {
+        const int from = uniform(source(o));
+        if (from / kPage == place) continue;
         const int64_t c = cell(from / kPage);
-        const unsigned code = *reinterpret_cast<const unsigned*>(data + c * (kPage * R) + from % kPage * R + 4 * w);
-        *reinterpret_cast<unsigned*>(codes + i * R + 4 * w) = code;
-        if (from / kPage != place && 4 * w < a.bytes8) {
-          const float by = scale[c];
-          measure(__builtin_amdgcn_cvt_f32_fp8(code, 0), by);
-          measure(__builtin_amdgcn_cvt_f32_fp8(code, 1), by);
-          measure(__builtin_amdgcn_cvt_f32_fp8(code, 2), by);
-          measure(__builtin_amdgcn_cvt_f32_fp8(code, 3), by);
+        const float by = scale[c];
+        if (!values) {
+          if (4 * lane < a.bytes8) {
+            const unsigned code = *reinterpret_cast<const unsigned*>(data + c * (kPage * R) + from % kPage * R + 4 * lane);
+            measure(__builtin_amdgcn_cvt_f32_fp8(code, 0), by);
+            measure(__builtin_amdgcn_cvt_f32_fp8(code, 1), by);
+            measure(__builtin_amdgcn_cvt_f32_fp8(code, 2), by);
+            measure(__builtin_amdgcn_cvt_f32_fp8(code, 3), by);
+          }
+        } else {
+          for (int d = lane; d < a.bytes8; d += kWave) measure(__builtin_amdgcn_cvt_f32_fp8(data[c * (kPage * R) + d * kPage + from % kPage], 0), by);
         }
       }
-    } else {
-      for (int n = tid; n < moves * R; n += 256) {
-        const int i = n / R, d = n % R, from = (int)source(i);
-        const int64_t c = cell(from / kPage);
-        const unsigned code = data[c * (kPage * R) + d * kPage + from % kPage];
-        codes[d * (kPage + 4) + begin + i] = (unsigned char)code;
-        if (from / kPage != place && d < a.bytes8) measure(__builtin_amdgcn_cvt_f32_fp8(code, 0), scale[c]);
-      }
-    }
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    if (lane_id() == 0) tops[tid / kWave] = top;
-    __syncthreads();
-    const float now = fmaxf(old, scale_for(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]))));
+      for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+      now = fmaxf(old, scale_for(top));
+    }
     const bool grows = now > old;
-    if (tid == 0 && grows) scale[mine] = now;                // (everybody has the old one)
-    auto by_of = [&](int i) { const int from = (int)source(i) / kPage; return from == place ? old / now : scale[cell(from)] / now; };
+    if (grows && lane == 0) scale[mine] = now;
+    auto by_of = [&](int from) { return from / kPage == place ? old / now : scale[cell(from / kPage)] / now; };
     unsigned char* const to = data + mine * (kPage * R);
     if (!values) {
-      for (int n = tid; n < moves * (R / 4); n += 256) {
-        const int i = n / (R / 4), w = n % (R / 4);
-        const float by = by_of(i);
-        const unsigned code = *reinterpret_cast<const unsigned*>(codes + i * R + 4 * w);
-        *reinterpret_cast<unsigned*>(to + (begin + i) * R + 4 * w) = by == 1.0f ? code : rescale8(code, by);
+      // 16 tokens on their way together; a token is R / 4 words
+      constexpr int kWords = R / 4, kTokens = kWave / kWords, kLoads = 16 / kTokens;
+      const int w = lane % kWords;
+      for (int o0 = begin; o0 < until; o0 += 16) {
+        unsigned code[kLoads];
+        float by[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int o = o0 + i * kTokens + lane / kWords;
+          by[i] = 1.0f;
+          if (o < until) {
+            const int from = source(o);
+            code[i] = *reinterpret_cast<const unsigned*>(data + cell(from / kPage) * (kPage * R) + from % kPage * R + 4 * w);
+            by[i] = by_of(from);
+          }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (the tokens are there before others take their places)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int o = o0 + i * kTokens + lane / kWords;
+          if (o < until) *reinterpret_cast<unsigned*>(to + o * R + 4 * w) = by[i] == 1.0f ? code[i] : rescale8(code[i], by[i]);
+        }
       }
       if (grows)
-        for (int n = tid; n < begin * (R / 4); n += 256) reinterpret_cast<unsigned*>(to)[n] = rescale8(reinterpret_cast<unsigned*>(to)[n], old / now);
+        for (int n = lane; n < begin * kWords; n += kWave) reinterpret_cast<unsigned*>(to)[n] = rescale8(reinterpret_cast<unsigned*>(to)[n], old / now);
     } else {
-      const int w0 = grows ? 0 : begin / 4, words = (until + 3) / 4 - w0;
-      for (int n = tid; n < words * R; n += 256) {
-        const int d = n / words, o = (w0 + n % words) * 4;
-        unsigned* p = reinterpret_cast<unsigned*>(to + d * kPage + o);
-        const unsigned was = *p, again = grows ? rescale8(was, old / now) : was;
-        unsigned word = 0;
+      // the page's values come to LDS as rows of 16 bytes and go back so, a row of 64 tokens to a channel; in between a lane has R / 64 channels
+      constexpr int kChannels = R / kWave, kRows = kWave / 4, kPitch = kPage / 4 + 1;      // words of a row in LDS: no two of 64 rows begin in the same bank
+      unsigned(&tile)[R][kPitch] = tiles[wave / 2];
+      const int w0 = grows ? 0 : begin / 4, w1 = (until + 3) / 4;
+      u32x4 chunk[R / kRows];
+#pragma unroll
+      for (int i = 0; i < R / kRows; ++i) chunk[i] = *reinterpret_cast<const u32x4*>(to + (lane / 4 + i * kRows) * kPage + lane % 4 * 16);
+#pragma unroll
+      for (int i = 0; i < R / kRows; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) tile[lane / 4 + i * kRows][lane % 4 * 4 + j] = chunk[i][j];
+      in_wave_order();
+      for (int w = w0; w < w1; ++w) {
+        unsigned word[kChannels];
+#pragma unroll
+        for (int c = 0; c < kChannels; ++c) word[c] = tile[lane + c * kWave][w];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-          unsigned byte = (o + b < begin ? again : was) >> (8 * b) & 0xffu;
-          if (o + b >= begin && o + b < until) {
-            byte = codes[d * (kPage + 4) + o + b];
-            const float by = by_of(o + b - begin);
-            if (by != 1.0f) byte = to8(__builtin_amdgcn_cvt_f32_fp8(byte, 0) * by, 0.0f, 0.0f, 0.0f) & 0xffu;
+          const int o = 4 * w + b;
+          if (o >= until) break;
+          const int from = o < begin ? t0 + o : uniform(source(o));
+          const float by = by_of(from);
+          if (from == t0 + o && by == 1.0f) continue;
+#pragma unroll
+          for (int c = 0; c < kChannels; ++c) {
+            unsigned x;
+            if (from / kPage == place) x = reinterpret_cast<const unsigned char*>(tile[lane + c * kWave])[from % kPage];
+            else x = data[cell(from / kPage) * (kPage * R) + (lane + c * kWave) * kPage + from % kPage];
+            if (by != 1.0f) x = to8(__builtin_amdgcn_cvt_f32_fp8(x, 0) * by, 0.0f, 0.0f, 0.0f) & 0xffu;
+            word[c] = (word[c] & ~(0xffu << (8 * b))) | x << (8 * b);
           }
-          word |= byte << (8 * b);
         }
-        *p = word;
+#pragma unroll
+        for (int c = 0; c < kChannels; ++c) tile[lane + c * kWave][w] = word[c];      // (what a later token is taken from lies behind)
       }
+      in_wave_order();
+      if (lane % 4 >= w0 / 4 && lane % 4 <= (w1 - 1) / 4)
+#pragma unroll
+        for (int i = 0; i < R / kRows; ++i) {
+          u32x4 v;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = tile[lane / 4 + i * kRows][lane % 4 * 4 + j];
+          *reinterpret_cast<u32x4*>(to + (lane / 4 + i * kRows) * kPage + lane % 4 * 16) = v;
+        }
+      in_wave_order();
     }
-    __syncthreads();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
 }
 
