@@ -41,11 +41,29 @@ __device__ __forceinline__ Loaded<T> load_some(const T* row, int64_t at, int voc
   return r;
 }
 
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) v += __shfl_xor(v, d);
-  return v;
+// Sums of 64 bits over the lanes up to each, by moves within the registers.
+template <int CTRL, int ROWS, bool BOUND>
+__device__ __forceinline__ double from_lanes(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)u, CTRL, ROWS, 0xf, BOUND), hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, ROWS, 0xf, BOUND);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
+__device__ __forceinline__ double row_scan(double v) {      // over the 16 lanes of a row
+  v += from_lanes<0x111, 0xf, true>(v);
+  v += from_lanes<0x112, 0xf, true>(v);
+  v += from_lanes<0x114, 0xf, true>(v);
+  return v + from_lanes<0x118, 0xf, true>(v);
+}
+__device__ __forceinline__ double wave_scan(double v) {
+  v = row_scan(v);
+  v += from_lanes<0x142, 0xa, false>(v);      // the last lane of rows 0 and 2 to rows 1 and 3, then of row 1 to rows 2 and 3
+  return v + from_lanes<0x143, 0xc, false>(v);
+}
+__device__ __forceinline__ double lane_of(double v, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(u >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)u, lane));
+}
+__device__ __forceinline__ double wave_sum(double v) { return lane_of(wave_scan(v), kWave - 1); }
 
 // Is child `i` taken at its parent's rows as they are?
 template <typename T, bool DRAFT>
@@ -232,14 +250,12 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
     __syncthreads();
     have = true;
   };
-  auto total = [&](int which) {
-    double v = 0.0;
-    for (int w = 0; w < kVerifyWaves; ++w) v += parts[which][w];
-    return v;
-  };
+  static_assert(kVerifyWaves == 16, "a row of lanes");
+  auto total = [&](int which) { return lane_of(row_scan(parts[which][lane % kVerifyWaves]), kVerifyWaves - 1); };
   // the sum over children of f(group, lane's child)
   auto over = [&](auto f) {
     double v = 0.0;
+    if (groups == 0) return v;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
       if (g < groups && x[g] >= 0) v += f(g);
@@ -325,18 +341,14 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
   int begin = 0, size = part;
   double sum = 0.0;
   for (int level = 0; level < 2; ++level) {
-    int pick = -1;
-    double at = sum;
-    for (int i = 0; i < kVerifyWaves; ++i) {
-      const double mine = parts[0][i];
-      if (mine > 0.0 && (pick < 0 || at <= goal)) { pick = i; sum = at; }
-      at += mine;
-      if (at > goal && pick >= 0) break;
-    }
-    if (pick < 0) {                      // (nothing above 0)
+    const double mine16 = parts[0][lane % kVerifyWaves], upto16 = row_scan(mine16);
+    const unsigned some = (unsigned)__ballot(mine16 > 0.0) & 0xffffu, passed = (unsigned)__ballot(sum + upto16 > goal) & some;
+    if (!some) {                         // (nothing above 0)
       if (threadIdx.x == 0) a.onward[token] = make_int2(-1, -1);
       return;
     }
+    const int pick = passed ? __builtin_ctz(passed) : 31 - __builtin_clz(some);
+    sum += lane_of(upto16, pick) - lane_of(mine16, pick);
     begin += pick * size;
     if (level == 1) break;
     const int limit = min(begin + size, a.vocab);
@@ -366,31 +378,21 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
         for (int i = 0; i < kCount; ++i) each[i] += kids.token[j] == v0 + i ? weights[j] : 0.0;
 #pragma unroll
     for (int i = 0; i < kCount; ++i) mine += each[i];
-    double upto = mine;                  // of the lanes up to this one
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const double o = __shfl_up(upto, d);
-      upto += lane >= d ? o : 0.0;
-    }
-    const double whole = __shfl(upto, kWave - 1);
+    const double upto = wave_scan(mine);
     double at = sum + (upto - mine);
-    int first = a.vocab, above = -1;     // the lane's first token that passes the goal, its last above 0
+    int first = -1, above = -1;          // the lane's first token that passes the goal, its last above 0
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
       at += each[i];
       if (each[i] > 0.0) {
         above = v0 + i;
-        if (at > goal && first == a.vocab) first = above;
+        if (at > goal && first < 0) first = above;
       }
     }
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      first = min(first, __shfl_xor(first, d));
-      above = max(above, __shfl_xor(above, d));
-    }
-    best = first < a.vocab ? first : max(best, above);
-    if (first < a.vocab) break;
-    sum += whole;
+    const unsigned long long some = __ballot(above >= 0), passed = __ballot(first >= 0);
+    if (passed) { best = __builtin_amdgcn_readlane(first, __builtin_ctzll(passed)); break; }
+    if (some) best = __builtin_amdgcn_readlane(above, 63 - __builtin_clzll(some));
+    sum += lane_of(upto, kWave - 1);
   }
   if (lane == 0) a.onward[token] = make_int2(-1, best);
 }
