@@ -68,8 +68,7 @@ def symbolic(handle: sg.Handle, ptr: torch.Tensor, parent: torch.Tensor, most: i
     t = TreesStruct(ptr.numel() - 1, parent.numel(), _array(ptr, "ptr", torch.int64, ptr), _array(parent, "parent", torch.int32, ptr), int(most))
     nbytes = max(lib.spdraft_plan_bytes(C.byref(t)), 1)
     memory = at._results(handle, lambda: ptr.new_empty(nbytes, dtype=torch.uint8))
-    checked = C.c_int32(0)
-    handle._check(lib.spdraft_symbolic(handle.ptr, C.byref(t), memory.data_ptr(), nbytes, C.byref(checked) if check else None))
+    handle._check(lib.spdraft_symbolic(handle.ptr, C.byref(t), memory.data_ptr(), nbytes, C.byref(C.c_int32(0)) if check else None))
     t.parent = None            # (what follows needs the plan only)
     return Trees(t, ptr, memory)
 

@@ -115,6 +115,35 @@ def test_attend(h, name, dtype):
     check(name, o, *tree_reference(HostCache(cache, 1), rows, lens, trees, q, 1 / math.sqrt(d), c.get("cap", 0.0), slopes, c.get("window", 0)))
 
 
+@pytest.mark.parametrize("seqs, longest", [(64, 3000), (65, 700), (200, 2000), (512, 1500), (513, 1500), (700, 40)])
+def test_attend_many_sequences(h, seqs, longest):
+    """Sequences of all lengths, some without a tree or without tokens: long ones among them are cut, and which workgroup has what is found in several steps, or by the table's row pointers."""
+    rng = random.Random(seqs)
+    trees = [grown(rng.choice([0, 1, 2, rng.randint(3, 40)]), 300 + s) for s in range(seqs)]
+    lens = [longest if s % 97 == 5 else len(t) + rng.choice([0, rng.randint(0, 100)]) if s % 11 else 0 for s, t in enumerate(trees)]
+    pages = sum(-(-n // PAGE) for n in lens) + 2
+    cache, rows = filled(48, 1, pages, 2, 64), rows_for(lens, pages, 3)
+    gen = torch.Generator(device="cuda").manual_seed(49)
+    q = randn(gen, (sum(map(len, trees)), 8, 64), BF, 1.5)
+    o = dr.attend(h, cache, 0, at.PageTable(*flat(rows)), i32(lens), planned(h, trees), q)
+    check("o", o, *tree_reference(HostCache(cache, 0), rows, lens, trees, q, 1 / 8))
+
+
+def test_attend_row_pointers_that_do_not_ascend(h):
+    """A table whose rows overlap and fall back: what that gives is not said, but nothing outside of what the call has is written."""
+    cache = filled(37, 1, 40, 2, 64)
+    before = clone(cache)
+    gen = torch.Generator(device="cuda").manual_seed(38)
+    trees = [grown(20, 39)] * 6
+    out = torch.full((140, 4, 64), 7.0, dtype=BF, device="cuda")
+    q, plan, lens = randn(gen, (120, 4, 64), BF), planned(h, trees), i32([2560] * 6)
+    table = at.PageTable(i64([0, 40, 0, 40, -9, 90, 40]), i32(list(range(40))))
+    rc = dr._lib().spdraft_attend(h.ptr, C.byref(cache._struct), 0, C.byref(table.struct(cache)), lens.data_ptr(), C.byref(plan._struct), plan.memory.data_ptr(), 4, at.BF16, 0.125, 0.0, None, 0,
+                                  at._tensor(q, "q"), at.TensorStruct(out.data_ptr(), 256, 64))
+    torch.cuda.synchronize()
+    assert rc == 0 and (out[120:] == 7.0).all() and torch.equal(cache.k, before.k) and torch.equal(cache.v, before.v)
+
+
 @pytest.mark.parametrize("most", [9, 64, 65, 256])
 def test_attend_most_is_a_bound(h, most):
     """A larger `most` than any tree has changes nothing but memory."""
@@ -395,6 +424,20 @@ def test_verify_by_hand(h):
     assert verified(h, [[-1, -1, 0]], i32([0, 1, 1]), u(.1, 0, .2), p, None) == ([0, 2, -1], [2], [1])
     # the same token twice
     assert verified(h, [[-1, 0, 0, 0]], i32([0, 0, 0, 2]), u(.9, .9, .9, .7), rows_of([.5, .2, .3], [1, 0, 0], [1, 0, 0], [0, 0, 1]), rows_of([.9, .05, .05], [1, 0, 0], [1, 0, 0], [1, 0, 0]))
+
+
+@pytest.mark.parametrize("by_draft", [True, False], ids=["drawn", "chosen"])
+def test_verify_entries_that_are_none(h, by_draft):
+    """NaN and negative entries anywhere in both rows count as 0."""
+    gen = torch.Generator(device="cuda").manual_seed(63)
+    trees = [grown(30, 64, 4), grown(12, 65, 3), [-1, 0, 0, 0]]
+    for dtype, vocab in ((F32, 5003), (BF, 1000)):
+        target, draft, ids, u = drawn(gen, trees, vocab, dtype, noise=1.5)
+        for t in (target, draft):
+            strange = torch.rand(t.shape, generator=gen, device="cuda")
+            t[strange < 0.2] = math.nan
+            t[strange > 0.8] *= -1
+        verified(h, trees, ids, u, target, draft if by_draft else None)
 
 
 def test_verify_rows_that_are_not_asked(h):
