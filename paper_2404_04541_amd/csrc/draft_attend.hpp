@@ -294,16 +294,18 @@ struct TreeRows {
   template <int H>
   __device__ __forceinline__ bool weigh(const TreeAttendArgs& a, const TreePages& sp, f32x16 (&x)[2], int k0, bool whole, float ks, float vs, int half, vec8<f16_t> (&p)[4]) {
     const float c = fmaxf(scale2 * ks, 1.17549435e-38f);      // (above 0: what is not seen is -inf times it)
-    float unit2 = c;                                            // of x, in units of log 2
+    // a score, in units of log 2, is zero + unit2 x; with a cap alone x is 1 / (e^2y + 1), of which the tanh is 1 - 2 x, so that a smaller x is a larger score and what is not seen has x = inf
+    constexpr bool kFalls = CAP && !BIAS;
+    constexpr float kUnseen = kFalls ? INFINITY : -INFINITY;
+    const float unit2 = kFalls ? -2.0f * cap2 : BIAS ? 1.0f : c, zero = kFalls ? cap2 : 0.0f;
     if constexpr (CAP || BIAS) {
-      unit2 = BIAS ? 1.0f : cap2;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           float y = x[t][i] * c;
-          if constexpr (CAP) y = tanh_of(y);
-          if constexpr (CAP && BIAS) y *= cap2;
+          if constexpr (kFalls) y = fast_rcp(fast_exp2(y) + 1.0f);
+          else if constexpr (CAP) y = tanh_of(y) * cap2;
           x[t][i] = y;
         }
     }
@@ -333,13 +335,13 @@ struct TreeRows {
             const int between = nodes.above + (b < 32 ? __popc(own_lo & above) + __popc(own_hi) : __popc(own_hi & above));
             x[t][i] -= slope2 * (float)(b < context ? away - b : between);
           }
-          x[t][i] = sees ? x[t][i] : -INFINITY;
+          x[t][i] = sees ? x[t][i] : kUnseen;
         }
     }
-    float top = __builtin_elementwise_maximum(x[0][0], x[1][0]);                  // (NaN where a score is: then nothing else matters of the row)
+    float top = kFalls ? __builtin_elementwise_minimum(x[0][0], x[1][0]) : __builtin_elementwise_maximum(x[0][0], x[1][0]);      // (NaN where a score is: then nothing else matters of the row)
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = max3(top, x[0][i], x[1][i]);
-    top = max_halves(top) * unit2;
+    for (int i = 1; i < 16; ++i) top = kFalls ? min3(top, x[0][i], x[1][i]) : max3(top, x[0][i], x[1][i]);
+    top = max_halves(__builtin_fmaf(top, unit2, zero));
     // The sums go to a new unit only where some row's maximum has grown by more than 2^3, or the page's scale is larger than the unit or much smaller.  Not further down than 2^-64 of the
     // largest scale so far: a page of zeros has the scale 2^-100, next to which sums of large values would overflow.
     const int exponent = uniform((int)(__float_as_uint(vs) >> 23));
@@ -358,7 +360,7 @@ struct TreeRows {
         for (int i = 0; i < 16; ++i) acc[j][i] = __builtin_amdgcn_ldexpf(acc[j][i] * by, shift);
     }
     const int below = max(exponent - unit, -40);                                  // 0 and less; what lies further down only the sum of probabilities shows
-    const float base = (m == -INFINITY ? 0.0f : m) - (float)(kTreeShift + below);
+    const float base = (m == -INFINITY ? 0.0f : m) - (float)(kTreeShift + below) - zero;
     float sum = 0.0f;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
