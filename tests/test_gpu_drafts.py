@@ -82,6 +82,7 @@ CASES = {
     "most": dict(lens=[500, 256, 300], trees=[grown(256, 8, 4), grown(256, 9, 2), grown(200, 10, 30)], heads=(4, 2), d=64),
     "two_blocks": dict(lens=[1000], trees=[grown(12, 11)], heads=(10, 2), d=128),
     "group_of_24": dict(lens=[200, 70], trees=[grown(9, 12), grown(30, 13)], heads=(24, 1), d=72),
+    "group_of_160": dict(lens=[70, 3], trees=[grown(3, 38), [-1, -1]], heads=(160, 1), d=64),
     "wide_roots": dict(lens=[90, 66], trees=[grown(20, 14, 3, 5), grown(33, 15, 8, 33)], heads=(4, 4), d=64),
     "window": dict(lens=[1000, 64, 40, 300], trees=[grown(17, 16, 1), grown(8, 17), grown(30, 18), []], heads=(4, 2), d=64, window=70),
     "window_in_tree": dict(lens=[130, 128, 100], trees=[list(range(-1, 39)), grown(70, 19, 1), grown(20, 20)], heads=(2, 1), d=64, window=3),
