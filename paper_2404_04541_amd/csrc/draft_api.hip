@@ -114,7 +114,7 @@ int spdraft_attend(spgemm_handle h, const spcache* c, int64_t layer, const spgem
     a.window = (int)(window < kMaxTokens ? window : 0);
     a.score = {scale, cap, slopes};
     const int room = room_of(c);
-    a.places = h->num_cus * kTreeResident;
+    a.places = h->num_cus * tree_resident(room);
     // Up to kMostEven sequences every workgroup finds its piece by itself.  Pieces: never more than kMostTurns times the places, or the units and as many pieces more as the places (pages_of_piece);
     // nor more than the units and one for every kLeastPages pages.  Cells are for pieces of cut units alone, at most two for every kLeastPages pages.  Beyond, places of chunks are found by the table's row pointers.
     const int64_t units = n * c->kv_heads * a.tiles, work = table->nnz * c->kv_heads * a.tiles;

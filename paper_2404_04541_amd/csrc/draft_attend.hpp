@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(1024) k_trees_check(TreeView t, const int32_t*
 // ---- attention --------------------------------------------------------------------------------
 
 constexpr int kTreeRows = 128;    // rows of a workgroup, at most: 32 a wave
-constexpr int kTreeResident = 2;  // workgroups of a compute unit (registers)
+constexpr int tree_resident(int room) { return room == 64 ? 3 : 2; }      // workgroups of a compute unit (registers)
 
 struct TreeAttendArgs {
   CacheView c;
@@ -608,7 +608,7 @@ __device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const Tr
 
 // A workgroup has `chunk` pages of a sequence, a key head and up to 128 rows.  The second product is in float16 whatever the type: e4m3 values are exact in it, and probabilities keep 11 digits instead of bfloat16's 8.
 template <typename T, int R, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(256, kTreeResident) k_tree_attend(TreeAttendArgs a) {
+__global__ void __launch_bounds__(256, tree_resident(R)) k_tree_attend(TreeAttendArgs a) {
   constexpr int kSteps = R / 16, kBlocks = R / 32;
   const int lane = lane_id(), half = lane >> 5, col = lane & 31, wave = uniform(threadIdx.x / kWave);
   TreePlace at;
