@@ -222,13 +222,13 @@ class PagedCache:
 
     def __init__(self, head_dim: int, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
         room = 64 if head_dim <= 64 else 128
-        if k.dim() != 5 or tuple(k.shape[3:]) != (PAGE, room) or tuple(v.shape) != (*k.shape[:3], room, PAGE):
+        shape = k.shape
+        if len(shape) != 5 or shape[3:] != (PAGE, room) or v.shape != (*shape[:3], room, PAGE):
             raise ValueError("cache: keys are [layers, pages, kv_heads, 64, room], values [layers, pages, kv_heads, room, 64]")
-        for t in (k_scale, v_scale):
-            if tuple(t.shape) != tuple(k.shape[:3]):
-                raise ValueError("cache: scales are [layers, pages, kv_heads]")
+        if k_scale.shape != shape[:3] or v_scale.shape != shape[:3]:
+            raise ValueError("cache: scales are [layers, pages, kv_heads]")
         self.head_dim, self.k, self.v, self.k_scale, self.v_scale = int(head_dim), k, v, k_scale, v_scale
-        self.layers, self.pages, self.kv_heads = (int(x) for x in k.shape[:3])
+        self.layers, self.pages, self.kv_heads = shape[:3]
         self._struct = CacheStruct(self.layers, self.pages, self.kv_heads, self.head_dim, _array(k, "cache keys", torch.uint8), _array(v, "cache values", torch.uint8),
                                    _array(k_scale, "cache scales", torch.float32), _array(v_scale, "cache scales", torch.float32))
 
@@ -270,7 +270,8 @@ def read(handle: sg.Handle, cache: PagedCache, layer: int, table: PageTable, len
     if tokens < 0:
         raise ValueError("tokens: a negative number")
     rows = _array(ptr, "ptr", torch.int64, table.rows + 1)
-    k, v = _results(handle, lambda: tuple(torch.empty((int(tokens), cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.k.device) for _ in range(2)))
+    k = _results(handle, lambda: cache.k.new_empty((int(tokens), cache.kv_heads, cache.head_dim), dtype=dtype))
+    v = _results(handle, lambda: torch.empty_like(k))
     handle._check(lib.spcache_read(handle.ptr, C.byref(cache._struct), int(layer), C.byref(table.struct(cache)), _array(lens, "lens", torch.int32, table.rows), rows,
                                    int(tokens), _dtype(k), _result(k), _result(v)))
     return k, v

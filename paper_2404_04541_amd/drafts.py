@@ -65,7 +65,7 @@ def symbolic(handle: sg.Handle, ptr: torch.Tensor, parent: torch.Tensor, most: i
     lib = _lib()
     if ptr.numel() < 1:
         raise ValueError("ptr: rows + 1 elements are wanted")
-    t = TreesStruct(ptr.numel() - 1, parent.numel(), _array(ptr, "ptr", torch.int64, ptr), _array(parent, "parent", torch.int32, ptr), int(most))
+    t = TreesStruct(ptr.numel() - 1, parent.numel(), at._array(ptr, "ptr", torch.int64), _array(parent, "parent", torch.int32, ptr), int(most))
     nbytes = max(lib.spdraft_plan_bytes(C.byref(t)), 1)
     memory = at._results(handle, lambda: ptr.new_empty(nbytes, dtype=torch.uint8))
     handle._check(lib.spdraft_symbolic(handle.ptr, C.byref(t), memory.data_ptr(), nbytes, C.byref(C.c_int32(0)) if check else None))
@@ -76,7 +76,9 @@ def symbolic(handle: sg.Handle, ptr: torch.Tensor, parent: torch.Tensor, most: i
 def _array(t: torch.Tensor, name: str, dtype: torch.dtype, like: torch.Tensor, n: Optional[int] = None) -> Optional[int]:
     if t.device != like.device:
         raise ValueError(f"{name}: on {t.device}, not on {like.device}")
-    return at._array(t, name, dtype, n)
+    if t.dtype is not dtype or not t.is_contiguous() or (n is not None and t.numel() != n):
+        return at._array(t, name, dtype, n)      # (which says what is wrong)
+    return t.data_ptr() or None
 
 
 def attend(handle: sg.Handle, cache: at.PagedCache, layer: int, table: at.PageTable, lens: torch.Tensor, trees: Trees, q, scale: Optional[float] = None, cap: float = 0.0,
