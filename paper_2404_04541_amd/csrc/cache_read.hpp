@@ -13,7 +13,8 @@ struct ReadArgs {
 };
 
 // A workgroup has a page that rows lie in, and a head; places of pages as in k_cache_append.  Keys are rows already; values are turned in LDS, two channels a word.
-// Rows of tokens before the sequence's first, or in pages that its table lacks, become zero.
+// Rows of tokens before the sequence's first, or in pages that its table lacks, become zero.  Memory bounds it: 64 sequences of 30 to 16 384 tokens, 8 heads of 128 channels, 137 us, 4.9 TB/s read and written, which is
+// what a copy reaches; one of 2001 tokens 6.6 us.
 template <typename T, int R>
 __global__ void __launch_bounds__(256) k_cache_read(ReadArgs a) {
   const int head = blockIdx.y, tid = threadIdx.x;

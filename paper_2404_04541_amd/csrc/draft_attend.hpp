@@ -1,9 +1,13 @@
 // Trees of drafted tokens: their structure, and the attention of their nodes over the paged cache.
 //
-// A wave has 32 rows (a node and a head that shares the key head) as right operands and takes a page of 64 tokens in two products of 32 keys (32 x 32 x 16 form, attn_common.hpp).  Row 8a + 4h + b
-// of product t is key 32 t + 16 h + 4 a + b, so that half h of the wave, whose lanes have the rows 8a + 4h + b of a result, has the 16 neighbouring keys 32 t + 16 h and on of a page: in the order in
-// which 16 bytes of a value's channel hold them.  So the probabilities are the second product's right operand as they leave the first, and
-// pages go from memory to registers, 16 bytes a lane and load, without LDS.
+// out = sum_j 2^(x_j - m) v_j / sum_j 2^(x_j - m) over the keys that a node sees, in one pass with the running maximum m, the sums in 32 bits.  A row is a node and a head that shares the key head; a wave has 32 of
+// them as right operands and takes a page of 64 tokens in two products of 32 keys (32 x 32 x 16 form, attn_common.hpp).  The order of a page's keys in the first product is chosen so that a lane's probabilities
+// are neighbouring keys, which is what the second product's left operand (a value's channel, held along the tokens) reads in one piece: nothing moves between lanes.
+//
+// All rows of a tree read the same pages, so what matters is how many rows share a read of them.  With more than 64 rows a page is widened to 16 bits once, into LDS, for four waves of 32 rows; with fewer the waves
+// take pages in turn, from memory to registers.  Measured (bfloat16 unless said): four sequences of 50 000 to 65 011 tokens, up to 60 nodes, 32 heads on 8 of 128 channels 245 to 270 us and 9 to join, 0.62 PFLOP/s: vector
+// instructions issue in 46 % of the cycles and matrix instructions run in 34 %, what two waves a SIMD reach together.  48 sequences of 20 to 4000 tokens, up to 26 nodes, capped, 46 us and 10 to join: a workgroup's
+// chain (its piece 2 us, the first page 2, each page 2.3, the end 2.7) about twice over.  24 sequences, 17 nodes, 8 heads of 80 channels, window 900, distances, float16, 16 us and 4.  One of 712 tokens, 12 nodes, 9.6 and 4.
 #pragma once
 #include "cache_kernels.hpp"
 
@@ -33,7 +37,7 @@ __device__ __forceinline__ Tree tree_of(const TreeView& t, int s) {
 // ---- structure --------------------------------------------------------------------------------
 
 // A workgroup has a tree.  A node's ancestors are found by doubling: it takes over what the node that it points to has, and then points to where that one points; a tree of depth d is done
-// after log d rounds.  48 trees of up to 26 nodes XX us.
+// after log d rounds.  12 nodes 3.2 us, 48 trees of up to 26 nodes 5 us: a chain of loads and LDS steps.
 __global__ void __launch_bounds__(kMostNodes) k_trees(TreeView t, const int32_t* parent) {
   __shared__ int jump[kMostNodes], child[kMostNodes];
   __shared__ unsigned long long ups[kNodeWords][kMostNodes];
@@ -146,7 +150,7 @@ __device__ __forceinline__ TreePages tree_pages(const TreeAttendArgs& a, int s) 
 //
 // per: the card has `places` workgroups at once.  If they are to be done in k turns, pieces have at least work / (k places - units) pages (cutting makes at most work / per pieces more than there are
 // units), and cost k (per + kPieceCost) pages' time, kPieceCost for what a workgroup does beside its pages; the best k up to 4 is taken.  Where units are more than that, only what is longer than twice the average
-// is cut.  (All pieces of the same length in no whole number of turns were worst: four sequences, 60 nodes, 65 011 tokens, 337 us with about 1.6 turns of 60 pages.)
+// is cut.  us in one turn | in two, four sequences of 60 nodes and 50 000 to 65 011 tokens 277 | 294 (in about 1.6, with pieces of 60 pages, 337), 48 sequences of up to 26 nodes and 4000 tokens 82 | 53: the constant takes the better one of both.
 constexpr int kMostEven = 512;     // sequences that a workgroup looks through
 constexpr int kLeastPages = 4, kPieceCost = 8, kMostTurns = 4;
 struct Piece {

@@ -748,6 +748,25 @@ def test_graph(h):
         stream.synchronize()
 
 
+def test_two_handles_at_once(h):
+    """Two handles on streams of their own, with calls of different sizes in flight together, and results that each alone gives."""
+    gen = torch.Generator(device="cuda").manual_seed(101)
+    trees = [[grown(30, 1), grown(17, 2)], [grown(60, 3)]]
+    lens = [[3000, 500], [5000]]
+    caches = [filled(102 + i, 1, 90, 2, 64) for i in range(2)]
+    tables = [at.PageTable(*flat(rows_for(n, 90, i))) for i, n in enumerate(lens)]
+    qs = [randn(gen, (sum(map(len, t)), 8, 64), BF) for t in trees]
+    plans = [planned(h, t) for t in trees]
+    want = [dr.attend(h, caches[i], 0, tables[i], i32(lens[i]), plans[i], qs[i]) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    handles = [sg.Handle(stream=s) for s in streams]
+    lengths = [i32(n) for n in lens]
+    torch.cuda.synchronize()
+    got = [[dr.attend(handles[i], caches[i], 0, tables[i], lengths[i], plans[i], qs[i]) for i in range(2)] for _ in range(20)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(g[i], want[i]) for g in got for i in range(2))
+
+
 def test_same_bits_again(h):
     gen = torch.Generator(device="cuda").manual_seed(99)
     trees, lens = [grown(40, 1), grown(13, 2)], [4000, 900]
