@@ -5,7 +5,7 @@
 // not taken costs a pass over both rows, in which wave w has the w-th part: the sums of these parts are what the token is looked for in, if no other child is taken.  Children that were chosen, not drawn, cost
 // one pass together.
 //
-// Measured: 64 trees of up to 26 nodes, rows of 131 072 in 32 bits, 62 us and 5 for the walk: the nodes with most refusals, some 10 us a pass (a compute unit's memory and 64-bit instructions about alike), while
+// Measured: 64 trees of up to 26 nodes, rows of 131 072 in 32 bits, 61 us and 5 for the walk: the nodes with most refusals, some 10 us a pass (a compute unit's memory and 64-bit instructions about alike), while
 // others are done.  16 trees of up to 40 nodes, chosen children, rows of 100 003 in bfloat16, 20 us; a chain of 8, rows of 32 003, 13 us: dependent loads and one pass.
 #pragma once
 #include "draft_attend.hpp"
@@ -25,8 +25,10 @@ struct VerifyArgs {
   int32_t *path, *kept, *next;
 };
 
-// An entry of a row: what is negative or NaN counts as 0 (of three numbers one of which is NaN the instruction gives the smallest).
-template <typename T> __device__ __forceinline__ float proper(T v) { return __builtin_amdgcn_fmed3f((float)v, 0.0f, INFINITY); }
+// An entry of a row: what is negative or NaN counts as 0 (a maximum of NaN and 0 is 0).  In the loops that is taken in 64 bits, where it is one instruction; in 32 bits a second one first
+// quiets NaN (64 trees over 131 072 tokens 62.5 -> 60.8 us).
+template <typename T> __device__ __forceinline__ float proper(T v) { return fmaxf((float)v, 0.0f); }
+__device__ __forceinline__ double proper64(float v) { return fmax((double)v, 0.0); }
 
 template <typename T>
 struct Loaded {            // 16 bytes of a row, which may begin at any element
@@ -81,7 +83,7 @@ __device__ __forceinline__ bool first_taken(const VerifyArgs& a, int64_t parent,
 
 // The sum of f(token, entry of p, entry of q) over a part of the rows, by one wave.  Tokens of children are left out: where a batch of tokens may hold one (a bit of `marks` for every
 // batch, of 64 in turn) each is compared.  The loads of two batches are on their way while two others are
-// used (of four and four, of six and six: 68 | 69 and 90 us for 64 trees over 131 072 tokens).  With DRAFT p's entries come as they are: what is made of them is a maximum with 0.
+// used (of four and four, of six and six: 68 | 69 and 90 us for 64 trees over 131 072 tokens).  Entries come as they are.
 constexpr int kInFlight = 2;
 template <typename T, bool DRAFT, typename F>
 __device__ __forceinline__ void walk_tokens(const T* p, const T* q, int vocab, int from, int to, unsigned long long marks, const int* children, int count, F each) {
@@ -95,10 +97,10 @@ __device__ __forceinline__ void walk_tokens(const T* p, const T* q, int vocab, i
         out |= at >= 0 && at < kCount ? 1u << at : 0u;
       }
 #pragma unroll
-      for (int i = 0; i < kCount; ++i) each(v0 + i, out >> i & 1 ? 0.0f : DRAFT ? (float)r.v[i] : proper(r.v[i]), DRAFT && !(out >> i & 1) ? proper(s.v[i]) : 0.0f);
+      for (int i = 0; i < kCount; ++i) each(v0 + i, out >> i & 1 ? 0.0f : (float)r.v[i], DRAFT && !(out >> i & 1) ? (float)s.v[i] : 0.0f);
     } else {
 #pragma unroll
-      for (int i = 0; i < kCount; ++i) each(v0 + i, DRAFT ? (float)r.v[i] : proper(r.v[i]), DRAFT ? proper(s.v[i]) : 0.0f);
+      for (int i = 0; i < kCount; ++i) each(v0 + i, (float)r.v[i], DRAFT ? (float)s.v[i] : 0.0f);
     }
   };
   Loaded<T> r[2][kInFlight], s[2][kInFlight];
@@ -237,14 +239,15 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
     by = times;
     if (DRAFT && first)
       walk_tokens<T, DRAFT>(p, q, a.vocab, from, to, marks, kids.token, count, [&](int, float r0, float q0) {
-        sum += fmax(__builtin_fma(-by, (double)q0, (double)r0), 0.0);
-        other += (double)q0;
+        const double qv = proper64(q0);
+        sum += fmax(__builtin_fma(-by, qv, (double)r0), 0.0);
+        other += qv;
       });
     else if (DRAFT && by != 0.0)
       walk_tokens<T, DRAFT>(p, q, a.vocab, from, to, marks, kids.token, count,
-                            [&](int, float r0, float q0) { sum += fmax(__builtin_fma(-by, (double)q0, (double)r0), 0.0); });
+                            [&](int, float r0, float q0) { sum += fmax(__builtin_fma(-by, proper64(q0), (double)r0), 0.0); });
     else                                 // (the draft's row of a node without children may hold anything)
-      walk_tokens<T, false>(p, q, a.vocab, from, to, marks, kids.token, count, [&](int, float r0, float) { sum += (double)r0; });
+      walk_tokens<T, false>(p, q, a.vocab, from, to, marks, kids.token, count, [&](int, float r0, float) { sum += proper64(r0); });
     sum = wave_sum(sum);
     if (first) other = wave_sum(other);
     __syncthreads();                     // (whoever read the parts before is done)
@@ -339,8 +342,8 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
   const double goal = (double)a.u[tree.first] * total(0);
   auto weights_of = [&](int b, int e, auto f) {
     if (DRAFT && by != 0.0)
-      walk_tokens<T, DRAFT>(p, q, a.vocab, b, e, marks, kids.token, count, [&](int v, float r0, float q0) { f(v, unit * fmax(__builtin_fma(-by, (double)q0, (double)r0), 0.0)); });
-    else walk_tokens<T, false>(p, q, a.vocab, b, e, marks, kids.token, count, [&](int v, float r0, float) { f(v, unit * (double)r0); });
+      walk_tokens<T, DRAFT>(p, q, a.vocab, b, e, marks, kids.token, count, [&](int v, float r0, float q0) { f(v, unit * fmax(__builtin_fma(-by, proper64(q0), (double)r0), 0.0)); });
+    else walk_tokens<T, false>(p, q, a.vocab, b, e, marks, kids.token, count, [&](int v, float r0, float) { f(v, unit * proper64(r0)); });
   };
   // The part in which the running sum passes the goal, the share of it, and the token: where rounding lets none pass, the last that is above 0.
   int begin = 0, size = part;
