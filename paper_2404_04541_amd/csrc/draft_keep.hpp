@@ -104,7 +104,8 @@ __global__ void __launch_bounds__(256) k_draft_keep(KeepArgs a) {
     }
     const bool grows = now > old;
     if (grows && lane == 0) scale[mine] = now;
-    auto by_of = [&](int from) { return from / kPage == place ? old / now : scale[cell(from / kPage)] / now; };
+    // (A code that is not 0 has made the page's scale grow; zeros of a page of large scale have not, and infinity times 0 would be NaN.)
+    auto by_of = [&](int from) { return from / kPage == place ? old / now : fminf(scale[cell(from / kPage)] / now, 0x1p126f); };
     unsigned char* const to = data + mine * (kPage * R);
     if (!values) {
       // 16 tokens on their way together; a token is R / 4 words

@@ -1,0 +1,47 @@
+"""Drafted tokens at the ends of the ranges."""
+import pytest
+import torch
+
+from attn_helpers import HostCache, flat
+from draft_helpers import keep_reference
+from paper_2404_04541_amd import attention as at
+from paper_2404_04541_amd import binding as sg
+from paper_2404_04541_amd import drafts as dr
+from test_gpu_drafts import i32, planned
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def h():
+    return sg.Handle()
+
+
+def kept_as_by_hand(h, cache, rows, ctx, parent, path):
+    host = HostCache(cache, 0)
+    keep_reference(host, rows[0], ctx, path)
+    new = dr.keep(h, cache, at.PageTable(*flat(rows)), i32([ctx + len(parent)]), planned(h, [parent]), i32(path + [-1] * (len(parent) - len(path))), i32([len(path)]))
+    now = HostCache(cache, 0)
+    assert new.tolist() == [ctx + len(path)]
+    for x in (0, 1):
+        assert torch.equal(now.scale[x], host.scale[x])
+        assert torch.equal(now.code[x][..., :host.d].nan_to_num(1e9), host.code[x][..., :host.d].nan_to_num(1e9))
+    return now
+
+
+@pytest.mark.parametrize("exponent", [20, 27, 28, 30, 120])
+@pytest.mark.parametrize("d", [8, 64, 128])
+def test_keep_zeros_of_a_large_page_into_an_empty_one(h, exponent, d):
+    """A token of zeros on a page of the scale 2^exponent comes to one that holds nothing but zeros so far, of the scale 2^-100: zeros it stays, and NaN in it NaN."""
+    cache = at.PagedCache.empty(1, 4, 1, d)
+    cache.k_scale[0, 1], cache.v_scale[0, 1] = 2.0 ** -100, 2.0 ** -100
+    cache.k_scale[0, 2], cache.v_scale[0, 2] = 2.0 ** exponent, 2.0 ** exponent
+    cache.k[0, 2], cache.v[0, 2] = 0x38, 0x38                           # 1: refused
+    cache.k[0, 2, 0, 5], cache.v[0, 2, 0, :, 5] = 0x00, 0x00            # zeros: taken
+    cache.k[0, 2, 0, 6], cache.v[0, 2, 0, :, 6] = 0x80, 0x80            # ... and those below 0
+    cache.k[0, 2, 0, 6, 3], cache.v[0, 2, 0, 3, 6] = 0x7F, 0xFF
+    parent = list(range(-1, 8)) + [2, 9]                                # nodes at 60 .. 70: 4 .. 10 lie in the second page
+    now = kept_as_by_hand(h, cache, [[1, 2]], 60, parent, [0, 1, 9, 10])
+    for x in (0, 1):
+        token = now.code[x][1, 0, 63, :d]
+        assert token[3].isnan() and (token.nan_to_num(0) == 0).all() and (now.code[x][1, 0, :63] == 0).all() and now.scale[x][1, 0] == 2.0 ** -100
