@@ -78,9 +78,9 @@ __global__ void __launch_bounds__(256) k_draft_keep(KeepArgs a) {
     const float old = scale[mine];
     float now = old;
     if (source(until - 1) / kPage != place) {
-      // what comes from other pages: its largest magnitude
+      // what comes from other pages: its largest magnitude (2^-9 times it, for 256 times the largest scale is 2^128; the smallest code times the smallest scale is 2^-109)
       float top = 0.0f;
-      auto measure = [&](float code, float by) { const float v = fabsf(code) * by; top = v < INFINITY ? fmaxf(top, v) : top; };
+      auto measure = [&](float code, float by) { const float v = fabsf(code) * (by * 0x1p-9f); top = v < INFINITY ? fmaxf(top, v) : top; };
       for (int o = begin; o < until; ++o) {
         const int from = uniform(source(o));
         if (from / kPage == place) continue;
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(256) k_draft_keep(KeepArgs a) {
       }
 #pragma unroll
       for (int d = 1; d < kWave; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-      now = fmaxf(old, scale_for(top));
+      now = fmaxf(old, scale_for(top * 0x1p9f));      // (of infinity the largest scale)
     }
     const bool grows = now > old;
     if (grows && lane == 0) scale[mine] = now;

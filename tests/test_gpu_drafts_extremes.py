@@ -7,9 +7,10 @@ from draft_helpers import keep_reference
 from paper_2404_04541_amd import attention as at
 from paper_2404_04541_amd import binding as sg
 from paper_2404_04541_amd import drafts as dr
-from test_gpu_drafts import i32, planned
+from test_gpu_drafts import i32, i64, planned, randn
 
 pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
 
 
 @pytest.fixture(scope="module")
@@ -45,3 +46,21 @@ def test_keep_zeros_of_a_large_page_into_an_empty_one(h, exponent, d):
     for x in (0, 1):
         token = now.code[x][1, 0, 63, :d]
         assert token[3].isnan() and (token.nan_to_num(0) == 0).all() and (now.code[x][1, 0, :63] == 0).all() and now.scale[x][1, 0] == 2.0 ** -100
+
+
+@pytest.mark.parametrize("d", [8, 64, 128])
+def test_keep_the_largest_values(h, d):
+    """What bfloat16's largest value becomes in 8 bits, 256 times 2^120, is more than 32 bits hold as a number; it moves to a page of small values all the same, whose scale grows for it."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    cache, rows = at.PagedCache.empty(1, 4, 1, d), [[1, 2]]
+    k, v = randn(gen, (70, 1, d), BF), randn(gen, (70, 1, d), BF)
+    k[66], v[66] = torch.finfo(BF).max, -torch.finfo(BF).max
+    at.append(h, cache, 0, at.PageTable(*flat(rows)), i32([70]), i64([0, 70]), k, v)
+    assert cache.k_scale[0, 2, 0] == 2.0 ** 120
+    parent = list(range(-1, 8)) + [0]
+    parent[6] = 1
+    now = kept_as_by_hand(h, cache, rows, 60, parent, [0, 1, 6])
+    for x, sign in ((0, 1), (1, -1)):
+        assert now.scale[x][1, 0] == 2.0 ** 120 and (now.code[x][1, 0, 62, :d] == sign * 256).all()
+    cache.k[0, 2, 0, 4], cache.v[0, 2, 0, :, 4] = 0x7E, 0xFE            # 448 times 2^120
+    kept_as_by_hand(h, cache, [[3, 2]], 60, parent, [0, 6, 8])
