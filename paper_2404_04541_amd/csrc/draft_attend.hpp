@@ -292,11 +292,11 @@ struct TreeRows {
   }
 
   // From the products q.k of a page's keys to its probabilities.  x[t][i] is key H half + 32 t + i (H 16) or 32 t + 16 (i / 8) + i % 8 (H 8) of the page; p[2 t + i / 8][i % 8] becomes its probability, as an
-  // operand; false where the page's values are too small for them to show.
+  // operand, 0 where the page's values are too small for them to show: the product is made all the same, so that a value that is NaN reaches the rows.
   template <int H>
   static __device__ __forceinline__ constexpr int key(int t, int i) { return H == 16 ? 32 * t + i : 32 * t + 16 * (i / 8) + i % 8; }
   template <int H>
-  __device__ __forceinline__ bool weigh(const TreeAttendArgs& a, const TreePages& sp, f32x16 (&x)[2], int k0, bool whole, float ks, float vs, int half, vec8<f16_t> (&p)[4]) {
+  __device__ __forceinline__ void weigh(const TreeAttendArgs& a, const TreePages& sp, f32x16 (&x)[2], int k0, bool whole, float ks, float vs, int half, vec8<f16_t> (&p)[4]) {
     const float c = fmaxf(scale2 * ks, 1.17549435e-38f);      // (above 0: what is not seen is -inf times it)
     // a score, in units of log 2, is zero + unit2 x; with a cap alone x is 1 / (e^2y + 1), of which the tanh is 1 - 2 x, so that a smaller x is a larger score and what is not seen has x = inf
     constexpr bool kFalls = CAP && !BIAS;
@@ -375,7 +375,9 @@ struct TreeRows {
         p[2 * t + i / 8][i % 8] = (f16_t)e;
       }
     l += __builtin_amdgcn_ldexpf(sum, -kTreeShift - below);
-    return exponent - unit == below;
+    if (exponent - unit != below)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = vec8<f16_t>{};
   }
 };
 
@@ -482,7 +484,7 @@ __device__ __forceinline__ bool tree_few_rows(const TreeAttendArgs& a, const Tre
       const int k0 = n * kPage;
       const bool whole = k0 + kPage <= sp.ctx && k0 >= last_lo;
       vec8<f16_t> p[4];
-      const bool shows = rows.template weigh<16>(a, sp, x, k0, whole, ks, vs, half, p);
+      rows.template weigh<16>(a, sp, x, k0, whole, ks, vs, half, p);
       if (!whole) {
         const unsigned long long live = seen_context(sp.len - k0, sp.lo - k0) >> in_loop(16 * half);
 #pragma unroll
@@ -494,11 +496,10 @@ __device__ __forceinline__ bool tree_few_rows(const TreeAttendArgs& a, const Tre
             for (int j = 0; j < kBlocks; ++j) vw[j][t][w] = proper_bytes(vw[j][t][w] & bytes, strange);
           }
       }
-      if (shows)
 #pragma unroll
-        for (int j = 0; j < kBlocks; ++j)
+      for (int j = 0; j < kBlocks; ++j)
 #pragma unroll
-          for (int u = 0; u < 4; ++u) rows.acc[j] = mma(widen(u32x2{vw[j][u / 2][2 * (u % 2)], vw[j][u / 2][2 * (u % 2) + 1]}, f16_t()), p[u], rows.acc[j]);
+        for (int u = 0; u < 4; ++u) rows.acc[j] = mma(widen(u32x2{vw[j][u / 2][2 * (u % 2)], vw[j][u / 2][2 * (u % 2) + 1]}, f16_t()), p[u], rows.acc[j]);
       if (next_page >= 0) load_v(next_page);
     } else if (next_page >= 0) {
       scales.load(a, next_page, at.kv);
@@ -596,13 +597,12 @@ __device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const Tr
       __builtin_amdgcn_s_setprio(0);
       const bool whole = whole_page(n);
       vec8<f16_t> p[4];
-      const bool shows = rows.template weigh<8>(a, sp, x, n * kPage, whole, ks, vs, half, p);
+      rows.template weigh<8>(a, sp, x, n * kPage, whole, ks, vs, half, p);
       __builtin_amdgcn_s_setprio(1);
-      if (shows)
 #pragma unroll
-        for (int j = 0; j < kBlocks; ++j)
+      for (int j = 0; j < kBlocks; ++j)
 #pragma unroll
-          for (int u = 0; u < 4; ++u) rows.acc[j] = mma(SV::template row<f16_t>(vt, v_base, 32 * j, u), p[u], rows.acc[j]);
+        for (int u = 0; u < 4; ++u) rows.acc[j] = mma(SV::template row<f16_t>(vt, v_base, 32 * j, u), p[u], rows.acc[j]);
     }
     __builtin_amdgcn_s_setprio(0);
     if (next >= 0) {

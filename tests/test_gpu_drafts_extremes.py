@@ -1,13 +1,15 @@
 """Drafted tokens at the ends of the ranges."""
+import math
+
 import pytest
 import torch
 
-from attn_helpers import HostCache, flat
-from draft_helpers import keep_reference
+from attn_helpers import PAGE, HostCache, check, flat
+from draft_helpers import keep_reference, tree_reference
 from paper_2404_04541_amd import attention as at
 from paper_2404_04541_amd import binding as sg
 from paper_2404_04541_amd import drafts as dr
-from test_gpu_drafts import i32, i64, planned, randn
+from test_gpu_drafts import grown, i32, i64, planned, randn, rows_for
 
 pytestmark = pytest.mark.gpu
 BF = torch.bfloat16
@@ -64,3 +66,39 @@ def test_keep_the_largest_values(h, d):
         assert now.scale[x][1, 0] == 2.0 ** 120 and (now.code[x][1, 0, 62, :d] == sign * 256).all()
     cache.k[0, 2, 0, 4], cache.v[0, 2, 0, :, 4] = 0x7E, 0xFE            # 448 times 2^120
     kept_as_by_hand(h, cache, [[3, 2]], 60, parent, [0, 6, 8])
+
+
+@pytest.mark.parametrize("nodes", [12, 40], ids=["few_rows", "many_rows"])
+@pytest.mark.parametrize("first", [0, 4], ids=["large_first", "zeros_first"])
+@pytest.mark.parametrize("where", ["context", "tree"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_feels_nan_on_a_page_of_next_to_no_scale(h, nodes, first, where, d):
+    """Pages that hold zeros and a value that is NaN have the scale 2^-100: next to pages of large values nothing else shows of them, but NaN does, to every node that sees it and in its channel.  (Among so many
+    sequences a workgroup has eight pages.)"""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    pages, seqs, mine = 16, 520, 300
+    tokens = pages * PAGE + (nodes - PAGE if where == "tree" else 20)
+    lens, trees = [0] * seqs, [[]] * seqs
+    lens[mine], trees[mine] = tokens, grown(nodes, 5, 2)
+    cache, rows = at.PagedCache.empty(1, pages + 1, 2, d), rows_for(lens, pages + 1, 4)
+    table, plan = at.PageTable(*flat(rows)), planned(h, trees)
+    k, v = randn(gen, (tokens, 2, d), BF), torch.zeros((tokens, 2, d), device="cuda")
+    page = torch.arange(tokens, device="cuda") // PAGE
+    large = (page + first) % 8 < 4 if where == "context" else page < pages - 1
+    v[large] = (torch.rand((int(large.sum()), 2, d), generator=gen, device="cuda") + 0.5) * 2.0 ** 20
+    at.append(h, cache, 0, table, i32(lens), i64([0] * (mine + 1) + [tokens] * (seqs - mine)), k, v.to(BF))
+    q = randn(gen, (nodes, 8, d), BF)
+    attend = lambda: dr.attend(h, cache, 0, table, i32(lens), plan, q)  # noqa: E731
+    clean = attend()
+    check("clean", clean, *tree_reference(HostCache(cache, 0), rows, lens, trees, q, 1 / math.sqrt(d)))
+    # NaN in channel 3 of key head 0: in each of the pages of zeros, or in the tree's root
+    zeros = [x * PAGE + 7 for x in range(pages) if not large[x * PAGE]]
+    for token in [tokens - nodes] if where == "tree" else zeros:
+        at_page = rows[mine][token // PAGE]
+        assert cache.v_scale[0, at_page, 0] == 2.0 ** -100
+        cache.v[0, at_page, 0, 3, token % PAGE] = 0x7F
+        o = attend()
+        assert o[:, :4, 3].isnan().all(), token
+        o[:, :4, 3] = clean[:, :4, 3]
+        assert torch.equal(o, clean)
+        cache.v[0, at_page, 0, 3, token % PAGE] = 0
