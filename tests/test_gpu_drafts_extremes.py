@@ -1,4 +1,5 @@
 """Drafted tokens at the ends of the ranges."""
+import ctypes as C
 import math
 
 import pytest
@@ -9,7 +10,7 @@ from draft_helpers import keep_reference, tree_reference
 from paper_2404_04541_amd import attention as at
 from paper_2404_04541_amd import binding as sg
 from paper_2404_04541_amd import drafts as dr
-from test_gpu_drafts import grown, i32, i64, planned, randn, rows_for
+from test_gpu_drafts import filled, grown, i32, i64, planned, randn, rows_for
 
 pytestmark = pytest.mark.gpu
 BF = torch.bfloat16
@@ -102,3 +103,24 @@ def test_attend_feels_nan_on_a_page_of_next_to_no_scale(h, nodes, first, where, 
         o[:, :4, 3] = clean[:, :4, 3]
         assert torch.equal(o, clean)
         cache.v[0, at_page, 0, 3, token % PAGE] = 0
+
+
+def test_attend_rows_that_overlap_and_have_more_pieces_than_the_launch(h):
+    """A table of 1000 entries whose row pointers go back and forth, so that the rows have 256 times as many pages: what that gives is not said, but the call ends, whatever its memory holds
+    of sequences that no workgroup came to, and writes its output alone."""
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    own = sg.Handle()
+    cache = filled(14, 1, 50, 1, 64)
+    before = cache.k.clone(), cache.v.clone()
+    plan, lens = planned(own, [[-1]] * 512), i32([64000] * 512)
+    table = at.PageTable(i64([0, 1000] * 256 + [0]), i32([i % 50 for i in range(1000)]))
+    q = randn(gen, (512, 1, 64), BF)
+    out = torch.full((520, 1, 64), 7.0, dtype=BF, device="cuda")
+    for pattern in ([0, 0, 2 ** 31 - 1, 1], [0, 1, 2 ** 31 - 1, 1], [2 ** 31 - 1] * 4, [-1, 0, -1, 0], [-2 ** 31, 1, 2 ** 31 - 1, 1]):
+        for memory in own._live.values():                            # (of the first call: none)
+            words = memory[:memory.numel() // 16 * 16].view(torch.int32).view(-1, 4)
+            words.copy_(i32(pattern).expand_as(words))
+        rc = dr._lib().spdraft_attend(own.ptr, C.byref(cache._struct), 0, C.byref(table.struct(cache)), lens.data_ptr(), C.byref(plan._struct), plan.memory.data_ptr(), 1, at.BF16, 0.125, 0.0, None, 0,
+                                      at._tensor(q, "q"), at.TensorStruct(out.data_ptr(), 64, 64))
+        torch.cuda.synchronize()
+        assert rc == 0 and (out[512:] == 7.0).all() and torch.equal(cache.k, before[0]) and torch.equal(cache.v, before[1])
