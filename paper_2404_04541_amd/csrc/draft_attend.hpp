@@ -771,7 +771,7 @@ __global__ void __launch_bounds__(256) k_tree_join(TreeAttendArgs a) {
   if (sp.first < sp.last) {
     if (a.chunk == 0) {
       const Cut cut = load_uniform(a.cuts + place.z);
-      pieces = (int)min((int64_t)cut.z, a.cells);      // (no unit has more; of rows whose pointers do not ascend the launch may not have come to write this)
+      pieces = cut.z == 1 ? 1 : (int)min((int64_t)cut.z, a.cells);      // (no cut unit has more; of rows whose pointers do not ascend the launch may not have come to write this)
       tiles = cut.w;
       cell0 = cut.x;
       stride = cut.y;
