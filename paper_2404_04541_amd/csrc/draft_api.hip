@@ -1,8 +1,6 @@
 // C ABI of drafted tokens over the paged cache (see include/spdraft.h): argument checks, scratch memory, launches.  All device work is in the draft_ headers beside this file.
 #include "../../include/spdraft.h"
 
-#include <algorithm>
-
 #include "attn_host.hpp"
 #include "draft_attend.hpp"
 #include "draft_keep.hpp"
@@ -115,15 +113,13 @@ int spdraft_attend(spgemm_handle h, const spcache* c, int64_t layer, const spgem
     a.score = {scale, cap, slopes};
     const int room = room_of(c);
     a.places = h->num_cus * tree_resident(room);
-    // Up to kMostEven sequences every workgroup finds its piece by itself.  Pieces: never more than kMostTurns times the places, or the units and as many pieces more as the places (pages_of_piece);
-    // nor more than the units and one for every kLeastPages pages.  Cells are for pieces of cut units alone, at most two for every kLeastPages pages.  Beyond, places of chunks are found by the table's row pointers.
+    // Up to kMostEven sequences every workgroup finds its piece by itself; beyond, places of chunks are found by the table's row pointers.
     const int64_t units = n * c->kv_heads * a.tiles, work = table->nnz * c->kv_heads * a.tiles;
     int64_t pieces, cells;
     if (n <= kMostEven) {
       a.chunk = 0;
-      const int64_t most = std::max<int64_t>((int64_t)kMostTurns * a.places, units + a.places);
-      pieces = std::min(most, units + work / kLeastPages);
-      cells = std::min((int64_t)kMostTurns * a.places, 2 * (work / kLeastPages));
+      pieces = most_pieces(work, units, a.places);
+      cells = most_cells(work, a.places);
     } else {
       const int64_t chunk = ceil_div(work, 2 * a.places);
       a.chunk = (int)(chunk < 8 ? 8 : ceil_div(chunk, 4) * 4);

@@ -10,6 +10,7 @@
 // chain (its piece 2 us, the first page 2, each page 2.3, the end 2.7) about twice over.  24 sequences, 17 nodes, 8 heads of 80 channels, window 900, distances, float16, 16 us and 4.  One of 712 tokens, 12 nodes, 9.6 and 4.
 #pragma once
 #include "cache_kernels.hpp"
+#include "draft_pieces.hpp"
 
 namespace spg {
 
@@ -145,14 +146,8 @@ __device__ __forceinline__ TreePages tree_pages(const TreeAttendArgs& a, int s) 
   return r;
 }
 
-// What has to be done is units: a sequence's pages (those that its nodes see), a tile of its rows, a key head.  Long units are cut into pieces of about `per` pages, for which there are cells where the
-// pieces' sums wait to be joined.  Every workgroup finds `per` and its piece by itself, from the lengths of all sequences, a lane each; that is one chain of loads more or less as long as a search for its sequence would be.
-//
-// per: the card has `places` workgroups at once.  If they are to be done in k turns, pieces have at least work / (k places - units) pages (cutting makes at most work / per pieces more than there are
-// units), and cost k (per + kPieceCost) pages' time, kPieceCost for what a workgroup does beside its pages; the best k up to 4 is taken.  Where units are more than that, only what is longer than twice the average
-// is cut.  us in one turn | in two, four sequences of 60 nodes and 50 000 to 65 011 tokens 277 | 294 (in about 1.6, with pieces of 60 pages, 337), 48 sequences of up to 26 nodes and 4000 tokens 82 | 53: the constant takes the better one of both.
-constexpr int kMostEven = 512;     // sequences that a workgroup looks through
-constexpr int kLeastPages = 4, kPieceCost = 8, kMostTurns = 4;
+// Units of work and how they are cut: draft_pieces.hpp.  There are cells where the sums of cut units' pieces wait to be joined.  Every workgroup finds `per` and its piece by itself, from the lengths of all sequences, a lane
+// each; that is one chain of loads more or less as long as a search for its sequence would be.
 struct Piece {
   TreePages sp;                    // of its sequence
   int kv, tile, piece, pieces;     // pieces: of the unit; 0 where there is nothing to do
@@ -174,18 +169,6 @@ __device__ __forceinline__ int64_t of_lane(int64_t v, int lane) {
   return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, lane));
 }
 
-__device__ __forceinline__ int pages_of_piece(float work, float units, int places) {
-  float best = INFINITY;
-  int per = 0;
-#pragma unroll
-  for (int k = 1; k <= kMostTurns; ++k) {
-    const float room = (float)(k * places) - units;
-    // (in 24 digits the sums and the quotient are off by less than 2^-12 of them: what is added keeps the number of pieces within k places)
-    const float pages = fmaxf(ceilf(work * (1.0f + 0x1p-11f) * fast_rcp(room)), (float)kLeastPages), cost = (float)k * (pages + kPieceCost);
-    if (room > 0.0f && cost < best) { best = cost; per = (int)fminf(pages, 1e9f); }
-  }
-  return per ? per : (int)fminf(fmaxf(ceilf(2.0f * work * fast_rcp((float)places)), (float)kLeastPages), 1e9f);
-}
 // Piece number `at` of the list: those of cut units first, which take longest; sequence by sequence; of one its pieces, of those the key heads, of those the tiles.  By the whole wave.
 __device__ __forceinline__ Piece schedule(const TreeAttendArgs& a, int64_t at) {
   float work = 0.0f, units = 0.0f;
@@ -205,7 +188,7 @@ __device__ __forceinline__ Piece schedule(const TreeAttendArgs& a, int64_t at) {
     work += (float)pages * (float)tiles;
     units += (float)tiles;
   }
-  const int per = uniform(pages_of_piece(wave_total(work) * (float)a.c.heads, wave_total(units) * (float)a.c.heads, a.places));
+  const int per = uniform(pages_of_piece(wave_total(work) * (float)a.c.heads, wave_total(units) * (float)a.c.heads, a.places, [](float x) { return fast_rcp(x); }));
   Piece p{};
   int64_t before = 0;              // pieces of cut units, then of all, of the sequences before these 64
   for (int cut = 1; cut >= 0 && p.pieces == 0; --cut)

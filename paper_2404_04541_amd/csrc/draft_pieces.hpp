@@ -1,0 +1,44 @@
+// Into which pieces the pages of trees' attention are cut (plain C++: the host sizes a launch, and the kernels cut, by the same numbers).
+//
+// What has to be done is units: a sequence's pages (those that its nodes see), a tile of its rows, a key head.  `work` is the pages of all units.  Units of more than `per` pages are cut into pieces of about
+// as many.  The card has `places` workgroups at once.  If they are to be done in k turns, pieces have at least work / (k places - units) pages (cutting makes at most work / per pieces more than there are
+// units), and cost k (per + kPieceCost) pages' time, kPieceCost for what a workgroup does beside its pages; the best k up to 4 is taken.  us in one turn | in two, four sequences of 60 nodes and
+// 50 000 to 65 011 tokens 277 | 294 (in about 1.6, with pieces of 60 pages, 337), 48 sequences of up to 26 nodes and 4000 tokens 82 | 53: the constant takes the better one of both.
+//
+// But no piece is longer than twice the average of a place.  Where units nearly fill the turns, what is left of them would have long units stay whole (with one place left all the work goes to one piece), and where units
+// are more than that nothing else cuts them.
+#pragma once
+#include <cstdint>
+
+namespace spg {
+
+constexpr int kMostEven = 512;     // sequences that a workgroup looks through
+constexpr int kLeastPages = 4, kPieceCost = 8, kMostTurns = 4;
+
+// rcp: 1 / x in 32 bits.
+template <typename F>
+constexpr int pages_of_piece(float work, float units, int places, F rcp) {
+  float best = __builtin_inff(), per = __builtin_inff();
+#pragma unroll
+  for (int k = 1; k <= kMostTurns; ++k) {
+    const float room = (float)(k * places) - units;
+    // (in 24 digits the sums and the quotient are off by less than 2^-12 of them: what is added keeps the number of pieces within k places)
+    const float pages = __builtin_ceilf(work * (1.0f + 0x1p-11f) * rcp(room)), cost = (float)k * (__builtin_fmaxf(pages, (float)kLeastPages) + kPieceCost);
+    if (room > 0.0f && cost < best) { best = cost; per = pages; }
+  }
+  return (int)__builtin_fminf(__builtin_fmaxf(__builtin_fminf(per, __builtin_ceilf(2.0f * work * rcp((float)places))), (float)kLeastPages), 1e9f);
+}
+
+// Bounds that the host has, which knows how much work and how many units there are at most.  Pieces: with the k turns at most k places; with pieces of twice the average half a place more than the units for each; and never
+// more than the units and one for every kLeastPages pages.
+constexpr int64_t most_pieces(int64_t work, int64_t units, int places) {
+  const int64_t turns = (int64_t)kMostTurns * places, some = units + places, most = turns > some ? turns : some, each = units + work / kLeastPages;
+  return most < each ? most : each;
+}
+// Cells are for pieces of cut units alone: the k turns, or (a unit that is cut has at most two pieces for every `per` pages) a place each; and at most two for every kLeastPages pages.
+constexpr int64_t most_cells(int64_t work, int places) {
+  const int64_t turns = (int64_t)kMostTurns * places, each = 2 * (work / kLeastPages);
+  return turns < each ? turns : each;
+}
+
+}  // namespace spg

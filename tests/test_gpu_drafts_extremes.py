@@ -1,6 +1,7 @@
 """Drafted tokens at the ends of the ranges."""
 import ctypes as C
 import math
+import random
 
 import pytest
 import torch
@@ -10,7 +11,7 @@ from draft_helpers import keep_reference, tree_reference
 from paper_2404_04541_amd import attention as at
 from paper_2404_04541_amd import binding as sg
 from paper_2404_04541_amd import drafts as dr
-from test_gpu_drafts import filled, grown, i32, i64, planned, randn, rows_for
+from test_gpu_drafts import filled, grown, i32, i64, planned, randn, rows_for, sums
 
 pytestmark = pytest.mark.gpu
 BF = torch.bfloat16
@@ -124,3 +125,54 @@ def test_attend_rows_that_overlap_and_have_more_pieces_than_the_launch(h):
                                       at._tensor(q, "q"), at.TensorStruct(out.data_ptr(), 64, 64))
         torch.cuda.synchronize()
         assert rc == 0 and (out[512:] == 7.0).all() and torch.equal(cache.k, before[0]) and torch.equal(cache.v, before[1])
+
+
+def times(run, n=5):
+    """us of the fastest of n runs, after one that does not count."""
+    out = []
+    for _ in range(n + 1):
+        begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        begin.record()
+        run()
+        end.record()
+        torch.cuda.synchronize()
+        out.append(begin.elapsed_time(end) * 1e3)
+    return min(out[1:])
+
+
+def test_attend_one_long_sequence_among_nearly_as_many_as_fill_the_card(h):
+    """A few sequences fewer than four turns of the card take does not mean that the long one among them stays whole."""
+    gen = torch.Generator(device="cuda").manual_seed(15)
+    took = {}
+    cache = filled(16, 1, 3100, 8, 128)
+    for seqs in (200, 250, 255, 257):
+        lens, trees = [60000] + [500] * (seqs - 1), [grown(8, s) for s in range(seqs)]
+        table, plan, lengths = at.PageTable(*flat(rows_for(lens, 3100, 7))), planned(h, trees), i32(lens)
+        q = randn(gen, (8 * seqs, 8, 128), BF)
+        took[seqs] = times(lambda: dr.attend(h, cache, 0, table, lengths, plan, q))
+    assert max(took.values()) < 2 * took[257], took
+
+
+# places of workgroups are 768 for heads of up to 64 channels, else 512, with four turns: numbers of units on both sides of three and of four, in sequences of 8 key heads
+@pytest.mark.parametrize("seqs, d", [(190, 128), (193, 128), (254, 128), (255, 128), (256, 128), (300, 128), (287, 64), (383, 64), (384, 64), (385, 64), (512, 64), (520, 64), (520, 128)])
+@pytest.mark.parametrize("window", [0, 400])
+def test_attend_as_many_units_as_places(h, seqs, d, window):
+    """Long sequences among many short ones are cut, whether or not units fill the turns, with trees of more than 128 rows among them; sequences without tokens or nodes in between count as nothing."""
+    rng = random.Random(seqs + d)
+    some = sorted(rng.sample(range(seqs), 12))
+    empty = {s for s in some[6:9]}
+    trees = [[] if s in empty else grown(40 if s in some[:3] else 1 + s % 5, s, 2) for s in range(seqs + len(empty))]
+    lens = [2500 + 200 * s // seqs if s in some[1:5] else len(t) + rng.randint(1, 60) for s, t in enumerate(trees)]
+    lens[some[6]] = 0
+    pages = sum(-(-n // PAGE) for n in lens) + 1
+    cache, rows = filled(17, 1, pages, 8, d), rows_for(lens, pages, 8)
+    gen = torch.Generator(device="cuda").manual_seed(18)
+    q = randn(gen, (sum(map(len, trees)), 32, d), BF, 1.5)
+    o = dr.attend(h, cache, 0, at.PageTable(*flat(rows)), i32(lens), planned(h, trees), q, window=window)
+    ptr, host = sums(map(len, trees)), HostCache(cache, 0)
+    shown = sorted(set(some) | set(range(0, len(trees), 25)) | {len(trees) - 1})
+    for head in (0, 5, 7):
+        of = lambda t: torch.cat([t[ptr[s]:ptr[s + 1], 4 * head:4 * head + 4] for s in shown])  # noqa: E731
+        one = HostCache(cache, 0)
+        one.code, one.scale = [c[:, head:head + 1] for c in host.code], [c[:, head:head + 1] for c in host.scale]
+        check(f"head {head}", of(o), *tree_reference(one, [rows[s] for s in shown], [lens[s] for s in shown], [trees[s] for s in shown], of(q), 1 / math.sqrt(d), window=window))
