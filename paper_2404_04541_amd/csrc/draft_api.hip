@@ -121,9 +121,9 @@ int spdraft_attend(spgemm_handle h, const spcache* c, int64_t layer, const spgem
       pieces = most_pieces(work, units, a.places);
       cells = most_cells(work, a.places);
     } else {
-      const int64_t chunk = ceil_div(work, 2 * a.places);
-      a.chunk = (int)(chunk < 8 ? 8 : ceil_div(chunk, 4) * 4);
-      pieces = cells = (table->nnz / a.chunk + n) * c->kv_heads * a.tiles;
+      a.chunk = chunk_pages(work, a.places);
+      pieces = (table->nnz / a.chunk + n) * c->kv_heads * a.tiles;
+      cells = chunk_cell(table->nnz, a.chunk) * c->kv_heads * a.tiles;
     }
     if (pieces > 0xffffff - 128) return fail(h, SPGEMM_UNSUPPORTED, "too many pages");      // (2^32 threads are a launch's limit)
     const size_t part = align_up((size_t)cells * a.part_rows * room * sizeof(float)), ml = align_up((size_t)cells * a.part_rows * sizeof(float2)), cuts = n <= kMostEven ? (size_t)n * sizeof(int4) : 0;

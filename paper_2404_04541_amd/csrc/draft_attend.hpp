@@ -628,7 +628,7 @@ __global__ void __launch_bounds__(256, tree_resident(R)) k_tree_attend(TreeAtten
     if (piece < 0 || piece * a.chunk >= at.sp.last) return;
     at.begin = uniform(max(at.sp.first, (int)piece * a.chunk));
     at.end = uniform(min(at.sp.last, (int)(piece + 1) * a.chunk));
-    at.cell = at.sp.first / a.chunk == (at.sp.last - 1) / a.chunk ? -1 : number;
+    at.cell = at.sp.first / a.chunk == (at.sp.last - 1) / a.chunk ? -1 : ((chunk_cell(at.sp.at, a.chunk) + piece) * a.c.heads + at.kv) * a.tiles + at.tile;
   }
   const TreePages& sp = at.sp;
   at.rows = uniform(min(sp.tree.n * a.group - at.tile * kTreeRows, kTreeRows));
@@ -761,7 +761,7 @@ __global__ void __launch_bounds__(256) k_tree_join(TreeAttendArgs a) {
     } else {
       const int c0 = sp.first / a.chunk;
       pieces = (sp.last - 1) / a.chunk + 1 - c0;
-      cell0 = (sp.at / a.chunk + place.z + c0) * a.c.heads * a.tiles;
+      cell0 = (chunk_cell(sp.at, a.chunk) + c0) * a.c.heads * a.tiles;
       stride = (int64_t)a.c.heads * a.tiles;
     }
     if (pieces == 1) return;

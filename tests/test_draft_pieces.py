@@ -18,6 +18,8 @@ def lib(tmp_path_factory):
     src.write_text('#include "draft_pieces.hpp"\n'
                    'extern "C" int per(float work, float units, int places, float off) { return spg::pages_of_piece(work, units, places, [=](float x) { return 1.0f / x * (1.0f + off); }); }\n'
                    'extern "C" long long pieces(long long work, long long units, int places) { return spg::most_pieces(work, units, places); }\n'
+                   'extern "C" int chunk(long long work, int places) { return spg::chunk_pages(work, places); }\n'
+                   'extern "C" long long chunk_cell(long long at, int chunk) { return spg::chunk_cell(at, chunk); }\n'
                    'extern "C" long long cells(long long work, int places) { return spg::most_cells(work, places); }\n')
     so = d / "pieces.so"
     subprocess.run(["g++", "-std=c++17", "-O1", "-fPIC", "-shared", "-I", CSRC, "-o", str(so), str(src)], check=True)
@@ -25,6 +27,7 @@ def lib(tmp_path_factory):
     lib.per.argtypes = [C.c_float, C.c_float, C.c_int, C.c_float]
     lib.pieces.argtypes, lib.pieces.restype = [C.c_longlong, C.c_longlong, C.c_int], C.c_longlong
     lib.cells.argtypes, lib.cells.restype = [C.c_longlong, C.c_int], C.c_longlong
+    lib.chunk.argtypes, lib.chunk_cell.argtypes, lib.chunk_cell.restype = [C.c_longlong, C.c_int], [C.c_longlong, C.c_int], C.c_longlong
     return lib
 
 
@@ -62,3 +65,24 @@ def test_long_sequences_are_cut_whatever_the_number_of_the_others(lib, places):
     for seqs in range(2, 513):
         per, pieces, _, work, count = cut(lib, [(938, 8), (8, 8 * (seqs - 1))], places)
         assert min(per, 938) <= max(2.01 * work / places + 1, 8), (seqs, per)
+
+
+@pytest.mark.parametrize("places", PLACES)
+def test_chunks_have_cells_of_their_own(lib, places):
+    """Rows of a table one after another: the pieces of those that are cut have different cells, all within what the host asks for, and that is a few for each place of the card."""
+    rng = random.Random(places + 1)
+    for _ in range(300):
+        heads, tiles = rng.choice([1, 8, 16]), rng.choice([1, 2, 8])
+        rows = [rng.choice([0, 1, 2, 9, int(2 ** rng.uniform(0, 11))]) for _ in range(rng.randint(513, 900))]
+        if rng.random() < 0.3:
+            rows[rng.randrange(len(rows))] = rng.randint(1000, 40000)
+        nnz = sum(rows)
+        chunk = lib.chunk(nnz * heads * tiles, places)
+        at, end = 0, 0
+        for p in rows:
+            pieces, cell = -(-p // chunk), lib.chunk_cell(at, chunk)
+            if pieces > 1:
+                assert cell >= end
+                end = cell + pieces
+            at += p
+        assert end <= lib.chunk_cell(nnz, chunk) and lib.chunk_cell(nnz, chunk) * heads * tiles <= 4 * places

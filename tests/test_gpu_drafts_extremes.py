@@ -176,3 +176,33 @@ def test_attend_as_many_units_as_places(h, seqs, d, window):
         one = HostCache(cache, 0)
         one.code, one.scale = [c[:, head:head + 1] for c in host.code], [c[:, head:head + 1] for c in host.scale]
         check(f"head {head}", of(o), *tree_reference(one, [rows[s] for s in shown], [lens[s] for s in shown], [trees[s] for s in shown], of(q), 1 / math.sqrt(d), window=window))
+
+
+def held(handle):
+    return sum(t.numel() for t in handle._live.values())
+
+
+@pytest.mark.parametrize("most, window", [(64, 0), (256, 0), (64, 300)])
+def test_attend_memory_of_many_sequences(most, window):
+    """More sequences than every workgroup looks through: memory is for what is cut, so that one sequence more does not cost gigabytes."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    d, kv, heads, use = 128, 8, 64, {}
+    for seqs in (512, 600):
+        h = sg.Handle()
+        trees = [grown(1 + s % 3 + (40 if s % 200 == 9 else 0), s) for s in range(seqs)]
+        lens = [3000 + s if s % 97 == 5 else len(t) + s % 70 for s, t in enumerate(trees)]
+        pages = sum(-(-n // PAGE) for n in lens)
+        cache, rows = filled(12, 1, pages, kv, d), rows_for(lens, pages, 6)
+        q = randn(gen, (sum(map(len, trees)), heads, d), BF)
+        o = dr.attend(h, cache, 0, at.PageTable(*flat(rows)), i32(lens), planned(h, trees, most), q, window=window)
+        torch.cuda.synchronize()
+        use[seqs] = held(h)
+        some = [s for s in range(seqs) if s % 97 == 5 or s % 200 == 9 or s % 50 == 0]      # (long ones, large trees, others)
+        ptr = sums(map(len, trees))
+        of = lambda t: torch.cat([t[ptr[s]:ptr[s + 1], :8] for s in some])  # noqa: E731
+        host = HostCache(cache, 0)
+        host.code, host.scale = [c[:, :1] for c in host.code], [c[:, :1] for c in host.scale]
+        check(str(seqs), of(o), *tree_reference(host, [rows[s] for s in some], [lens[s] for s in some], [trees[s] for s in some], of(q), 1 / math.sqrt(d), window=window))
+    # a cell is 128 rows of 128 channels in 32 bits; four for each workgroup that the card holds
+    cells = 4 * 2 * torch.cuda.get_device_properties(0).multi_processor_count
+    assert use[600] <= cells * (128 * 128 * 4 + 128 * 8) + 2 ** 20, use
