@@ -41,10 +41,12 @@ constexpr int64_t most_cells(int64_t work, int places) {
   return turns < each ? turns : each;
 }
 
+constexpr int kLongest = 1 << 25;   // pages of a sequence: lengths are below 2^31
+
 // More sequences than a workgroup looks through: pieces are chunks of so many pages of a sequence, found by the table's row pointers (page `at` of the table is the sequence's first).
 constexpr int chunk_pages(int64_t work, int places) {
   const int64_t chunk = (work + 2 * (int64_t)places - 1) / (2 * (int64_t)places);
-  return (int)(chunk < 8 ? 8 : (chunk + 3) / 4 * 4);
+  return (int)(chunk < 8 ? 8 : chunk < kLongest ? (chunk + 3) / 4 * 4 : kLongest);
 }
 // Cells again for what is cut alone: p pages make ceil(p / chunk) pieces, which is at most floor(2 p / chunk) where it is more than one; so sequences have places of their own by their begins, and all together at
 // most four for each place of the card, however many they are.

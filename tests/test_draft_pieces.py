@@ -86,3 +86,11 @@ def test_chunks_have_cells_of_their_own(lib, places):
                 end = cell + pieces
             at += p
         assert end <= lib.chunk_cell(nnz, chunk) and lib.chunk_cell(nnz, chunk) * heads * tiles <= 4 * places
+
+
+def test_chunks_of_very_large_tables(lib):
+    """Pages of all rows, key heads and tiles go far beyond 32 bits; a chunk is never longer than a sequence can be."""
+    for places in PLACES:
+        for work in (1, 2 ** 20, 2 ** 35, 2 ** 35 + 1, 2 ** 41, 2 ** 42, 2 ** 57):
+            chunk = lib.chunk(work, places)
+            assert 8 <= chunk <= 2 ** 25 and chunk % 4 == 0 and (chunk == 2 ** 25 or chunk * 2 * places >= work), (work, places)
