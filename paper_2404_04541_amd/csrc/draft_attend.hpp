@@ -656,6 +656,7 @@ __global__ void __launch_bounds__(256, tree_resident(R)) k_tree_attend(TreeAtten
   struct Joined {
     float ms[4][32], ls[4][32], by[4][32];             // by: what a wave's sums of a row are multiplied by
     int64_t to[kTreeRows];                             // bytes from the results' first element, of a row that is written there
+    unsigned long long nan[R];                         // of a page's channels: the tokens whose value is NaN
     __align__(16) float sums[4][32][R + 4];
   };
   __shared__ __align__(16) union { TreeTiles<T, R> tiles; Joined joined; } lds;
@@ -679,25 +680,34 @@ __global__ void __launch_bounds__(256, tree_resident(R)) k_tree_attend(TreeAtten
     }
   __syncthreads();
   if (strange) {
-    // rows that see a value that is NaN: looked up element by element
-    for (int i = threadIdx.x; i < at.rows * R; i += 256) {
-      const int row = i / R, d = i % R, rt = at.tile * kTreeRows + row;
-      const int64_t its = sp.tree.first + rt / a.group;
-      const int stands = sp.ctx + a.trees.node[its].w;
-      for (int n = at.begin; n < at.end; ++n) {
-        const int64_t page = a.t.page[sp.at + n];
-        if (page < 0 || page >= a.c.pages) continue;
-        const int k0 = n * kPage;
+    // rows that see a value that is NaN: of every page whose values were made proper the tokens that are, channel by channel, and then two threads a row.  (Of pages that all rows see the product has made the rows NaN.)
+    const int last_lo = a.window ? sp.ctx + sp.tree.n - a.window : 0, rt = threadIdx.x / 2;
+    for (int n = at.begin; n < at.end; ++n) {
+      const int k0 = n * kPage;
+      const int64_t page = a.t.page[sp.at + n];
+      if ((k0 + kPage <= sp.ctx && k0 >= last_lo) || page < 0 || page >= a.c.pages) continue;
+      if (threadIdx.x < R) {
+        const u32x4* v = reinterpret_cast<const u32x4*>(a.c.v + (page * a.c.heads + at.kv) * (kPage * R) + threadIdx.x * kPage);
+        unsigned long long nan = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const u32x4 w = v[i];
+#pragma unroll
+          for (int b = 0; b < 4; ++b) nan |= (unsigned long long)((nan_bytes(w[b]) >> 7) * 0x10204080u >> 28) << (16 * i + 4 * b);      // (a bit for each byte)
+        }
+        j.nan[threadIdx.x] = nan;
+      }
+      __syncthreads();
+      if (rt < at.rows) {
+        const int64_t its = sp.tree.first + (at.tile * kTreeRows + rt) / a.group;
+        const int stands = sp.ctx + a.trees.node[its].w;
         const unsigned long long sees = seen_context(min(max(sp.ctx - k0, 0), kPage), a.window ? stands - a.window + 1 - k0 : 0) |
                                         seen_nodes(a.trees.up + its * a.trees.words, a.trees.words, k0 - sp.ctx, a.window).bits;
-        const unsigned* v = reinterpret_cast<const unsigned*>(a.c.v + (page * a.c.heads + at.kv) * (kPage * R) + d * kPage);
-        for (int w = 0; w < kPage / 4; ++w) {
-          const unsigned bits = (unsigned)(sees >> (4 * w)) & 15u, nan = nan_bytes(v[w]) >> 7;
-          if (bits & ((nan & 1) | (nan >> 7 & 2) | (nan >> 14 & 4) | (nan >> 21 & 8))) j.sums[row / 32][row % 32][d] = NAN;
-        }
+        for (int d = threadIdx.x % 2; d < R; d += 2)
+          if (sees & j.nan[d]) j.sums[rt / 32][rt % 32][d] = NAN;
       }
+      __syncthreads();
     }
-    __syncthreads();
   }
   const int row = threadIdx.x;
   if (row < at.rows) {

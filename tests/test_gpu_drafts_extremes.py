@@ -206,3 +206,17 @@ def test_attend_memory_of_many_sequences(most, window):
     # a cell is 128 rows of 128 channels in 32 bits; four for each workgroup that the card holds
     cells = 4 * 2 * torch.cuda.get_device_properties(0).multi_processor_count
     assert use[600] <= cells * (128 * 128 * 4 + 128 * 8) + 2 ** 20, use
+
+
+def test_attend_one_nan_among_drafted_values_costs_little(h):
+    """A drafted value that is NaN is looked for in the pages that some node does not see as a whole, not in a whole context."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    lens, trees = [40000, 39000], [grown(60, 8, 4), grown(50, 9, 4)]
+    cache, rows = filled(10, 1, 1260, 4, 128), rows_for(lens, 1260, 5)
+    table, plan, lengths, q = at.PageTable(*flat(rows)), planned(h, trees), i32(lens), randn(gen, (110, 16, 128), BF)
+    run = lambda: dr.attend(h, cache, 0, table, lengths, plan, q)  # noqa: E731
+    clean, before = run(), times(run)
+    token = lens[0] - 1
+    cache.v[0, rows[0][token // PAGE], 0, 5, token % PAGE] = 0x7F
+    assert (run().isnan() != clean.isnan()).sum() == 4                  # (the last node, the four heads of key head 0, a channel)
+    assert times(run) < 1.5 * before + 20
