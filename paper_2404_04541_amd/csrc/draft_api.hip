@@ -35,7 +35,7 @@ TreeView carve_trees(const spdraft_trees* t, void* mem, size_t* bytes, int** err
   TreeView v{};
   v.ptr = t->ptr; v.rows = (int)t->rows; v.most = t->most; v.words = (int)ceil_div(t->most, 64); v.tokens = t->tokens;
   *error = c.take<int>(1);
-  v.node = c.take<int4>(t->tokens);
+  v.node = c.take<TreeNode>(t->tokens);
   v.place = c.take<int4>(t->tokens);
   v.up = c.take<unsigned long long>(t->tokens * v.words);
   *bytes = c.used;

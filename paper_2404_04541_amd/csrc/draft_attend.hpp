@@ -16,12 +16,13 @@ namespace spg {
 
 constexpr int kMostNodes = 256, kNodeWords = kMostNodes / 64;
 
+struct TreeNode { int parent, eldest, depth; };      // parent: -1 without one; eldest: the parent's first child
 struct TreeView {
   const int64_t* ptr;             // rows + 1
   int rows, most, words;          // words: of 64 bits, that a node's ancestors take
   int64_t tokens;
   unsigned long long* up;         // [tokens][words]: the node's ancestors and itself
-  int4* node;                     // [tokens]: parent and first child (-1: none), the first child of the parent, depth
+  TreeNode* node;                 // [tokens]
   int4* place;                    // [tokens]: the first of the node's tree, how many it has (0: a node of none), its sequence
 };
 
@@ -82,8 +83,7 @@ __global__ void __launch_bounds__(kMostNodes) k_trees(TreeView t, const int32_t*
     depth += __popcll(up[w]);
     if (w < t.words) t.up[(tree.first + i) * t.words + w] = up[w];
   }
-  const int first = child[i];
-  t.node[tree.first + i] = make_int4(p, first < kMostNodes ? first : -1, p >= 0 ? child[p] : i, depth);
+  t.node[tree.first + i] = TreeNode{p, p >= 0 ? child[p] : i, depth};
   t.place[tree.first + i] = make_int4((int)tree.first, tree.n, (int)blockIdx.x, 0);
 }
 
@@ -270,7 +270,7 @@ struct TreeRows {
     scale2 = CAP ? a.score.scale / a.score.cap * (2.0f * kLog2e) : a.score.scale * kLog2e;
     cap2 = a.score.cap * kLog2e;
     slope2 = BIAS && real ? a.score.slopes[head] * kLog2e : 0.0f;
-    diag = sp.ctx + (real ? a.trees.node[token].w : 0);
+    diag = sp.ctx + (real ? a.trees.node[token].depth : 0);
     row_lo = a.window ? diag - a.window + 1 : 0;
   }
 
@@ -700,7 +700,7 @@ __global__ void __launch_bounds__(256, tree_resident(R)) k_tree_attend(TreeAtten
       __syncthreads();
       if (rt < at.rows) {
         const int64_t its = sp.tree.first + (at.tile * kTreeRows + rt) / a.group;
-        const int stands = sp.ctx + a.trees.node[its].w;
+        const int stands = sp.ctx + a.trees.node[its].depth;
         const unsigned long long sees = seen_context(min(max(sp.ctx - k0, 0), kPage), a.window ? stands - a.window + 1 - k0 : 0) |
                                         seen_nodes(a.trees.up + its * a.trees.words, a.trees.words, k0 - sp.ctx, a.window).bits;
         for (int d = threadIdx.x % 2; d < R; d += 2)

@@ -172,13 +172,13 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_nodes(VerifyArgs a) {
     float px = 0.0f, qx = 0.0f, ux = 0.0f;
     if (i < kMostNodes) {
       if (i < tree.n && i / 64 < a.trees.words && a.trees.up[token * a.trees.words + i / 64] >> (i % 64) & 1) {
-        const int4 at = a.trees.node[tree.first + i];
-        if (at.x < 0 || at.x >= tree.n || at.z >= tree.n) barred = i != 0;
-        else barred = first_taken<T, DRAFT>(a, tree.first + at.x, tree.first + at.z) != (at.z == i);
+        const TreeNode at = a.trees.node[tree.first + i];
+        if (at.parent < 0 || at.parent >= tree.n || at.eldest >= tree.n) barred = i != 0;
+        else barred = first_taken<T, DRAFT>(a, tree.first + at.parent, tree.first + at.eldest) != (at.eldest == i);
       }
     } else if (i < 2 * kMostNodes) {
       i -= kMostNodes;
-      if (i < tree.n && a.trees.node[tree.first + i].x == node) {
+      if (i < tree.n && a.trees.node[tree.first + i].parent == node) {
         x = a.ids[tree.first + i];
         mine = x >= 0 && x < a.vocab;
         if (mine) {
