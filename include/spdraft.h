@@ -74,7 +74,7 @@ int spdraft_verify(spgemm_handle h, const spdraft_trees* t, const void* plan_mem
  * that entry.  A token that comes from another page is rounded under the scale of its new page, which grows as with spcache_append where the token does not
  * fit; the tokens before and beside it are then rounded again.  Bytes behind the tokens that stay are left as they were.  A sequence with
  * fewer tokens than its tree, or whose table lacks pages that the tree's nodes lie in, is left as it is, new_lens[s] = lens[s].
- * Pages that hold a tree's nodes belong to its sequence alone.  new_lens: device, rows; not lens itself. */
+ * Pages that hold a tree's nodes belong to its sequence alone.  new_lens: device, rows; it must not overlap lens, path or kept. */
 int spdraft_keep(spgemm_handle h, const spcache* c, const spgemm_csr* table, const int32_t* lens, const spdraft_trees* t, const int32_t* path, const int32_t* kept,
                  int32_t* new_lens);
 

@@ -192,9 +192,10 @@ int spdraft_keep(spgemm_handle h, const spcache* c, const spgemm_csr* table, con
     if ((rc = check_table(h, c, table, lens)) || (rc = check_trees(h, t)) || (rc = check_rows(h, table, t))) return rc;
     if (t->rows == 0) return SPGEMM_OK;
     if (!kept || !new_lens || (t->tokens > 0 && !path)) return fail(h, SPGEMM_INVALID_ARG, "null array");
-    if (new_lens == lens) return fail(h, SPGEMM_INVALID_ARG, "new_lens must not be lens");
     if (c->layers * 2 > 65535) return fail(h, SPGEMM_UNSUPPORTED, "too many layers");
     if (t->rows * c->kv_heads * c->layers * 2 > 0xffffff) return fail(h, SPGEMM_UNSUPPORTED, "too many sequences, heads and layers");      // (2^32 threads are a launch's limit)
+    auto overlaps = [&](const int32_t* p, int64_t n) { return new_lens < p + n && p < new_lens + t->rows; };
+    if (overlaps(lens, t->rows) || overlaps(kept, t->rows) || overlaps(path, t->tokens)) return fail(h, SPGEMM_INVALID_ARG, "new_lens must not overlap lens, path or kept");
     if ((rc = ensure_device(h))) return rc;
     KeepArgs a{};
     a.data[0] = static_cast<unsigned char*>(c->k); a.data[1] = static_cast<unsigned char*>(c->v);

@@ -126,6 +126,19 @@ def test_keep_is_refused(dr, h, parts):
     assert keep(t=trees(dr, rows=0, tokens=0), tab=table(rows=0)) == 0
 
 
+def test_keep_into_its_inputs_is_refused(dr, h, parts):
+    """Every workgroup of a sequence reads its length, its path and how much of it stays, and one writes the new length: that may lie in none of them."""
+    cache, table, _ = parts
+    lib, at = dr._lib(), dict(lens=1024, path=2048, kept=4096)
+
+    def keep(out):
+        return lib.spdraft_keep(h, cache(), table(), C.c_void_p(at["lens"]), C.byref(trees(dr)), C.c_void_p(at["path"]), C.c_void_p(at["kept"]), C.c_void_p(out))
+
+    for name, size in (("lens", 8), ("path", 40), ("kept", 8)):
+        for out in range(at[name] - 4, at[name] + size, 4):
+            assert keep(out) == INVALID_ARG, (name, out)
+
+
 def test_read_is_refused(dr, h, parts):
     cache, table, tensor = parts
     lib, p, good = dr._lib(), C.c_void_p(256), tensor(1024, 512, 64)
