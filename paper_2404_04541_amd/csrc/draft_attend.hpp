@@ -570,24 +570,20 @@ __device__ __forceinline__ bool tree_many_rows(const TreeAttendArgs& a, const Tr
     if (page >= 0 && busy) {
       const unsigned char *kt = tiles.k[from], *vt = tiles.v[from];
       f32x16 x[2];
-      __builtin_amdgcn_s_setprio(1);                 // (matrix instructions before the vector ones of the unit's other wave: 60 nodes over 65 011 tokens 284 | 272 us)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         x[t] = f32x16{};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) x[t] = mma(SK::template row<T>(kt, k_base, 32 * t, i), q[i], x[t]);
       }
-      __builtin_amdgcn_s_setprio(0);
       const bool whole = whole_page(n);
       vec8<f16_t> p[4];
       rows.template weigh<8>(a, sp, x, n * kPage, whole, ks, vs, half, p);
-      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int j = 0; j < kBlocks; ++j)
 #pragma unroll
         for (int u = 0; u < 4; ++u) rows.acc[j] = mma(SV::template row<f16_t>(vt, v_base, 32 * j, u), p[u], rows.acc[j]);
     }
-    __builtin_amdgcn_s_setprio(0);
     if (next >= 0) {
       store(n + 1, from ^ 1);
       ks = uniform_of(scales.k);
