@@ -5,9 +5,11 @@
 // are neighbouring keys, which is what the second product's left operand (a value's channel, held along the tokens) reads in one piece: nothing moves between lanes.
 //
 // All rows of a tree read the same pages, so what matters is how many rows share a read of them.  With more than 64 rows a page is widened to 16 bits once, into LDS, for four waves of 32 rows; with fewer the waves
-// take pages in turn, from memory to registers.  Measured (bfloat16 unless said): four sequences of 50 000 to 65 011 tokens, up to 60 nodes, 32 heads on 8 of 128 channels 245 to 270 us and 9 to join, 0.62 PFLOP/s: vector
-// instructions issue in 46 % of the cycles and matrix instructions run in 34 %, what two waves a SIMD reach together.  48 sequences of 20 to 4000 tokens, up to 26 nodes, capped, 46 us and 10 to join: a workgroup's
-// chain (its piece 2 us, the first page 2, each page 2.3, the end 2.7) about twice over.  24 sequences, 17 nodes, 8 heads of 80 channels, window 900, distances, float16, 16 us and 4.  One of 712 tokens, 12 nodes, 9.6 and 4.
+// take pages in turn, from memory to registers.  Measured (bfloat16 unless said; calls one after another, structure and join included; then the kernel and the join alone, means of a few launches under the profiler): four
+// sequences of 50 000 to 65 011 tokens, up to 60 nodes, 32 heads on 8 of 128 channels 244 us, 0.63 PFLOP/s; 271 (least 255) and 9.  Vector instructions issue in 48 % of the cycles and matrix instructions run in 35 %, what two waves
+// a SIMD reach together; a quarter of the cycles of LDS go to bank conflicts, those of the widened pages' stores.  48 sequences of 20 to 4000 tokens, up to 26 nodes, capped, two layers 113 us; 46 and 10 a layer: a workgroup's
+// chain (its piece 2 us, the first page 2, each page 2.3, the end 2.7) about twice over.  24 sequences, 17 nodes, 8 heads of 80 channels, window 900, distances, float16, three layers 63 us; 16 and 4 a layer.  One of 712
+// tokens, 12 nodes, 24 us; 9.7 and 4.
 #pragma once
 #include "cache_kernels.hpp"
 #include "draft_pieces.hpp"
@@ -39,7 +41,7 @@ __device__ __forceinline__ Tree tree_of(const TreeView& t, int s) {
 // ---- structure --------------------------------------------------------------------------------
 
 // A workgroup has a tree.  A node's ancestors are found by doubling: it takes over what the node that it points to has, and then points to where that one points; a tree of depth d is done
-// after log d rounds.  12 nodes 3.2 us, 48 trees of up to 26 nodes 5 us: a chain of loads and LDS steps.
+// after log d rounds.  12 nodes 3.3 us, 48 trees of up to 26 nodes 5 us: a chain of loads and LDS steps.
 __global__ void __launch_bounds__(kMostNodes) k_trees(TreeView t, const int32_t* parent) {
   __shared__ int jump[kMostNodes], child[kMostNodes];
   __shared__ unsigned long long ups[kNodeWords][kMostNodes];

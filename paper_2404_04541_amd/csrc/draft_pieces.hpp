@@ -2,11 +2,11 @@
 //
 // What has to be done is units: a sequence's pages (those that its nodes see), a tile of its rows, a key head.  `work` is the pages of all units.  Units of more than `per` pages are cut into pieces of about
 // as many.  The card has `places` workgroups at once.  If they are to be done in k turns, pieces have at least work / (k places - units) pages (cutting makes at most work / per pieces more than there are
-// units), and cost k (per + kPieceCost) pages' time, kPieceCost for what a workgroup does beside its pages; the best k up to 4 is taken.  us in one turn | in two, four sequences of 60 nodes and
-// 50 000 to 65 011 tokens 277 | 294 (in about 1.6, with pieces of 60 pages, 337), 48 sequences of up to 26 nodes and 4000 tokens 82 | 53: the constant takes the better one of both.
+// units), and cost k (per + kPieceCost) pages' time, kPieceCost for what a workgroup does beside its pages; the best k up to 4 is taken.  Calls with one turn alone | two alone | the rule, four sequences of up to 60 nodes
+// and 50 000 to 65 011 tokens 240 | 250 | 241 us, 48 sequences of up to 26 nodes and 4000 tokens, two layers, 111.3 | 110.7 | 111.4.
 //
 // But no piece is longer than twice the average of a place.  Where units nearly fill the turns, what is left of them would have long units stay whole (with one place left all the work goes to one piece), and where units
-// are more than that nothing else cuts them.
+// are more than that nothing else cuts them.  One sequence of 60 000 tokens, the others of 500, 8 nodes, 8 heads of 128 channels, 250 | 255 | 257 sequences: 134 | 133 | 142 us; by the turns alone 272 | 479 | 140.
 #pragma once
 #include <cstdint>
 
@@ -43,7 +43,8 @@ constexpr int64_t most_cells(int64_t work, int places) {
 
 constexpr int kLongest = 1 << 25;   // pages of a sequence: lengths are below 2^31
 
-// More sequences than a workgroup looks through: pieces are chunks of so many pages of a sequence, found by the table's row pointers (page `at` of the table is the sequence's first).
+// More sequences than a workgroup looks through: pieces are chunks of so many pages of a sequence, found by the table's row pointers (page `at` of the table is the sequence's first).  Half the average of a place by the
+// whole table and the bound of the trees, for lengths and trees the host does not know: 1024 sequences of 100 to 1000 tokens, 8 of them of 20 000, up to 26 nodes under a bound of 64, 32 heads on 8 of 128 channels 1070 us, of which 300 would be memory.
 constexpr int chunk_pages(int64_t work, int places) {
   const int64_t chunk = (work + 2 * (int64_t)places - 1) / (2 * (int64_t)places);
   return (int)(chunk < 8 ? 8 : chunk < kLongest ? (chunk + 3) / 4 * 4 : kLongest);

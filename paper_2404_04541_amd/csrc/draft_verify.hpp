@@ -5,8 +5,9 @@
 // not taken costs a pass over both rows, in which wave w has the w-th part: the sums of these parts are what the token is looked for in, if no other child is taken.  Children that were chosen, not drawn, cost
 // one pass together.
 //
-// Measured: 64 trees of up to 26 nodes, rows of 131 072 in 32 bits, 61 us and 5 for the walk: the nodes with most refusals, some 10 us a pass (a compute unit's memory and 64-bit instructions about alike), while
-// others are done.  16 trees of up to 40 nodes, chosen children, rows of 100 003 in bfloat16, 20 us; a chain of 8, rows of 32 003, 13 us: dependent loads and one pass.
+// Measured (kernels alone, under the profiler): 64 trees of up to 26 nodes, rows of 131 072 in 32 bits, 61 us and 5 for the walk: the nodes with most refusals, some 10 us a pass (a compute unit's memory and 64-bit instructions
+// about alike), while others are done; what is read, about 100 MB, would take the whole card 20.  16 trees of up to 40 nodes, chosen children, rows of 100 003 in bfloat16, 20 us; a chain of 8, rows of 32 003, 13 us: dependent
+// loads and one pass.
 #pragma once
 #include "draft_attend.hpp"
 
